@@ -386,6 +386,151 @@ entro_status entro_encode_device(const uint8_t *q, uint64_t n, const entro_codeb
  * small), ENTRO_ERR_SIZE (the stream would reach 4 GiB). */
 entro_status entro_encode_device_status(uint32_t status_word);
 
+/* ------------------------------------------------ device side: the token cache
+ * Token generation reads, after the weights, the keys and values of every token
+ * so far ("Latency Reduction from Huffman Coding": the phase is bound by bytes
+ * read).  These calls keep them in 8 bits, on Eq. 1's grid with a zero-point of
+ * 128 and one scale for each block of tokens and head, attend over them, and
+ * move their blocks.  What goes in (keys and values of new tokens) may be the
+ * fp32 or bf16 output of a product; what comes out may be the x of the next.
+ *
+ *   - A pool (entro_cache) holds pages of page_tokens tokens, for all layers:
+ *       k: codes [layers][pages][kv_heads][page_tokens][width]
+ *       v: codes [layers][pages][kv_heads][width][page_tokens]  (dimensions
+ *          first: the product with the probabilities takes tokens in a row)
+ *       k_scale, v_scale: float [layers][pages][kv_heads]
+ *     width = entro_cache_width(head_dim).  A value is (code - 128) * scale, code
+ *     1..255.  Bytes of dimensions head_dim.. are never looked at, nor are pages
+ *     that no table names: the pool needs no clearing.
+ *   - A table (entro_cache_table) names the pages of every sequence: slot j of
+ *     its row holds the page of positions j * page_tokens ...  An entry outside
+ *     [0, pages) stands for no page: its tokens are seen by no query.  All layers
+ *     share the table.
+ *   - Rows of several sequences lie one after the other in q, k, v and out:
+ *     rows start[b] .. start[b+1] - 1 belong to sequence b and are its LAST
+ *     positions, lengths[b] - count .. lengths[b] - 1 (lengths counts them, also
+ *     before entro_cache_append has written them).  Rows that no sequence has
+ *     are left alone.  Positions before 0, past the table's last slot or without a
+ *     page are not written (entro_cache_append), read as zeros (entro_cache_read)
+ *     and seen by no query (entro_cache_attend).
+ *   - max_new and max_len bound how many rows and tokens a sequence has.  They size
+ *     the launch and choose between kernels; results do not depend on them beyond
+ *     the order of sums, and they may be exceeded.
+ *   - Tables, lengths and starts are device memory that the kernels read, so that
+ *     a captured HIP graph can be replayed as they change.  All calls only enqueue
+ *     kernels.
+ */
+#define ENTRO_CACHE_MAX_DIM 256
+
+/* The pool.  Plain data, caller-owned. */
+typedef struct {
+    void *k, *v;                 /* device: codes, entro_cache_codes_bytes each */
+    float *k_scale, *v_scale;    /* device: [layers][pages][kv_heads] */
+    uint32_t layers, pages;
+    uint32_t page_tokens;        /* 16, 32, 64, 128 or 256 */
+    uint32_t kv_heads;
+    uint32_t head_dim;           /* 1 .. ENTRO_CACHE_MAX_DIM */
+    uint32_t reserved;           /* 0 */
+} entro_cache;
+
+/* Pages and lengths of the sequences. */
+typedef struct {
+    int32_t *slots;              /* device: [seqs][stride] page numbers */
+    int32_t *lengths;            /* device: [seqs] tokens */
+    uint32_t seqs, stride;
+} entro_cache_table;
+
+/* Keys and values of some rows, [tokens][kv_heads][head_dim] with strides in elements (dimensions lie side by side). */
+typedef struct {
+    void *k, *v;                 /* device: read by entro_cache_append, written by entro_cache_read */
+    uint64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+    const int32_t *start;        /* device: [seqs + 1] */
+    uint32_t tokens;             /* rows of k and v */
+    uint32_t max_new;            /* most rows a sequence has here */
+    uint32_t type;               /* ENTRO_F32 or ENTRO_BF16 */
+    uint32_t layer;
+} entro_cache_rows;
+
+/* Queries and results of some rows, [tokens][q_heads][head_dim] with strides in elements. */
+typedef struct {
+    const void *q;               /* device */
+    void *out;                   /* device: the type of q */
+    float *lse;                  /* device: [tokens][q_heads], or NULL */
+    uint64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride;
+    const int32_t *start;        /* device: [seqs + 1] */
+    uint32_t tokens;             /* rows of q and out */
+    uint32_t max_new, max_len;   /* most rows and most tokens a sequence has */
+    uint32_t q_heads;            /* a multiple of kv_heads: query head h reads head h / (q_heads / kv_heads) */
+    uint32_t type;               /* ENTRO_F32 or ENTRO_BF16 */
+    uint32_t layer;
+    uint32_t window, sinks;      /* window 0: a query sees all tokens up to its own; otherwise the last `window` of them and the first `sinks` of all */
+    float scale;                 /* of the products, 1 / sqrt(head_dim) as a rule */
+    uint32_t reserved;           /* 0 */
+} entro_cache_query;
+
+/* Host: bytes a dimension row takes in the pool (the layouts on Eq. 1's grid given above): head_dim rounded up to 64, 96,
+ * 128, 192 or 256; 0 for a head_dim of 0 or above ENTRO_CACHE_MAX_DIM. */
+uint32_t entro_cache_width(uint32_t head_dim);
+
+/* Host: bytes of the codes (Eq. 1's integers) of k, and as many of v, that this pool needs; 0 if its sizes are not valid. */
+uint64_t entro_cache_codes_bytes(const entro_cache *c);
+
+/* Eq. 1's grid map for the keys and values of new tokens, into the pages of their positions.  For every block, head, and
+ * each of k and v:
+ *   a = the largest |x| among the block's new finite elements; s' = max(s, a / 127), s being the block's scale, or 0 if it
+ *   holds no tokens before the new ones; code = clamp(rint(x / s'), -127, 127) + 128;
+ *   where s' > s, the block's older codes c become rint((c - 128) * s / s') + 128.
+ * binary32 arithmetic, round-half-even, true division.  A NaN becomes 128 (the value 0), an infinity the end of the grid; s' = 0 makes
+ * all codes 128.  Writing the same rows again changes nothing.  A page must belong to one sequence at the positions
+ * written (entro_cache_regroup sees to that), and calls for one pool are to be ordered. */
+entro_status entro_cache_append(const entro_cache *c, const entro_cache_table *t, const entro_cache_rows *r, void *hip_stream);
+
+/* The inverse of Eq. 1's grid map for tokens of the cache: k and v rows receive (code - 128) * scale (bf16: rounded to
+ * nearest even), zeros where a position has no page. */
+entro_status entro_cache_read(const entro_cache *c, const entro_cache_table *t, const entro_cache_rows *r, void *hip_stream);
+
+/* Bytes of device workspace entro_cache_attend ("Latency Reduction from Huffman Coding": the phase's work split over the
+ * chip) needs for these sizes on the current device; may be 0.  Only max_new, max_len and sizes count, no pointer is followed. */
+uint64_t entro_cache_attend_workspace_bytes(const entro_cache *c, const entro_cache_table *t, const entro_cache_query *q);
+
+/* Attention of token generation and of prompts over the cache, whose 8-bit codes are read as they are ("Latency Reduction
+ * from Huffman Coding": fewer bytes read per token).  For the query at position i of a sequence and a query head:
+ *   out = sum_j p_j v_j, p = softmax_j(scale * q . k_j), lse = log(sum_j exp(scale * q . k_j)), over the positions j <= i that have a
+ *   page and, if window > 0, i - j < window or j < sinks.
+ * A query that sees nothing gets out 0 and lse -inf.  Sums are held in fp32.  bf16: q is taken exactly, probabilities
+ * are rounded to 11 bits before their product; fp32: q and probabilities keep at least 22 bits.
+ * The order of sums depends on sizes, never on the run. */
+entro_status entro_cache_attend(const entro_cache *c, const entro_cache_table *t, const entro_cache_query *q, void *workspace,
+                                uint64_t workspace_bytes, void *hip_stream);
+
+/* Bytes of device workspace the two calls below need (blocks of tokens as the segments of Fig. 3: independent pieces of known place). */
+uint64_t entro_cache_pages_workspace_bytes(const entro_cache *c, const entro_cache_table *t, const entro_cache_table *next);
+
+/* The table of the next step (each sequence's pages, like Fig. 3's segments, are found through a table alone, so that sequences can share them):
+ * row b of `next` goes on from row parent[b] of t (NULL: from row b; a value outside t: an empty row, the sequence has
+ * ended).  It keeps the first min(length, length + grow[b]) tokens (grow NULL: all) and, if window > 0, drops pages that no
+ * further query can see (entro_cache_query's window and sinks); its length becomes max(0, length + grow[b]), with pages for the
+ * tokens to come.  Pages are shared by all rows that keep them, except one that is only partly filled in a row, which must be that
+ * row's own: where several rows hold it, the lowest row keeps it, or none if to some row it is a full page, and the
+ * others get copies (of all layers).  New pages are the lowest free ones, rows in ascending order, a row's copy
+ * before what it grows by; free is what no row of `next` holds, so pages that only t holds may be overwritten.  `next`
+ * has buffers of its own.
+ * parent, grow: device, [next->seqs].  status: device, 16-byte aligned, int32[4]: status word, pages in use, free pages, copies.
+ * Where pages or slots do not suffice the status word says so (entro_cache_status), nothing is copied and `next` is not to be used. */
+entro_status entro_cache_regroup(const entro_cache *c, const entro_cache_table *t, const int32_t *parent, const int32_t *grow,
+                                 uint32_t window, uint32_t sinks, const entro_cache_table *next, int32_t *status, void *workspace,
+                                 uint64_t workspace_bytes, void *hip_stream);
+
+/* Brings the pages that t names to the front of the pool (as Fig. 3's segments lie back to back): with n pages in use, the
+ * i-th used page of number n or above moves to the i-th free page below n, in all layers.  `next` (buffers of its own, seqs
+ * and stride of t) receives the table that names them there; pages n.. can be given back once it is in use.  No page in use is overwritten.
+ * status: as above; its last word counts the pages moved. */
+entro_status entro_cache_compact(const entro_cache *c, const entro_cache_table *t, const entro_cache_table *next, int32_t *status,
+                                 void *workspace, uint64_t workspace_bytes, void *hip_stream);
+
+/* Host: the meaning of a status word of the two calls above (tables of Fig. 3's kind): ENTRO_OK or ENTRO_ERR_CAPACITY. */
+entro_status entro_cache_status(int32_t status_word);
+
 /* Text of the last HIP error seen by the calling thread ("" if none) (error reporting; no
  * passage of the paper defines it). */
 const char *entro_last_device_error(void);

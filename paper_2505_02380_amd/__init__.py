@@ -18,6 +18,9 @@ from .binding import (  # noqa: F401
     entro_last_device_error, encode_tensor, to_device,
     entro_range_device, entro_qparams_from_range, entro_scheme_for_range, entro_quantize_device, entro_encoded_bytes,
     entro_encode_device, entro_encode_device_status, compress_on_device,
+    Cache, CacheTable, CacheRows, CacheQuery,
+    entro_cache_width, entro_cache_append, entro_cache_read, entro_cache_attend_workspace_bytes, entro_cache_attend,
+    entro_cache_pages_workspace_bytes, entro_cache_regroup, entro_cache_compact, entro_cache_status,
     ENTRO_UNSIGNED, ENTRO_ASYMMETRIC, ENTRO_U8, ENTRO_U4_PACKED, ENTRO_F32, ENTRO_BF16,
     ENTRO_OP_DECODE, ENTRO_OP_DEQUANT, ENTRO_OP_GEMV,
 )

@@ -48,6 +48,30 @@ class Plan(C.Structure):
                 ("off_partials", C.c_uint64), ("off_fix", C.c_uint64)]
 
 
+class CCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("layers", C.c_uint32),
+                ("pages", C.c_uint32), ("page_tokens", C.c_uint32), ("kv_heads", C.c_uint32), ("head_dim", C.c_uint32),
+                ("reserved", C.c_uint32)]
+
+
+class CCacheTable(C.Structure):
+    _fields_ = [("slots", C.c_void_p), ("lengths", C.c_void_p), ("seqs", C.c_uint32), ("stride", C.c_uint32)]
+
+
+class CCacheRows(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_token_stride", C.c_uint64), ("k_head_stride", C.c_uint64),
+                ("v_token_stride", C.c_uint64), ("v_head_stride", C.c_uint64), ("start", C.c_void_p), ("tokens", C.c_uint32),
+                ("max_new", C.c_uint32), ("type", C.c_uint32), ("layer", C.c_uint32)]
+
+
+class CCacheQuery(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("out", C.c_void_p), ("lse", C.c_void_p), ("q_token_stride", C.c_uint64),
+                ("q_head_stride", C.c_uint64), ("out_token_stride", C.c_uint64), ("out_head_stride", C.c_uint64),
+                ("start", C.c_void_p), ("tokens", C.c_uint32), ("max_new", C.c_uint32), ("max_len", C.c_uint32),
+                ("q_heads", C.c_uint32), ("type", C.c_uint32), ("layer", C.c_uint32), ("window", C.c_uint32), ("sinks", C.c_uint32),
+                ("scale", C.c_float), ("reserved", C.c_uint32)]
+
+
 class EntroError(RuntimeError):
     def __init__(self, status: int, what: str):
         msg = f"{what}: {entro_status_string(status)} (status {status})"
@@ -76,6 +100,7 @@ def lib():
     L = C.CDLL(path)
     u8p, u64p, f32p = C.POINTER(C.c_uint8), C.POINTER(C.c_uint64), C.POINTER(C.c_float)
     cbp, tp, pp = C.POINTER(Codebook), C.POINTER(CTensor), C.POINTER(Plan)
+    kp, kt = C.POINTER(CCache), C.POINTER(CCacheTable)
     sig = {
         "entro_quantize": (C.c_int, [f32p, C.c_uint64, C.c_int, C.c_int, u8p, C.POINTER(QParams)]),
         "entro_build_codebook": (C.c_int, [u8p, C.c_uint64, C.c_int, cbp]),
@@ -114,6 +139,17 @@ def lib():
         "entro_encode_device": (C.c_int, [C.c_void_p, C.c_uint64, cbp, C.c_uint32, C.c_void_p, C.c_uint64, C.c_void_p,
                                           C.c_void_p, C.c_void_p]),
         "entro_encode_device_status": (C.c_int, [C.c_uint32]),
+        "entro_cache_width": (C.c_uint32, [C.c_uint32]),
+        "entro_cache_codes_bytes": (C.c_uint64, [kp]),
+        "entro_cache_append": (C.c_int, [kp, kt, C.POINTER(CCacheRows), C.c_void_p]),
+        "entro_cache_read": (C.c_int, [kp, kt, C.POINTER(CCacheRows), C.c_void_p]),
+        "entro_cache_attend_workspace_bytes": (C.c_uint64, [kp, kt, C.POINTER(CCacheQuery)]),
+        "entro_cache_attend": (C.c_int, [kp, kt, C.POINTER(CCacheQuery), C.c_void_p, C.c_uint64, C.c_void_p]),
+        "entro_cache_pages_workspace_bytes": (C.c_uint64, [kp, kt, kt]),
+        "entro_cache_regroup": (C.c_int, [kp, kt, C.c_void_p, C.c_void_p, C.c_uint32, C.c_uint32, kt, C.c_void_p, C.c_void_p,
+                                          C.c_uint64, C.c_void_p]),
+        "entro_cache_compact": (C.c_int, [kp, kt, kt, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p]),
+        "entro_cache_status": (C.c_int, [C.c_int32]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -130,7 +166,10 @@ EXPORTED = ["entro_quantize", "entro_build_codebook", "entro_codebook_from_count
             "entro_workspace_bytes", "entro_plan_init", "entro_plan_staging_bytes", "entro_plan_init_staged", "entro_plan_run", "entro_decode_batch",
             "entro_decode_dequant_batch", "entro_decode_gemv_batch", "entro_last_device_error",
             "entro_range_device", "entro_qparams_from_range", "entro_scheme_for_range", "entro_quantize_device",
-            "entro_encoded_bytes", "entro_encode_device", "entro_encode_device_status"]
+            "entro_encoded_bytes", "entro_encode_device", "entro_encode_device_status",
+            "entro_cache_width", "entro_cache_codes_bytes", "entro_cache_append", "entro_cache_read",
+            "entro_cache_attend_workspace_bytes", "entro_cache_attend", "entro_cache_pages_workspace_bytes", "entro_cache_regroup",
+            "entro_cache_compact", "entro_cache_status"]
 
 
 def _ptr(a: np.ndarray, t):
@@ -482,3 +521,159 @@ def entro_decode_dequant_batch(ts, out_type, workspace, stream=None):
 
 def entro_decode_gemv_batch(ts, y_type, workspace, stream=None):
     _batch("entro_decode_gemv_batch", ts, y_type, workspace, stream)
+
+
+# ------------------------------------------------------------------- the token cache
+def entro_cache_width(head_dim: int) -> int:
+    return int(lib().entro_cache_width(head_dim))
+
+
+def _need(ok: bool, what: str):
+    """The C side sees addresses only: shapes and types of tensors are looked at here."""
+    if not ok:
+        raise ValueError(what)
+
+
+def _rows_type(x, what: str) -> int:
+    import torch
+    _need(x.dtype in (torch.float32, torch.bfloat16), f"{what} is float32 or bfloat16")
+    return ENTRO_F32 if x.dtype == torch.float32 else ENTRO_BF16
+
+
+def _ints(x, n: Optional[int], what: str):
+    import torch
+    _need(x.dtype == torch.int32 and x.is_contiguous() and (n is None or x.numel() == n), f"{what} is a contiguous int32 tensor"
+          + ("" if n is None else f" of {n}"))
+    return x.data_ptr()
+
+
+class Cache:
+    """A pool of pages (include/entro.h has the layouts): the tensors, and the descriptor that the calls take."""
+
+    def __init__(self, k, v, k_scale, v_scale, page_tokens: int, head_dim: int):
+        import torch
+        width = entro_cache_width(head_dim)
+        _need(width > 0, "head_dim is 1..256")
+        _need(k.dim() == 5 and k.dtype == torch.uint8 and k.is_contiguous(), "k is uint8 [layers][pages][kv_heads][page_tokens][width]")
+        layers, pages, heads = k.shape[:3]
+        _need(tuple(k.shape[3:]) == (page_tokens, width), f"k's pages are [{page_tokens}][{width}]")
+        _need(tuple(v.shape) == (layers, pages, heads, width, page_tokens) and v.dtype == torch.uint8 and v.is_contiguous(),
+              "v is uint8 [layers][pages][kv_heads][width][page_tokens]")
+        for x in (k_scale, v_scale):
+            _need(tuple(x.shape) == (layers, pages, heads) and x.dtype == torch.float32 and x.is_contiguous(),
+                  "scales are float32 [layers][pages][kv_heads]")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.layers, self.pages, self.kv_heads, self.page_tokens, self.head_dim, self.width = layers, pages, heads, page_tokens, head_dim, width
+        self.c = CCache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), layers, pages, page_tokens, heads, head_dim, 0)
+
+    @classmethod
+    def empty(cls, layers: int, pages: int, kv_heads: int, page_tokens: int, head_dim: int, device="cuda") -> "Cache":
+        """A pool in newly allocated memory (which needs no clearing)."""
+        import torch
+        width = entro_cache_width(head_dim)
+        _need(width > 0, "head_dim is 1..256")
+        k = torch.empty(layers, pages, kv_heads, page_tokens, width, dtype=torch.uint8, device=device)
+        v = torch.empty(layers, pages, kv_heads, width, page_tokens, dtype=torch.uint8, device=device)
+        ks, vs = (torch.empty(layers, pages, kv_heads, dtype=torch.float32, device=device) for _ in "kv")
+        return cls(k, v, ks, vs, page_tokens, head_dim)
+
+
+class CacheTable:
+    """Page numbers int32 [seqs][slots] and lengths int32 [seqs] of sequences."""
+
+    def __init__(self, slots, lengths):
+        _need(slots.dim() == 2, "slots is [seqs][slots]")
+        self.slots, self.lengths = slots, lengths
+        self.c = CCacheTable(_ints(slots, None, "slots"), _ints(lengths, slots.shape[0], "lengths"), slots.shape[0], slots.shape[1])
+
+    @classmethod
+    def empty(cls, seqs: int, slots: int, device="cuda") -> "CacheTable":
+        """A table of empty sequences."""
+        import torch
+        return cls(torch.full((seqs, slots), -1, dtype=torch.int32, device=device), torch.zeros(seqs, dtype=torch.int32, device=device))
+
+
+def _row_strides(x, what: str):
+    _need(x.dim() == 3 and (x.shape[2] == 1 or x.stride(2) == 1), f"{what} is [tokens][heads][head_dim], its dimensions side by side")
+    return x.stride(0), x.stride(1)
+
+
+class CacheRows:
+    """Keys and values [tokens][kv_heads][head_dim] of the last tokens of sequences; start: int32 [seqs + 1]."""
+
+    def __init__(self, k, v, start, max_new: int, layer: int = 0):
+        _need(k.shape == v.shape and k.dtype == v.dtype, "k and v have one shape and type")
+        self.k, self.v, self.start = k, v, start
+        self.c = CCacheRows(k.data_ptr(), v.data_ptr(), *_row_strides(k, "k"), *_row_strides(v, "v"), _ints(start, None, "start"),
+                            k.shape[0], max_new, _rows_type(k, "k"), layer)
+
+
+class CacheQuery:
+    """Queries and results [tokens][q_heads][head_dim] of the last tokens of sequences; start: int32 [seqs + 1]; lse: float32
+    [tokens][q_heads] or None; scale None: 1 / sqrt(head_dim)."""
+
+    def __init__(self, q, out, start, max_new: int, max_len: int, lse=None, scale: Optional[float] = None, window: int = 0,
+                 sinks: int = 0, layer: int = 0):
+        import torch
+        _need(q.shape == out.shape and q.dtype == out.dtype, "q and out have one shape and type")
+        _need(lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == tuple(q.shape[:2])),
+              "lse is float32 [tokens][q_heads]")
+        _need(q.dim() == 3 and not any(n > 1 and s == 0 for n, s in zip(out.shape, out.stride())), "out's elements have places of their own")
+        self.q, self.out, self.start, self.lse = q, out, start, lse
+        self.c = CCacheQuery(q.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(), *_row_strides(q, "q"),
+                             *_row_strides(out, "out"), _ints(start, None, "start"), q.shape[0], max_new, max_len, q.shape[1],
+                             _rows_type(q, "q"), layer, window, sinks, q.shape[2] ** -0.5 if scale is None else scale, 0)
+
+
+def _same_heads(cache: Cache, table: CacheTable, x, start):
+    _need(x.shape[2] == cache.head_dim, f"rows have {cache.head_dim} dimensions")
+    _need(start.numel() == table.c.seqs + 1, f"start is [{table.c.seqs} + 1]")
+
+
+def entro_cache_append(cache: Cache, table: CacheTable, rows: CacheRows, stream=None):
+    _same_heads(cache, table, rows.k, rows.start)
+    _need(rows.k.shape[1] == cache.kv_heads, f"rows have {cache.kv_heads} heads")
+    _check(lib().entro_cache_append(C.byref(cache.c), C.byref(table.c), C.byref(rows.c), _stream_ptr(stream)), "entro_cache_append")
+
+
+def entro_cache_read(cache: Cache, table: CacheTable, rows: CacheRows, stream=None):
+    _same_heads(cache, table, rows.k, rows.start)
+    _need(rows.k.shape[1] == cache.kv_heads, f"rows have {cache.kv_heads} heads")
+    _check(lib().entro_cache_read(C.byref(cache.c), C.byref(table.c), C.byref(rows.c), _stream_ptr(stream)), "entro_cache_read")
+
+
+def entro_cache_attend_workspace_bytes(cache: Cache, table: CacheTable, query: CacheQuery) -> int:
+    return int(lib().entro_cache_attend_workspace_bytes(C.byref(cache.c), C.byref(table.c), C.byref(query.c)))
+
+
+def _workspace(ws):
+    """(address, bytes) of a workspace tensor."""
+    return (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
+
+
+def entro_cache_attend(cache: Cache, table: CacheTable, query: CacheQuery, workspace=None, stream=None):
+    _same_heads(cache, table, query.q, query.start)
+    _check(lib().entro_cache_attend(C.byref(cache.c), C.byref(table.c), C.byref(query.c), *_workspace(workspace), _stream_ptr(stream)),
+           "entro_cache_attend")
+
+
+def entro_cache_pages_workspace_bytes(cache: Cache, table: CacheTable, following: CacheTable) -> int:
+    return int(lib().entro_cache_pages_workspace_bytes(C.byref(cache.c), C.byref(table.c), C.byref(following.c)))
+
+
+def entro_cache_regroup(cache: Cache, table: CacheTable, following: CacheTable, status, workspace, parent=None, grow=None,
+                        window: int = 0, sinks: int = 0, stream=None):
+    """`following` receives the table of the next step; status: int32 device tensor of 4 (entro_cache_status reads its first word)."""
+    n = following.c.seqs
+    _check(lib().entro_cache_regroup(C.byref(cache.c), C.byref(table.c), None if parent is None else _ints(parent, n, "parent"),
+                                     None if grow is None else _ints(grow, n, "grow"), window, sinks, C.byref(following.c),
+                                     _ints(status, 4, "status"), *_workspace(workspace), _stream_ptr(stream)), "entro_cache_regroup")
+
+
+def entro_cache_compact(cache: Cache, table: CacheTable, following: CacheTable, status, workspace, stream=None):
+    _check(lib().entro_cache_compact(C.byref(cache.c), C.byref(table.c), C.byref(following.c), _ints(status, 4, "status"),
+                                     *_workspace(workspace), _stream_ptr(stream)), "entro_cache_compact")
+
+
+def entro_cache_status(word: int) -> int:
+    return int(lib().entro_cache_status(int(word)))

@@ -16,9 +16,12 @@ DEVICE_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang"
                 "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument"]
 
 
+DEVICE_SOURCES = ["entro_device", "entro_compress", "entro_cache", "entro_attend"]
+
+
 def sources():
-    return [os.path.join(CSRC, "entro_host.cpp"), os.path.join(CSRC, "entro_device.hip"),
-            os.path.join(CSRC, "entro_compress.hip"), os.path.join(INCLUDE, "entro.h")]
+    return [os.path.join(CSRC, "entro_host.cpp"), os.path.join(CSRC, "entro_cache.h"), os.path.join(INCLUDE, "entro.h"),
+            *(os.path.join(CSRC, name + ".hip") for name in DEVICE_SOURCES)]
 
 
 def up_to_date() -> bool:
@@ -29,20 +32,24 @@ def build(force: bool = True, verbose: bool = False) -> str:
     if not force and up_to_date():
         return LIB
     os.makedirs(BUILD, exist_ok=True)
-    host_o = os.path.join(BUILD, "entro_host.o")
-    dev_o = os.path.join(BUILD, "entro_device.o")
-    comp_o = os.path.join(BUILD, "entro_compress.o")
-    cmds = [
-        ["g++", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off", "-Wall", "-Wextra", "-pthread",
-         "-I", INCLUDE, "-c", os.path.join(CSRC, "entro_host.cpp"), "-o", host_o],
-        [HIPCC, *DEVICE_FLAGS, "-I", INCLUDE, "-c", os.path.join(CSRC, "entro_device.hip"), "-o", dev_o],
-        [HIPCC, *DEVICE_FLAGS, "-I", INCLUDE, "-c", os.path.join(CSRC, "entro_compress.hip"), "-o", comp_o],
-        [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, host_o, dev_o, comp_o, "-pthread"],
-    ]
+    objects = [os.path.join(BUILD, name + ".o") for name in ["entro_host", *DEVICE_SOURCES]]
+    cmds = [["g++", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off", "-Wall", "-Wextra", "-pthread",
+             "-I", INCLUDE, "-c", os.path.join(CSRC, "entro_host.cpp"), "-o", objects[0]]]
+    cmds += [[HIPCC, *DEVICE_FLAGS, "-I", INCLUDE, "-c", os.path.join(CSRC, name + ".hip"), "-o", o]
+             for name, o in zip(DEVICE_SOURCES, objects[1:])]
+    link = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objects, "-pthread"]
+    # the sources compile side by side
+    running = []
     for c in cmds:
         if verbose:
             print(" ".join(c), flush=True)
-        subprocess.check_call(c)
+        running.append((c, subprocess.Popen(c)))
+    failed = [(c, p.returncode) for c, p in running if p.wait() != 0]
+    if failed:
+        raise subprocess.CalledProcessError(failed[0][1], failed[0][0])
+    if verbose:
+        print(" ".join(link), flush=True)
+    subprocess.check_call(link)
     return LIB
 
 

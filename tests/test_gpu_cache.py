@@ -1,0 +1,486 @@
+"""The token cache's calls against their definitions in 64 bits, through the C ABI.
+
+Bounds of the attention, fixed before the first run: scores are sums of at most 256 products in fp32 of factors with 22 bits or
+more, so each is off by less than 2^-16 of the sum of its terms' sizes (`size`); that moves every probability by a relative 2^-15
+of it at most; probabilities carry a rounding of 2^-12 (bf16) or 2^-21 (fp32) of their own, sums over keys less than that again, and
+the result one of 2^-9 or 2^-24."""
+import numpy as np
+import pytest
+import torch
+
+import cache_reference as ref
+import paper_2505_02380_amd as E
+from paper_2505_02380_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def dev(x):
+    return torch.from_numpy(np.ascontiguousarray(x)).to(DEV)
+
+
+def ints(x):
+    return torch.tensor([int(i) for i in x], dtype=torch.int32, device=DEV)
+
+
+def rounded(x, kind):
+    return torch.from_numpy(x.astype(np.float32)).to(TYPES[kind]).float().numpy()
+
+
+def make(rng, seqs, lengths, heads, dim, page, layers=1, spare=3, slots=None):
+    """A pool of random bytes and a table whose pages are in no order."""
+    need = [-(-n // page) for n in lengths]
+    pages = sum(need) + spare
+    pool = ref.Pool(rng, layers, pages, heads, page, dim)
+    table = np.full((seqs, slots or max(max(need), 1)), -1, np.int32)
+    order = rng.permutation(pages)
+    at = 0
+    for b, n in enumerate(need):
+        table[b, :n] = order[at: at + n]
+        at += n
+    return pool, table
+
+
+def scales(rng, pool, table):
+    """Scales for the pages that a table names; all others keep NaN."""
+    named = np.unique(table[(table >= 0) & (table < pool.pages)])
+    for s, f in ((pool.k_scale, 0.04), (pool.v_scale, 0.02)):
+        s[:, named] = (f * np.exp(rng.standard_normal((s.shape[0], len(named), s.shape[2])))).astype(np.float32)
+
+
+def cache_of(pool):
+    return E.Cache(dev(pool.k), dev(pool.v), dev(pool.k_scale), dev(pool.v_scale), pool.page, pool.dim)
+
+
+def starts(counts):
+    return np.concatenate([[0], np.cumsum(counts)]).astype(int)
+
+
+def run_attend(cache, table, lengths, q, start, kind, window=0, sinks=0, layer=0, scale=None, max_new=None, max_len=None, lse=True,
+               q_dev=None, out_dev=None):
+    t = E.CacheTable(dev(table), ints(lengths))
+    qd = dev(q).to(TYPES[kind]) if q_dev is None else q_dev
+    out = torch.full_like(qd, 7.0) if out_dev is None else out_dev
+    ld = torch.full(qd.shape[:2], 7.0, device=DEV) if lse else None
+    counts = np.diff(start)
+    query = E.CacheQuery(qd, out, ints(start), int(counts.max()) if max_new is None else max_new,
+                         int(max(lengths)) if max_len is None else max_len, lse=ld, scale=scale, window=window, sinks=sinks, layer=layer)
+    need = E.entro_cache_attend_workspace_bytes(cache, t, query)
+    ws = torch.full((max(need, 16),), 0xFF, dtype=torch.uint8, device=DEV)
+    E.entro_cache_attend(cache, t, query, ws)
+    torch.cuda.synchronize()
+    return out, ld
+
+
+def check_attend(pool, table, lengths, q, start, kind, got, lse, scale, window=0, sinks=0, layer=0):
+    want, want_lse, weight, size = ref.attend(pool, table, lengths, q, start, scale, window, sinks, layer)
+    mine = np.zeros(len(q), bool)
+    mine[start[0]: start[-1]] = True
+    got = got.float().cpu().numpy().astype(np.float64)
+    eps_p, eps_out = (2.0 ** -11, 2.0 ** -8) if kind == "bf16" else (2.0 ** -19, 2.0 ** -22)
+    bound = (2.0 ** -15 * size[..., None] + eps_p) * weight + eps_out * np.abs(want) + 1e-30
+    off = np.abs(got - want)
+    assert np.all(np.isfinite(got))
+    assert np.all(off[mine] <= bound[mine]), (float((off[mine] / bound[mine]).max()), np.argwhere((off > bound) & mine[:, None, None])[:4])
+    if lse is not None:
+        lse = lse.cpu().numpy().astype(np.float64)
+        empty = np.isneginf(want_lse)
+        assert np.array_equal(np.isneginf(lse[mine]), empty[mine])
+        some = mine[:, None] & ~empty
+        limit = 2.0 ** -15 * size + 2.0 ** -20 * (1 + np.abs(np.where(empty, 0, want_lse)))
+        assert np.all(np.abs(lse - np.where(empty, 0, want_lse))[some] <= limit[some])
+
+
+#        seqs' lengths            new tokens           q, kv heads  dim  page  type   window sinks
+ATTEND = [
+    ([1],                        [1],                  4, 4,        64, 16, "bf16", 0, 0),
+    ([1, 2, 15, 16, 17, 0],      [1, 1, 1, 1, 1, 0],   8, 2,       128, 16, "bf16", 0, 0),
+    ([63, 64, 65, 128, 129],     [1, 1, 1, 1, 1],      4, 1,       128, 64, "f32", 0, 0),
+    ([700, 3, 511],              [1, 1, 1],            3, 3,        96, 32, "bf16", 0, 0),
+    ([300, 41],                  [1, 1],              14, 2,        80, 128, "f32", 0, 0),
+    ([900],                      [1],                  7, 1,       256, 256, "bf16", 0, 0),
+    ([333, 90],                  [1, 1],              32, 1,        64, 16, "bf16", 0, 0),
+    ([257, 100],                 [1, 1],               6, 3,         1, 16, "bf16", 0, 0),
+    ([257, 100],                 [1, 1],               2, 1,        33, 32, "f32", 0, 0),
+    ([140, 77],                  [1, 1],               5, 5,       192, 64, "bf16", 0, 0),
+    # several tokens: as a draft's are looked at, and prompts
+    ([130, 64, 9],               [3, 4, 2],            8, 2,       128, 64, "bf16", 0, 0),
+    ([90, 200, 5],               [5, 1, 5],            4, 4,        64, 16, "f32", 0, 0),
+    ([70],                       [70],                 4, 2,       128, 32, "bf16", 0, 0),
+    ([150, 3, 260, 40],          [150, 0, 33, 1],      8, 2,        96, 64, "bf16", 0, 0),
+    ([301],                      [129],                3, 1,       256, 16, "bf16", 0, 0),
+    ([201],                      [201],                2, 2,        72, 128, "f32", 0, 0),
+    ([140, 80],                  [65, 80],            10, 2,       192, 64, "f32", 0, 0),
+    ([97],                       [97],                40, 1,        64, 16, "bf16", 0, 0),
+    # windows: smaller than a tile, at its edge, sinks that meet the window or lie apart from it
+    ([500, 20],                  [1, 1],               8, 2,       128, 16, "bf16", 7, 0),
+    ([500, 20, 66],              [1, 1, 1],            8, 2,        64, 64, "bf16", 64, 4),
+    ([513],                      [1],                  4, 4,        96, 32, "f32", 100, 17),
+    ([300],                      [1],                  4, 1,       128, 64, "bf16", 1, 0),
+    ([300],                      [1],                  4, 1,       128, 64, "bf16", 250, 60),
+    ([300, 50],                  [300, 20],            4, 2,        64, 16, "bf16", 33, 5),
+    ([400],                      [150],                2, 1,       128, 128, "f32", 64, 64),
+    ([260],                      [260],                2, 1,       128, 32, "bf16", 1, 1),
+    ([260],                      [40],                 4, 1,       128, 32, "bf16", 1000, 3),
+]
+
+
+@pytest.mark.parametrize("case", range(len(ATTEND)))
+def test_attend_against_the_definition(case):
+    lengths, new, q_heads, heads, dim, page, kind, window, sinks = ATTEND[case]
+    rng = np.random.default_rng(1000 + case)
+    pool, table = make(rng, len(lengths), lengths, heads, dim, page)
+    scales(rng, pool, table)
+    start = starts(new)
+    q = rounded(rng.standard_normal((start[-1], q_heads, dim)) * 2, kind)
+    out, lse = run_attend(cache_of(pool), table, lengths, q, start, kind, window, sinks)
+    check_attend(pool, table, lengths, q, start, kind, out, lse, dim ** -0.5, window, sinks)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [[1, 1, 1], [40, 1, 9]])
+def test_attend_where_pages_are_missing_and_hints_are_too_small(kind, new):
+    """Pages that were given back (negative, or past the pool), a sequence without any, more tokens than the hints say, a table
+    that ends before the sequence does, rows around the sequences' own, and pools whose other pages hold NaN scales."""
+    rng = np.random.default_rng(7)
+    lengths = [210, 75, 130]
+    pool, table = make(rng, 3, lengths, 2, 64, 16, spare=9)
+    scales(rng, pool, table)
+    table[0, 2], table[0, 5], table[0, 6] = -1, pool.pages, 1 << 30
+    table[1] = -1
+    table = np.ascontiguousarray(table[:, :12])                           # 192 of the 210 tokens
+    pool.k_scale[:, [i for i in range(pool.pages) if i not in table]] = np.nan
+    start = starts(new) + 3
+    q = rounded(rng.standard_normal((start[-1] + 5, 6, 64)) * 2, kind)
+    q[:3] = q[start[-1]:] = np.nan
+    for max_new, max_len in ((1, 1), (500, 100000)):
+        out, lse = run_attend(cache_of(pool), table, lengths, q, start, kind, max_new=max_new, max_len=max_len)
+        got = out.float().cpu().numpy()
+        assert np.all(got[:3] == 7.0) and np.all(got[start[-1]:] == 7.0) and torch.all(lse[:3] == 7.0)
+        own = slice(start[0], start[-1])
+        check_attend(pool, table, lengths, q[own], start - 3, kind, out[own], lse[own], 64 ** -0.5)
+        empty = slice(start[1], start[2])
+        assert np.all(got[empty] == 0) and torch.all(torch.isneginf(lse[empty]))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_attend_with_strides_layers_and_starts_that_lie(kind):
+    """q inside a wider product's rows, out with heads before tokens, the last layer of several, no lse; starts that leave the
+    rows are kept inside them."""
+    rng = np.random.default_rng(8)
+    lengths, new, heads, dim, page = [70, 33], [20, 2], 3, 40, 16
+    pool, table = make(rng, 2, lengths, heads, dim, page, layers=3)
+    scales(rng, pool, table)
+    start = starts(new)
+    q = rounded(rng.standard_normal((22, 6, dim)), kind)
+    wide = torch.full((22, 6 * dim + 7), float("nan"), dtype=TYPES[kind], device=DEV)
+    wide[:, : 6 * dim] = dev(q).to(TYPES[kind]).view(22, -1)
+    q_dev = wide[:, : 6 * dim].unflatten(1, (6, dim))
+    out_dev = torch.zeros(6, 22, dim, dtype=TYPES[kind], device=DEV).transpose(0, 1)
+    run_attend(cache_of(pool), table, lengths, q, start, kind, layer=2, lse=False, q_dev=q_dev, out_dev=out_dev, scale=0.3)
+    check_attend(pool, table, lengths, q, start, kind, out_dev, None, 0.3, layer=2)
+    # row 21 is the last: a sequence that claims rows 20..40 has 20 and 21, and negative starts are 0
+    lie = np.array([-5, 20, 40])
+    run_attend(cache_of(pool), table, lengths, q, lie, kind, layer=2, lse=False, q_dev=q_dev, out_dev=out_dev, scale=0.3)
+    check_attend(pool, table, lengths, q, start, kind, out_dev, None, 0.3, layer=2)
+
+
+@pytest.mark.parametrize("kind,new", [("bf16", 1), ("f32", 1), ("bf16", 64), ("f32", 64)])
+def test_attend_with_extreme_queries_and_scales(kind, new):
+    """Scores far apart and all alike, queries of very large and very small size, zero queries, a block of zeros, blocks whose scales are
+    orders of magnitude apart."""
+    rng = np.random.default_rng(9)
+    lengths, heads, dim, page = [400], 2, 128, 16
+    pool, table = make(rng, 1, lengths, heads, dim, page)
+    scales(rng, pool, table)
+    pool.v_scale[:, table[0, ::3]] *= 1e-6
+    pool.v_scale[:, table[0, 1::5]] *= 1e5
+    pool.k_scale[:, table[0, 4]] = 0
+    pool.v_scale[:, table[0, 7]] = 0
+    start = starts([new])
+    q = rng.standard_normal((new, 4, dim))
+    q[:, 0] *= 1e-20
+    q[:, 1] *= 40.0
+    q[:, 2] = 0
+    q[0, 3, 0] = 3e3
+    q = rounded(q, kind)
+    out, lse = run_attend(cache_of(pool), table, lengths, q, start, kind)
+    check_attend(pool, table, lengths, q, start, kind, out, lse, dim ** -0.5)
+
+
+def test_attend_long_context_splits_and_repeats():
+    """A context long enough to be split over the chip; the same call again gives the same bits."""
+    rng = np.random.default_rng(10)
+    lengths, heads, dim, page = [20011, 5], 2, 64, 64
+    pool, table = make(rng, 2, lengths, heads, dim, page)
+    scales(rng, pool, table)
+    start = starts([1, 1])
+    q = rounded(rng.standard_normal((2, 4, dim)) * 3, "bf16")
+    cache = cache_of(pool)
+    first = run_attend(cache, table, lengths, q, start, "bf16")
+    again = run_attend(cache, table, lengths, q, start, "bf16")
+    assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+    check_attend(pool, table, lengths, q, start, "bf16", *first, dim ** -0.5)
+
+
+# ---------------------------------------------------------------------------------------------------------------- append, read
+#          lengths             new             heads dim page type
+APPEND = [
+    ([1, 5, 16, 17, 0],        [1, 1, 1, 1, 0], 2, 64, 16, "bf16"),
+    ([100, 64, 65],            [1, 1, 1],       3, 128, 64, "f32"),
+    ([200, 31],                [200, 30],       2, 80, 32, "bf16"),
+    ([257, 300],               [3, 129],        1, 256, 128, "f32"),
+    ([90],                     [17],            4, 1, 16, "bf16"),
+    ([90, 20],                 [33, 20],        2, 33, 256, "bf16"),
+    ([140],                    [75],            2, 192, 64, "f32"),
+    ([64, 128],                [64, 65],        2, 96, 64, "bf16"),
+]
+
+
+def compare_pool(pool, cache, near, named):
+    for name in ("k", "v"):
+        scale = getattr(cache, name + "_scale").cpu().numpy()
+        want = getattr(pool, name + "_scale")
+        assert np.array_equal(scale[:, named], want[:, named], equal_nan=True), name + "_scale"
+        codes, want = getattr(cache, name).cpu().numpy().astype(int), getattr(pool, name).astype(int)
+        away = codes != want
+        assert not np.any(away & ~near[name]), np.argwhere(away & ~near[name])[:4]
+        assert np.abs(codes - want).max() <= 1
+
+
+@pytest.mark.parametrize("case", range(len(APPEND)))
+def test_append_and_read_against_the_definition(case):
+    """Row by row as tokens come, then all rows in one call: older codes move to the new grid where a block's scale grows."""
+    lengths, new, heads, dim, page, kind = APPEND[case]
+    rng = np.random.default_rng(2000 + case)
+    pool, table = make(rng, len(lengths), lengths, heads, dim, page, layers=2)
+    cache = cache_of(pool)
+    before = [n - m for n, m in zip(lengths, new)]
+    for counts, upto in ((before, before), (new, lengths)):
+        start = starts(counts)
+        if start[-1] == 0:
+            continue
+        k, v = (rounded(rng.standard_normal((start[-1], heads, dim)) * np.exp(rng.standard_normal((start[-1], 1, 1))), kind) for _ in "kv")
+        t = E.CacheTable(dev(table), ints(upto))
+        rows = E.CacheRows(dev(k).to(TYPES[kind]), dev(v).to(TYPES[kind]), ints(start), int(max(counts)), layer=1)
+        E.entro_cache_append(cache, t, rows)
+        near = ref.append(pool, table, upto, k, v, start, layer=1)
+        torch.cuda.synchronize()
+        compare_pool(pool, cache, near, np.unique(table[table >= 0]))
+        # a code that 32 bits round the other way is right, too: go on from the library's
+        pool.k, pool.v = cache.k.cpu().numpy(), cache.v.cpu().numpy()
+        written = [x.clone() for x in (cache.k, cache.v, cache.k_scale, cache.v_scale)]
+        E.entro_cache_append(cache, t, rows)
+        assert all(torch.equal(torch.nan_to_num(a.float()), torch.nan_to_num(b.float()))
+                   for a, b in zip(written, (cache.k, cache.v, cache.k_scale, cache.v_scale)))
+    whole = starts(lengths)
+    for out_kind in ("bf16", "f32"):
+        back = [torch.full((whole[-1], heads, dim), 7.0, dtype=TYPES[out_kind], device=DEV) for _ in "kv"]
+        E.entro_cache_read(cache, E.CacheTable(dev(table), ints(lengths)), E.CacheRows(*back, ints(whole), max(lengths), layer=1))
+        for got, want in zip(back, ref.read(pool, table, lengths, whole, whole[-1], layer=1)):
+            assert torch.equal(got.cpu(), torch.from_numpy(want.astype(np.float32)).to(TYPES[out_kind]))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_append_takes_values_that_are_no_numbers(kind):
+    """NaN, infinities, a block of zeros, values too small for a scale of their own, the largest finite ones."""
+    rng = np.random.default_rng(11)
+    lengths, heads, dim, page = [64], 2, 64, 16
+    pool, table = make(rng, 1, lengths, heads, dim, page)
+    k = rounded(rng.standard_normal((64, heads, dim)), kind)
+    v = rounded(rng.standard_normal((64, heads, dim)), kind)
+    k[3, 0, 5], k[4, 1, 6], k[5, 0, 7] = np.nan, np.inf, -np.inf
+    v[16:32] = 0
+    v[32:48] = rounded(v[32:48] * 1e-43, kind)
+    v[48:64, 0] = np.nan
+    v[48:64, 1, 0] = rounded(np.array(3.38e38), kind)
+    cache, start = cache_of(pool), starts([64])
+    E.entro_cache_append(cache, E.CacheTable(dev(table), ints(lengths)),
+                         E.CacheRows(dev(k).to(TYPES[kind]), dev(v).to(TYPES[kind]), ints(start), 64))
+    near = ref.append(pool, table, lengths, k, v, start)
+    compare_pool(pool, cache, near, np.unique(table))
+
+
+def test_append_leaves_all_else_alone():
+    """Positions without a page, past the table, before 0; other layers and pages; strided rows; hints that are too small."""
+    rng = np.random.default_rng(12)
+    lengths, heads, dim, page = [70, 40, 3], 2, 48, 16
+    pool, table = make(rng, 3, lengths, heads, dim, page, layers=3, spare=6)
+    table[0, 2] = -1
+    table[1, 1] = pool.pages + 4
+    table = np.ascontiguousarray(table[:, :4])                            # 64 of the 70 tokens
+    counts = [60, 40, 9]                                                  # the last sequence has 3 tokens only: 6 rows stand before it
+    start = starts(counts)
+    fused = torch.from_numpy(rng.standard_normal((start[-1], 2 * heads * dim + 3)).astype(np.float32)).to(DEV).to(torch.bfloat16)
+    kd, vd = (fused[:, i * heads * dim: (i + 1) * heads * dim].unflatten(1, (heads, dim)) for i in (0, 1))
+    # the tokens before the new ones of sequence 0
+    scales(rng, pool, table)
+    cache = cache_of(pool)
+    near = ref.append(pool, table, lengths, kd.float().cpu().numpy(), vd.float().cpu().numpy(), start, layer=1)
+    E.entro_cache_append(cache, E.CacheTable(dev(table), ints(lengths)), E.CacheRows(kd, vd, ints(start), 2, layer=1))
+    compare_pool(pool, cache, near, np.unique(table[(table >= 0) & (table < pool.pages)]))
+    back = [torch.zeros(2 * heads, start[-1], dim, dtype=torch.float32, device=DEV).transpose(0, 1)[:, ::2] for _ in "kv"]
+    pool.k, pool.v = cache.k.cpu().numpy(), cache.v.cpu().numpy()
+    E.entro_cache_read(cache, E.CacheTable(dev(table), ints(lengths)), E.CacheRows(*back, ints(start), 1, layer=1))
+    for got, want in zip(back, ref.read(pool, table, lengths, start, start[-1], layer=1)):
+        assert np.array_equal(got.cpu().numpy(), want.astype(np.float32))
+
+
+# ----------------------------------------------------------------------------------------------------------------- page tables
+def run_pages(pool, table, lengths, seqs, stride, call):
+    cache = cache_of(pool)
+    t = E.CacheTable(dev(table), ints(lengths))
+    following = E.CacheTable(torch.full((seqs, stride), 77, dtype=torch.int32, device=DEV), torch.full((seqs,), 77, dtype=torch.int32, device=DEV))
+    status = torch.full((4,), 77, dtype=torch.int32, device=DEV)
+    ws = torch.full((E.entro_cache_pages_workspace_bytes(cache, t, following),), 0xAB, dtype=torch.uint8, device=DEV)
+    for _ in range(2):                                                    # the same call again gives the same
+        call(cache, t, following, status, ws)
+        torch.cuda.synchronize()
+    return cache, following, status.cpu().numpy()
+
+
+def check_pages(pool, cache, following, status, want, pages):
+    table, lengths, copies, used = want
+    assert list(status) == [0, used, pages - used, len(copies)]
+    assert np.array_equal(following.slots.cpu().numpy(), table)
+    assert np.array_equal(following.lengths.cpu().numpy(), lengths)
+    ref.copy_pages(pool, copies)
+    for name in ("k", "v", "k_scale", "v_scale"):
+        assert np.array_equal(getattr(cache, name).cpu().numpy(), getattr(pool, name), equal_nan="scale" in name), name
+
+
+#          lengths                 rows  parents                      grow                       window sinks  page
+REGROUP = [
+    ([40, 17, 64, 0, 5],           5, None,                        None,                          0, 0, 16),
+    ([40, 17, 64, 0, 5],           5, None,                        [1, 1, 1, 1, 1],               0, 0, 16),
+    ([40, 17, 64, 0, 5],           7, [0, 0, 0, 2, 2, 3, 4],       [1, 0, 40, 1, 1, 20, -2],      0, 0, 16),
+    ([100],                        9, [0] * 9,                     [1] * 9,                       0, 0, 32),
+    ([100, 50],                    3, [-1, 1, 99],                 [5, 5, 5],                     0, 0, 32),
+    ([100, 50],                    4, [0, 0, 1, 1],                [-60, 0, -50, -99],            0, 0, 16),
+    ([100, 96],                    4, [0, 0, 1, 1],                [-10, -20, -1, 0],             0, 0, 32),
+    ([400, 90, 20],                3, None,                        [1, 1, 1],                     100, 4, 16),
+    ([400, 90, 20],                4, [0, 0, 1, 2],                [3, -70, 1, 0],                64, 40, 16),
+    ([400],                        2, [0, 0],                      [1, 1],                        1, 0, 64),
+    ([3000] + [1] * 40,            41, None,                       [7] * 41,                      0, 0, 16),
+]
+
+
+@pytest.mark.parametrize("case", range(len(REGROUP)))
+def test_regroup_against_the_definition(case):
+    lengths, rows, parent, grow, window, sinks, page = REGROUP[case]
+    rng = np.random.default_rng(3000 + case)
+    pool, table = make(rng, len(lengths), lengths, 2, 64, page, layers=2, spare=60)
+    scales(rng, pool, table)
+    stride = table.shape[1] + 4
+    want = ref.regroup(pool.pages, page, table, lengths, rows, stride, parent, grow, window, sinks)
+    assert want is not None
+    result = run_pages(pool, table, lengths, rows, stride, lambda cache, t, n, status, ws: E.entro_cache_regroup(
+        cache, t, n, status, ws, parent=None if parent is None else ints(parent), grow=None if grow is None else ints(grow),
+        window=window, sinks=sinks))
+    check_pages(pool, *result, want, pool.pages)
+
+
+def test_regroup_of_random_tables():
+    """Steps one after the other: what one leaves is the next one's table."""
+    rng = np.random.default_rng(13)
+    page, seqs, stride = 16, 12, 20
+    pool, _ = make(rng, 1, [0], 1, 16, page, layers=2, spare=150)
+    pool.k_scale[:], pool.v_scale[:] = 1, 1
+    table, lengths = np.full((seqs, stride), -1, np.int32), np.zeros(seqs, np.int32)
+    done = 0
+    for step in range(25):
+        parent = np.where(rng.random(seqs) < 0.6, np.arange(seqs), rng.integers(-2, seqs + 1, seqs))
+        grow = rng.integers(-20, 45, seqs)
+        window, sinks = (0, 0) if rng.random() < 0.7 else (int(rng.integers(1, 90)), int(rng.integers(0, 40)))
+        want = ref.regroup(pool.pages, page, table, lengths, seqs, stride, parent, grow, window, sinks)
+        cache, following, status = run_pages(pool, table, lengths, seqs, stride, lambda c, t, n, status, ws: E.entro_cache_regroup(
+            c, t, n, status, ws, parent=ints(parent), grow=ints(grow), window=window, sinks=sinks))
+        if want is None:
+            assert E.entro_cache_status(status[0]) == B.ENTRO_ERR_CAPACITY
+            for name in ("k", "v"):
+                assert np.array_equal(getattr(cache, name).cpu().numpy(), getattr(pool, name))
+            continue
+        check_pages(pool, cache, following, status, want, pool.pages)
+        table, lengths = want[:2]
+        done += 1
+    assert done >= 10
+
+
+@pytest.mark.parametrize("case", range(5))
+def test_compact_against_the_definition(case):
+    rng = np.random.default_rng(4000 + case)
+    lengths = [[40, 17, 64, 0, 5], [1], [0, 0], [5000, 300, 7], [16] * 30][case]
+    pool, table = make(rng, len(lengths), lengths, 3, 64, 16, layers=2, spare=[20, 40, 3, 2000, 0][case])
+    scales(rng, pool, table)
+    if case == 0:
+        table[1] = table[0, :table.shape[1]]                              # shared pages
+        table[2, 1], table[2, 2] = -9, pool.pages
+    want = ref.compact(pool.pages, table, np.array(lengths, np.int32))
+    result = run_pages(pool, table, lengths, *table.shape, lambda cache, t, n, status, ws: E.entro_cache_compact(cache, t, n, status, ws))
+    check_pages(pool, *result, want, pool.pages)
+
+
+def test_refusals_of_pages_that_do_not_suffice():
+    rng = np.random.default_rng(14)
+    pool, table = make(rng, 2, [20, 20], 1, 64, 16, spare=1)
+    scales(rng, pool, table)
+    for grow, stride in (([30, 30], 10), ([100, 0], 4)):
+        cache, following, status = run_pages(pool, table, [20, 20], 2, stride, lambda c, t, n, status, ws: E.entro_cache_regroup(
+            c, t, n, status, ws, grow=ints(grow)))
+        assert E.entro_cache_status(status[0]) == B.ENTRO_ERR_CAPACITY and status[3] == 0
+        assert np.array_equal(cache.k.cpu().numpy(), pool.k)
+
+
+# --------------------------------------------------------------------------------------------------- together, graphs, streams
+def test_a_step_in_a_graph_follows_lengths_that_change():
+    """Append and attend captured once and replayed as sequences grow, on another stream than the one the inputs came from,
+    with eager work between the replays: every replay against the eager calls and the definition."""
+    rng = np.random.default_rng(15)
+    heads, dim, page, seqs = 2, 64, 16, 3
+    pool, table = make(rng, seqs, [90, 90, 90], heads, dim, page)
+    lengths = np.array([30, 64, 1])
+    cache, twin = cache_of(pool), cache_of(pool)
+    table_dev, lengths_dev = dev(table), ints(lengths)
+    t = E.CacheTable(table_dev, lengths_dev)
+    start = ints([0, 1, 2, 3])
+    k, v, q, out = (torch.zeros(seqs, n, dim, dtype=torch.bfloat16, device=DEV) for n in (heads, heads, 4, 4))
+    rows, query = E.CacheRows(k, v, start, 1), E.CacheQuery(q, out, start, 1, 90)
+    ws = torch.empty(max(16, E.entro_cache_attend_workspace_bytes(cache, t, query)), dtype=torch.uint8, device=DEV)
+    # what stands in the cache before the steps
+    back = starts(lengths - 1)
+    old = [torch.randn(back[-1], heads, dim, device=DEV) for _ in "kv"]
+    short = E.CacheTable(table_dev, ints(lengths - 1))
+    for c in (cache, twin):
+        E.entro_cache_append(c, short, E.CacheRows(*old, ints(back), 63))
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    saved = [x.clone() for x in (cache.k, cache.v, cache.k_scale, cache.v_scale)]
+    with torch.cuda.stream(stream):
+        E.entro_cache_append(cache, t, rows)
+        E.entro_cache_attend(cache, t, query, ws)
+    stream.synchronize()
+    for x, y in zip((cache.k, cache.v, cache.k_scale, cache.v_scale), saved):
+        x.copy_(y)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        E.entro_cache_append(cache, t, rows)
+        E.entro_cache_attend(cache, t, query, ws)
+    out_twin = torch.zeros_like(out)
+    query_twin = E.CacheQuery(q, out_twin, start, 1, 90)
+    for step in range(5):
+        for x in (k, v, q):
+            x.copy_(torch.randn(x.shape, device=DEV))
+        lengths_dev.copy_(ints(lengths + step))
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            graph.replay()
+        stream.synchronize()
+        E.entro_cache_append(twin, t, rows)
+        E.entro_cache_attend(twin, t, query_twin, ws)
+        torch.cuda.synchronize()
+        assert torch.equal(out, out_twin) and torch.equal(cache.k, twin.k) and torch.equal(cache.v, twin.v)
+        pool.k, pool.v, pool.k_scale, pool.v_scale = (x.cpu().numpy() for x in (cache.k, cache.v, cache.k_scale, cache.v_scale))
+        check_attend(pool, table, list(lengths + step), q.float().cpu().numpy(), np.arange(4), "bf16", out, None, dim ** -0.5)
