@@ -15,82 +15,370 @@ struct Query {
     const int32_t *start;
     uint32_t tokens, q_heads, group, window, sinks;
     float scale;
+    bool aligned;                  // rows of q begin at multiples of 16 bytes
+    uint32_t splits, least;        // a group of rows takes at most `splits` workgroups, of at least `least` tiles each
+    float *part_o, *part_lse;      // [row][q_heads][splits][W], [row][q_heads][splits]: joined afterwards where splits > 1
 };
 
-// One workgroup per row and query head: scores of 256 keys at a time, a running maximum and sum, then a lane per dimension.
-template <typename T, typename S>
-__global__ __launch_bounds__(kWG) void k_attend_simple(Pool p, Query a, uint64_t work) {
-    __shared__ float q[ENTRO_CACHE_MAX_DIM], prob[kWG], red[kWG / 64];
-    __shared__ int32_t key_page[kWG];
-    const uint32_t tid = threadIdx.x, pt = 1u << p.page_shift;
-    for (uint64_t w = blockIdx.x; w < work; w += gridDim.x) {
-        const uint32_t h = static_cast<uint32_t>(w % a.q_heads), head = h / a.group;
-        const int32_t row = static_cast<int32_t>(w / a.q_heads);
-        uint32_t lo = 0, hi = p.seqs;
-        while (hi - lo > 1) {
-            const uint32_t mid = (lo + hi) / 2;
-            if (a.start[mid] <= row) lo = mid; else hi = mid;
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 half2 __attribute__((ext_vector_type(2)));
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kTile = 64;                      // tokens a wavefront takes at a time
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// Four codes c as halves c - 128: 0x6400 + c is 1024 + c, exactly.
+__device__ inline void codes_to_halves(uint32_t codes, half2 *lo, half2 *hi) {
+    const half2 off = {(_Float16)-1152.0f, (_Float16)-1152.0f};
+    *lo = __builtin_bit_cast(half2, __builtin_amdgcn_perm(0x64646464u, codes, 0x04010400u)) + off;
+    *hi = __builtin_bit_cast(half2, __builtin_amdgcn_perm(0x64646464u, codes, 0x04030402u)) + off;
+}
+
+__device__ inline half8 eight_codes(uint32_t a, uint32_t b) {
+    half2 h[4];
+    codes_to_halves(a, h, h + 1);
+    codes_to_halves(b, h + 2, h + 3);
+    return {h[0].x, h[0].y, h[1].x, h[1].y, h[2].x, h[2].y, h[3].x, h[3].y};
+}
+
+// The upper halves of two fp32 numbers: cut off to bf16.
+__device__ inline uint32_t upper_halves(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); }
+
+// Eight codes c as bf16 numbers c - 128, exactly.
+__device__ inline bf16x8 eight_values(uint32_t a, uint32_t b) {
+    const uint32_t s[2] = {a ^ 0x80808080u, b ^ 0x80808080u};
+    u32x4 r;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const float f0 = static_cast<float>(static_cast<int8_t>(s[i])), f1 = static_cast<float>(static_cast<int8_t>(s[i] >> 8));
+        const float f2 = static_cast<float>(static_cast<int8_t>(s[i] >> 16)), f3 = static_cast<float>(static_cast<int8_t>(s[i] >> 24));
+        r[2 * i] = upper_halves(f0, f1);
+        r[2 * i + 1] = upper_halves(f2, f3);
+    }
+    return __builtin_bit_cast(bf16x8, r);
+}
+
+// Eight weights of the second product as the sum of N bf16 numbers: 16 or 24 bits of each, at any size. (A half holds 11 bits in one
+// piece, but loses weights that are 2^-40 of the largest one; where the heavier tokens' codes are 0 those are the result.)
+template <int N>
+__device__ inline void split_weights(const float *x, bf16x8 *w) {
+    u32x4 r[N];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float a = x[2 * i], b = x[2 * i + 1];
+#pragma unroll
+        for (int n = 0; n < N - 1; ++n) {
+            r[n][i] = upper_halves(a, b);
+            a -= __uint_as_float(__float_as_uint(a) & 0xffff0000u);
+            b -= __uint_as_float(__float_as_uint(b) & 0xffff0000u);
         }
-        const Span s = span_of(a.start, p.lengths, lo, a.tokens);
-        if (row < s.row || row >= s.row + s.count) continue;
-        const int32_t pos = s.pos + row - s.row;
-        const T *qr = static_cast<const T *>(a.q) + static_cast<uint32_t>(row) * a.q_token_stride + h * a.q_head_stride;
-        for (uint32_t d = tid; d < p.head_dim; d += kWG) q[d] = S::load(qr + d);
-        float top = -INFINITY, sum = 0.0f, acc = 0.0f;
-        for (int32_t j0 = 0; j0 <= pos; j0 += kWG) {
-            const int32_t j = j0 + static_cast<int32_t>(tid);
-            int32_t page = -1;
-            if (j <= pos && (!a.window || static_cast<uint32_t>(pos - j) < a.window || static_cast<uint32_t>(j) < a.sinks)) page = page_of(p, lo, j >> p.page_shift);
-            __syncthreads();
-            float z = -INFINITY;
-            if (page >= 0) {
-                const uint64_t unit = uint64_t{static_cast<uint32_t>(page)} * p.kv_heads + head;
-                const uint8_t *k = p.k + (unit * pt + (static_cast<uint32_t>(j) & (pt - 1))) * p.width;
-                float dot = 0.0f;
-                for (uint32_t d = 0; d < p.head_dim; ++d) dot = fmaf(q[d], static_cast<float>(static_cast<int32_t>(k[d]) - 128), dot);
-                z = dot * p.k_scale[unit] * a.scale;
+        r[N - 1][i] = __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(a), static_cast<__bf16>(b)});
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) w[n] = __builtin_bit_cast(bf16x8, r[n]);
+}
+
+// Maximum over the four lanes that hold a column (lanes c, c + 16, c + 32, c + 48).
+__device__ inline float column_max(float v) {
+    v = fmaxf(v, __shfl_xor(v, 16));
+    return fmaxf(v, __shfl_xor(v, 32));
+}
+
+__device__ inline float column_sum(float v) {
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
+}
+
+// The tiles of kTile tokens that rows at positions first..last see: those of the first tokens, then those of the window.
+struct Tiles {
+    int32_t sinks, from, count;
+    __device__ int32_t at(int32_t i) const { return i < sinks ? i : from + i - sinks; }
+};
+
+__device__ inline Tiles tiles_of(const Pool &p, const Query &a, int32_t first, int32_t last) {
+    const int64_t end = min(int64_t{last} + 1, int64_t{p.stride} << p.page_shift);
+    Tiles t = {0, 0, 0};
+    if (end <= 0) return t;
+    const int32_t until = static_cast<int32_t>((end + kTile - 1) / kTile);
+    if (a.window) {
+        const int64_t lo = int64_t{first} - a.window + 1;
+        t.from = lo > 0 ? static_cast<int32_t>(min(lo / kTile, int64_t{until})) : 0;
+        t.sinks = static_cast<int32_t>(min((int64_t{a.sinks} + kTile - 1) / kTile, int64_t{t.from}));
+    }
+    t.count = t.sinks + until - t.from;
+    return t;
+}
+
+// How the tiles of a group of rows are shared out to at most `splits` workgroups.
+__device__ inline int32_t tiles_per_split(const Query &a, int32_t count) {
+    return max((count + static_cast<int32_t>(a.splits) - 1) / static_cast<int32_t>(a.splits), static_cast<int32_t>(a.least));
+}
+
+template <typename T> __device__ inline float load_as_f32(const T *p);
+template <> __device__ inline float load_as_f32<float>(const float *p) { return *p; }
+template <> __device__ inline float load_as_f32<uint16_t>(const uint16_t *p) { return bf16_to_f32(*p); }
+template <typename T> __device__ inline void store_as(T *p, float f);
+template <> __device__ inline void store_as<float>(float *p, float f) { *p = f; }
+template <> __device__ inline void store_as<uint16_t>(uint16_t *p, float f) { *p = f32_to_bf16(f); }
+
+// Eight elements of a row from dimension d on, zeros from head_dim on.
+template <typename T>
+__device__ inline void load_eight(const T *row, uint32_t d, uint32_t head_dim, bool aligned, float *x) {
+    if (aligned && d + 8 <= head_dim) {
+        if (sizeof(T) == 2) {
+            const u32x4 w = *reinterpret_cast<const u32x4 *>(row + d);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                x[2 * i] = __uint_as_float(w[i] << 16);
+                x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
             }
-            float m = z;
-            for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-            if ((tid & 63u) == 0) red[tid >> 6] = m;
-            __syncthreads();
-            for (int i = 0; i < kWG / 64; ++i) m = fmaxf(m, red[i]);
-            const float now = fmaxf(top, m), by = now == -INFINITY ? 0.0f : expf(top - now);
-            const float e = z == -INFINITY ? 0.0f : expf(z - now);
-            prob[tid] = e;
-            key_page[tid] = page;
-            __syncthreads();
-            sum *= by;
-            acc *= by;
-            top = now;
-            const int32_t n = min(kWG, pos - j0 + 1);
-            for (int32_t i = 0; i < n; ++i) {
-                if (key_page[i] < 0) continue;
-                sum += prob[i];
-                if (tid < p.head_dim) {
-                    const uint64_t unit = uint64_t{static_cast<uint32_t>(key_page[i])} * p.kv_heads + head;
-                    const uint8_t c = p.v[(unit * p.width + tid) * pt + (static_cast<uint32_t>(j0 + i) & (pt - 1))];
-                    acc = fmaf(prob[i] * p.v_scale[unit], static_cast<float>(static_cast<int32_t>(c) - 128), acc);
-                }
-            }
+        } else {
+            const f32x4 w0 = *reinterpret_cast<const f32x4 *>(row + d), w1 = *reinterpret_cast<const f32x4 *>(row + d + 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = w0[i], x[4 + i] = w1[i];
         }
-        if (tid < p.head_dim) {
-            T *o = static_cast<T *>(a.out) + static_cast<uint32_t>(row) * a.out_token_stride + h * a.out_head_stride;
-            o[tid] = S::store(sum > 0.0f ? acc / sum : 0.0f);
-        }
-        if (tid == 0 && a.lse) a.lse[uint64_t{static_cast<uint32_t>(row)} * a.q_heads + h] = sum > 0.0f ? top + logf(sum) : -INFINITY;
-        __syncthreads();
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = d + i < head_dim ? load_as_f32(row + d + i) : 0.0f;
+}
+
+// A query row's exponent e with |x| < 2^(e + 1): x * 2^(14 - e) is taken as halves, in one piece (exact for 11 bits) or two.
+__device__ inline int exponent_of(float most) { return max(static_cast<int>((__float_as_uint(most) >> 23) & 0xffu) - 127, -126); }
+
+template <int N>
+__device__ inline void split_halves(const float *x, half8 *hi, half8 *lo) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        (*hi)[i] = (_Float16)x[i];
+        if (N == 2) (*lo)[i] = (_Float16)(x[i] - (float)(*hi)[i]);
     }
 }
 
-struct AsF32 {
-    static __device__ float load(const float *p) { return *p; }
-    static __device__ float store(float f) { return f; }
-};
-struct AsBf16 {
-    static __device__ float load(const uint16_t *p) { return bf16_to_f32(*p); }
-    static __device__ uint16_t store(float f) { return f32_to_bf16(f); }
-};
+// ------------------------------------------------------------------------------------------------- few rows: token generation
+//
+// A wavefront multiplies 64 tokens at a time with up to 16 rows (tokens of a sequence and query heads that share a key head) on
+// v_mfma_f32_16x16x32_f16. It computes scores transposed, tokens x rows: a lane then holds 16 tokens of one row, and by the
+// choice of which key goes to which matrix row these are 16 tokens side by side in memory (lane group g: tokens 16 g ..
+// 16 g + 15), which is also what it loads of the values (16 bytes of one dimension) and what the second product wants of
+// the probabilities. Keys, values and probabilities so go from memory through registers to the matrix units, with no
+// exchange between lanes but for the maximum. Matrix unit slots that a tile of 16 rows leaves empty cost nothing: the bytes bound it.
+template <int W, typename T>
+__global__ __launch_bounds__(kWG, 2) void k_attend_few(Pool p, Query a) {
+    constexpr int kParts = sizeof(T) == 2 ? 1 : 2;         // halves that make a factor of the first product
+    constexpr int kWeights = sizeof(T) == 2 ? 2 : 3;       // bf16 numbers that make a weight of the second
+    constexpr int kFull = W / 64, kRest = W % 64 ? 1 : 0;   // loads of 64 dimensions of 16 tokens, and of 32
+    constexpr int kDims = W / 16;
+    __shared__ float merge_o[4][16][W + 4];
+    __shared__ float merge_m[4][16], merge_l[4][16];
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6, g = lane >> 4, c = lane & 15u;
+    const uint32_t split = blockIdx.x % a.splits, unit = blockIdx.x / a.splits, head = unit % p.kv_heads, b = unit / p.kv_heads;
+    const Span s = span_of(a.start, p.lengths, b, a.tokens);
+    const uint64_t token_bytes = W, page_bytes = uint64_t{W} << p.page_shift, page_stride = page_bytes * p.kv_heads;
+    const uint8_t *k_head = p.k + head * page_bytes, *v_head = p.v + head * page_bytes;
+    const float *ks_head = p.k_scale + head, *vs_head = p.v_scale + head;
+    const uint32_t in_page = (1u << p.page_shift) - 1;
+    const int64_t rows = int64_t{s.count} * a.group;
+    for (int64_t row0 = 0; row0 < rows; row0 += 16) {
+        const int32_t first = s.pos + static_cast<int32_t>(row0 / a.group);
+        const int32_t last = s.pos + static_cast<int32_t>(min(row0 + 15, rows - 1) / a.group);
+        const Tiles tiles = tiles_of(p, a, first, last);
+        const int32_t per = tiles_per_split(a, tiles.count), begin = static_cast<int32_t>(split) * per, end = min(begin + per, tiles.count);
+        if (begin >= end && split > 0) continue;
+        // the lane's row
+        const int64_t my_row = row0 + c;
+        const bool mine = my_row < rows;
+        const uint32_t my_token = static_cast<uint32_t>(s.row) + static_cast<uint32_t>((mine ? my_row : row0) / a.group);
+        const uint32_t my_head = head * a.group + static_cast<uint32_t>((mine ? my_row : row0) % a.group);
+        const int32_t my_pos = s.pos + static_cast<int32_t>(my_token) - s.row;
+        half8 q[kParts][W / 32];
+        float q_factor;
+        {
+            const T *row = static_cast<const T *>(a.q) + my_token * a.q_token_stride + my_head * a.q_head_stride;
+            float x[W / 32][8], most = 0.0f;
+#pragma unroll
+            for (int f = 0; f < W / 32; ++f) {
+                load_eight(row, f < 2 * kFull ? (f / 2) * 64 + g * 16 + (f & 1) * 8 : kFull * 64 + g * 8, p.head_dim, a.aligned, x[f]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(x[f][i]));
+            }
+            const int e = exponent_of(column_max(most));
+            const float sign = a.scale < 0.0f ? -1.0f : 1.0f;
+#pragma unroll
+            for (int f = 0; f < W / 32; ++f) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[f][i] = ldexpf(x[f][i] * sign, 14 - e);
+                split_halves<kParts>(x[f], &q[0][f], &q[kParts - 1][f]);
+            }
+            q_factor = ldexpf(fabsf(a.scale) * kLog2e, e - 14);
+        }
+        f32x4 o[kDims];
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) o[d] = f32x4{0, 0, 0, 0};
+        float m = -INFINITY, l = 0.0f;
+
+        for (int32_t i = begin + static_cast<int32_t>(wave); i < end; i += 4) {
+            const int32_t t0 = tiles.at(i) * kTile;
+            // this lane loads keys of the tokens 16 (c / 4) .. and values of the tokens 16 g ..
+            const int32_t k_at = t0 + 16 * static_cast<int32_t>(c >> 2), v_at = t0 + 16 * static_cast<int32_t>(g);
+            const int32_t k_page = page_of(p, b, k_at >> p.page_shift), v_page = page_of(p, b, v_at >> p.page_shift);
+            const uint8_t *kp = k_head + static_cast<uint32_t>(max(k_page, 0)) * page_stride + ((static_cast<uint32_t>(k_at) & in_page) + (c & 3u)) * token_bytes;
+            const uint8_t *vp = v_head + static_cast<uint32_t>(max(v_page, 0)) * page_stride + (uint64_t{c} << p.page_shift) + (static_cast<uint32_t>(v_at) & in_page);
+            const uint64_t scale_at = uint64_t{static_cast<uint32_t>(max(v_page, 0))} * p.kv_heads;
+            u32x4 kc[4][kFull + 0], vc[kDims];
+            u32x2 kr[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+#pragma unroll
+                for (int f = 0; f < kFull; ++f) kc[t][f] = *reinterpret_cast<const u32x4 *>(kp + 4 * t * W + 64 * f + 16 * g);
+                if (kRest) kr[t] = *reinterpret_cast<const u32x2 *>(kp + 4 * t * W + 64 * kFull + 8 * g);
+            }
+#pragma unroll
+            for (int d = 0; d < kDims; ++d) vc[d] = *reinterpret_cast<const u32x4 *>(vp + (uint64_t{16u * d} << p.page_shift));
+            const float ks = ks_head[scale_at], vs = vs_head[scale_at];
+
+            f32x4 z[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                z[t] = f32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int f = 0; f < kFull; ++f) {
+                    const half8 k0 = eight_codes(kc[t][f][0], kc[t][f][1]), k1 = eight_codes(kc[t][f][2], kc[t][f][3]);
+#pragma unroll
+                    for (int n = 0; n < kParts; ++n) {
+                        z[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[n][2 * f], z[t], 0, 0, 0);
+                        z[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q[n][2 * f + 1], z[t], 0, 0, 0);
+                    }
+                }
+                if (kRest) {
+                    const half8 k0 = eight_codes(kr[t][0], kr[t][1]);
+#pragma unroll
+                    for (int n = 0; n < kParts; ++n) z[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[n][2 * kFull], z[t], 0, 0, 0);
+                }
+            }
+            // scores in units of log2
+            const float factor = ks * q_factor;
+            float top = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int32_t key = v_at + 4 * t + j;
+                    const bool seen = v_page >= 0 && key <= my_pos && (!a.window || static_cast<uint32_t>(my_pos - key) < a.window || static_cast<uint32_t>(key) < a.sinks);
+                    z[t][j] = seen ? z[t][j] * factor : -INFINITY;
+                    top = fmaxf(top, z[t][j]);
+                }
+            const float now = fmaxf(m, column_max(top)), base = now == -INFINITY ? 0.0f : now;
+            const float by = __builtin_amdgcn_exp2f(m - base);
+            m = now;
+            l *= by;
+#pragma unroll
+            for (int d = 0; d < kDims; ++d) o[d] *= by;
+            // a page without a token that is seen may hold anything as its scale
+            const float scale = top > -INFINITY ? vs : 0.0f;
+            bf16x8 w[2][kWeights];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float x[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float e = __builtin_amdgcn_exp2f(z[2 * h + j / 4][j & 3] - base);
+                    l += e;
+                    x[j] = e * scale;
+                }
+                split_weights<kWeights>(x, w[h]);
+            }
+#pragma unroll
+            for (int d = 0; d < kDims; ++d) {
+                const bf16x8 v0 = eight_values(vc[d][0], vc[d][1]), v1 = eight_values(vc[d][2], vc[d][3]);
+#pragma unroll
+                for (int n = 0; n < kWeights; ++n) {
+                    o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, w[0][n], o[d], 0, 0, 0);
+                    o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, w[1][n], o[d], 0, 0, 0);
+                }
+            }
+        }
+        l = column_sum(l);
+        // the four wavefronts' parts
+        __syncthreads();
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) *reinterpret_cast<f32x4 *>(&merge_o[wave][c][16 * d + 4 * g]) = o[d];
+        if (g == 0) merge_m[wave][c] = m, merge_l[wave][c] = l;
+        __syncthreads();
+        const uint32_t r = tid >> 4, d0 = tid & 15u;           // 16 lanes to a row
+        if (row0 + r < rows) {
+            float most = -INFINITY, sum = 0.0f, share[4];
+            for (int i = 0; i < 4; ++i) most = fmaxf(most, merge_m[i][r]);
+            const float base = most == -INFINITY ? 0.0f : most;
+            for (int i = 0; i < 4; ++i) {
+                share[i] = __builtin_amdgcn_exp2f(merge_m[i][r] - base);
+                sum += merge_l[i][r] * share[i];
+            }
+            const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+            const uint32_t token = static_cast<uint32_t>(s.row) + static_cast<uint32_t>((row0 + r) / a.group);
+            const uint32_t q_head = head * a.group + static_cast<uint32_t>((row0 + r) % a.group);
+            const float lse = sum > 0.0f ? base + __builtin_amdgcn_logf(sum) : sum == sum ? -INFINITY : sum;
+            const uint64_t at = uint64_t{token} * a.q_heads + q_head;
+            for (uint32_t d = d0; d < p.head_dim; d += 16) {
+                float x = 0.0f;
+                for (int i = 0; i < 4; ++i) x += merge_o[i][r][d] * share[i];
+                x = sum == sum ? x * inv : sum;
+                if (a.splits == 1)
+                    store_as(static_cast<T *>(a.out) + token * a.out_token_stride + q_head * a.out_head_stride + d, x);
+                else
+                    a.part_o[(at * a.splits + split) * W + d] = x;
+            }
+            if (d0 == 0) {
+                if (a.splits > 1) a.part_lse[at * a.splits + split] = lse;
+                else if (a.lse) a.lse[at] = lse * kLn2;
+            }
+        }
+    }
+}
+
+// Joins the parts of rows whose tiles were split. A wavefront per row and head.
+template <int W, typename T>
+__global__ __launch_bounds__(kWG) void k_attend_join(Pool p, Query a, uint32_t rows_per_tile) {
+    const uint32_t lane = threadIdx.x & 63u;
+    const uint64_t at = uint64_t{blockIdx.x} * (kWG / 64) + (threadIdx.x >> 6);
+    if (at >= uint64_t{a.tokens} * a.q_heads) return;
+    const uint32_t token = static_cast<uint32_t>(at / a.q_heads), h = static_cast<uint32_t>(at % a.q_heads);
+    uint32_t lo = 0, hi = p.seqs;                // the last sequence that starts at or before the row
+    while (hi - lo > 1) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (a.start[mid] <= static_cast<int32_t>(token)) lo = mid; else hi = mid;
+    }
+    const Span s = span_of(a.start, p.lengths, lo, a.tokens);
+    if (static_cast<int32_t>(token) < s.row || static_cast<int32_t>(token) >= s.row + s.count) return;
+    const int64_t rows = int64_t{s.count} * a.group, row = int64_t(token - static_cast<uint32_t>(s.row)) * a.group + h % a.group;
+    const int64_t row0 = row / rows_per_tile * rows_per_tile;
+    const Tiles tiles = tiles_of(p, a, s.pos + static_cast<int32_t>(row0 / a.group),
+                                 s.pos + static_cast<int32_t>(min(row0 + rows_per_tile - 1, rows - 1) / a.group));
+    const int32_t per = tiles_per_split(a, tiles.count);
+    const uint32_t parts = static_cast<uint32_t>(max((tiles.count + per - 1) / per, 1));
+    float most = -INFINITY;
+    for (uint32_t i = lane; i < parts; i += 64) most = fmaxf(most, a.part_lse[at * a.splits + i]);
+    for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+    const float base = most == -INFINITY ? 0.0f : most;
+    float sum = 0.0f, x[W / 64 + 1] = {};
+    for (uint32_t i = 0; i < parts; ++i) {
+        const float by = __builtin_amdgcn_exp2f(a.part_lse[at * a.splits + i] - base);
+        sum += by;
+#pragma unroll
+        for (int j = 0; j < (W + 63) / 64; ++j)
+            if (64 * j + lane < p.head_dim) x[j] += by * a.part_o[(at * a.splits + i) * W + 64 * j + lane];
+    }
+    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+#pragma unroll
+    for (int j = 0; j < (W + 63) / 64; ++j)
+        if (64 * j + lane < p.head_dim)
+            store_as(static_cast<T *>(a.out) + token * a.out_token_stride + h * a.out_head_stride + 64 * j + lane, sum == sum ? x[j] * inv : sum);
+    if (lane == 0 && a.lse) a.lse[at] = sum > 0.0f ? (base + __builtin_amdgcn_logf(sum)) * kLn2 : (sum == sum ? -INFINITY : sum);
+}
 
 entro_status check_query_sizes(const entro_cache *c, const entro_cache_query *q) {
     if (!q) return ENTRO_ERR_NULL;
@@ -109,32 +397,84 @@ entro_status check_query(const entro_cache *c, const entro_cache_query *q) {
     return ENTRO_OK;
 }
 
+struct Shape {
+    uint32_t splits, least;
+    uint64_t bytes;
+};
+
+int compute_units() {
+    int device = 0, cus = 0;
+    if (hipGetDevice(&device) != hipSuccess || hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess) return 256;
+    return cus > 0 ? cus : 256;
+}
+
+// How far a call's tiles are split: as many workgroups as fill the chip, tiles of a workgroup not fewer than pay for the
+// join, which is a launch of its own.
+Shape shape_of(const entro_cache *c, const entro_cache_table *t, const entro_cache_query *q) {
+    Shape s = {1, 16, 0};
+    uint64_t len = q->max_len;
+    if (q->window && len > uint64_t{q->window} + q->sinks + q->max_new + 2 * kTile) len = uint64_t{q->window} + q->sinks + q->max_new + 2 * kTile;
+    const uint64_t tiles = (len + kTile - 1) / kTile, units = uint64_t{t->seqs} * c->kv_heads;
+    const uint64_t want = (uint64_t(compute_units()) * 4 + units - 1) / units, can = (tiles + s.least - 1) / s.least;
+    s.splits = static_cast<uint32_t>(want < can ? want : can);
+    if (s.splits < 1) s.splits = 1;
+    if (s.splits > 256) s.splits = 256;
+    if (s.splits > 1) s.bytes = uint64_t{q->tokens} * q->q_heads * s.splits * (entro_cache_width(c->head_dim) + 1) * 4;
+    return s;
+}
+
+template <typename T>
+void launch(const Pool &p, const Query &a, hipStream_t st) {
+    const dim3 grid(p.seqs * p.kv_heads * a.splits);
+    const dim3 join(static_cast<unsigned>((uint64_t{a.tokens} * a.q_heads + kWG / 64 - 1) / (kWG / 64)));
+#define ENTRO_WIDTH(W)                                                                                  \
+    case W:                                                                                             \
+        hipLaunchKernelGGL((k_attend_few<W, T>), grid, dim3(kWG), 0, st, p, a);                         \
+        if (a.splits > 1) hipLaunchKernelGGL((k_attend_join<W, T>), join, dim3(kWG), 0, st, p, a, 16u); \
+        break
+    switch (p.width) {
+        ENTRO_WIDTH(64);
+        ENTRO_WIDTH(96);
+        ENTRO_WIDTH(128);
+        ENTRO_WIDTH(192);
+        ENTRO_WIDTH(256);
+    }
+#undef ENTRO_WIDTH
+}
+
 }  // namespace
 
 extern "C" {
 
 uint64_t entro_cache_attend_workspace_bytes(const entro_cache *c, const entro_cache_table *t, const entro_cache_query *q) {
     if (check_sizes(c) != ENTRO_OK || check_table_sizes(t) != ENTRO_OK || check_query_sizes(c, q) != ENTRO_OK) return 0;
-    return 0;
+    return shape_of(c, t, q).bytes;
 }
 
 entro_status entro_cache_attend(const entro_cache *c, const entro_cache_table *t, const entro_cache_query *q, void *workspace,
                                 uint64_t workspace_bytes, void *hip_stream) {
-    (void)workspace, (void)workspace_bytes;
     if (const entro_status s = check_cache(c)) return s;
     if (const entro_status s = check_table(t)) return s;
     if (const entro_status s = check_query(c, q)) return s;
     if (q->tokens == 0) return ENTRO_OK;
+    const Shape shape = shape_of(c, t, q);
+    if (shape.bytes) {
+        if (!workspace) return ENTRO_ERR_NULL;
+        if (!aligned16(workspace)) return ENTRO_ERR_ALIGN;
+        if (workspace_bytes < shape.bytes) return ENTRO_ERR_CAPACITY;
+    }
+    if (uint64_t{t->seqs} * c->kv_heads * shape.splits > 0x7fffffffull || uint64_t{q->tokens} * q->q_heads > 0x1ffffffffull) return ENTRO_ERR_SIZE;
     const Pool p = pool_of(c, t, q->layer);
+    const bool aligned = ((q->q_token_stride | q->q_head_stride) & 7u) == 0;
+    float *part_lse = static_cast<float *>(workspace), *part_o = part_lse + uint64_t{q->tokens} * q->q_heads * shape.splits;
     const Query a = {q->q, q->out, q->lse, q->q_token_stride, q->q_head_stride, q->out_token_stride, q->out_head_stride, q->start,
-                     q->tokens, q->q_heads, q->q_heads / c->kv_heads, q->window, q->sinks, q->scale};
-    const uint64_t work = uint64_t{q->tokens} * q->q_heads;
-    const unsigned grid = static_cast<unsigned>(work < 65536 ? work : 65536);
+                     q->tokens, q->q_heads, q->q_heads / c->kv_heads, q->window, q->sinks, q->scale, aligned, shape.splits, shape.least,
+                     part_o, part_lse};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (q->type == ENTRO_F32)
-        hipLaunchKernelGGL((k_attend_simple<float, AsF32>), dim3(grid), dim3(kWG), 0, st, p, a, work);
+        launch<float>(p, a, st);
     else
-        hipLaunchKernelGGL((k_attend_simple<uint16_t, AsBf16>), dim3(grid), dim3(kWG), 0, st, p, a, work);
+        launch<uint16_t>(p, a, st);
     return hip_ok(hipGetLastError(), "entro_cache_attend") ? ENTRO_OK : ENTRO_ERR_DEVICE;
 }
 
