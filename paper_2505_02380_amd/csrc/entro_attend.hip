@@ -27,6 +27,7 @@ typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kTile = 64;                      // tokens a wavefront takes at a time
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -340,6 +341,242 @@ __global__ __launch_bounds__(kWG, 2) void k_attend_few(Pool p, Query a) {
     }
 }
 
+// ----------------------------------------------------------------------------------------------------- many rows: prompts
+//
+// A workgroup takes 32 rows a wavefront (tokens and the query heads of a key head side by side) and goes through the tokens 64 at
+// a time. All its threads turn the tile's codes into the numbers of the products, once, on their way to LDS: keys to halves
+// (q is scaled to halves exactly), values to bf16; rows in LDS are 16 bytes longer than their data, so that the 16 lanes that read
+// one place of 16 rows meet 64 different banks. While a tile is multiplied, the next one is written to the other half of the LDS and the
+// codes of the one after it, and the page numbers of a third, are on their way.
+//
+// v_mfma_f32_32x32x16, scores transposed as above: a lane holds 32 of a tile's scores of one row, tokens 8 i + 4 h + (0..3)
+// of each 32, h being the lane's half. The values' tokens lie in LDS in the order 0-3, 8-11, 4-7, 12-15 of each 16, so that what a
+// lane reads of them for the second product are the tokens whose weights it has.
+template <int W, typename T, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void k_attend_many(Pool p, Query a, uint32_t row_tiles) {
+    constexpr int kThreads = WAVES * 64, kRows = WAVES * 32;
+    constexpr int kParts = sizeof(T) == 2 ? 1 : 2, kWeights = sizeof(T) == 2 ? 2 : 3;
+    constexpr int kChunks = (W * 4 + kThreads - 1) / kThreads;      // pieces of 16 codes a thread turns, of keys and of values
+    constexpr int kKeyRow = 2 * W + 16, kValueRow = 2 * kTile + 16;   // bytes
+    constexpr int kValues = kTile * kKeyRow, kHalf = kValues + W * kValueRow;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kHalf];
+    __shared__ f32x4 tile_ks[2], tile_vs[2];
+    __shared__ int32_t tile_ok[2][4];
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6, h = lane >> 5, c = lane & 31u;
+    // workgroups of one key head follow each other at multiples of the number of heads: with 8 heads, on one XCD and its L2
+    const uint32_t units = p.seqs * p.kv_heads, unit = blockIdx.x % units, head = unit % p.kv_heads, b = unit / p.kv_heads;
+    const uint32_t split = blockIdx.x / units % a.splits, tile_from_end = blockIdx.x / units / a.splits;
+    const Span s = span_of(a.start, p.lengths, b, a.tokens);
+    const uint64_t page_bytes = uint64_t{W} << p.page_shift, page_stride = page_bytes * p.kv_heads;
+    const uint8_t *k_head = p.k + head * page_bytes, *v_head = p.v + head * page_bytes;
+    const uint32_t in_page = (1u << p.page_shift) - 1;
+    const int64_t rows = int64_t{s.count} * a.group;
+    const int64_t groups = (rows + kRows - 1) / kRows;
+    // the last rows see the most tokens: they come first
+    for (int64_t group = groups - 1 - tile_from_end; group >= 0; group -= row_tiles) {
+        const int64_t row0 = group * kRows;
+        const int32_t first = s.pos + static_cast<int32_t>(row0 / a.group);
+        const int32_t last = s.pos + static_cast<int32_t>(min(row0 + kRows - 1, rows - 1) / a.group);
+        const Tiles tiles = tiles_of(p, a, first, last);
+        const int32_t per = tiles_per_split(a, tiles.count), begin = static_cast<int32_t>(split) * per, end = min(begin + per, tiles.count);
+        if (begin >= end && split > 0) continue;
+        const int64_t my_row = row0 + 32 * wave + c;
+        const bool mine = my_row < rows;
+        const uint32_t my_token = static_cast<uint32_t>(s.row) + static_cast<uint32_t>((mine ? my_row : row0) / a.group);
+        const uint32_t my_head = head * a.group + static_cast<uint32_t>((mine ? my_row : row0) % a.group);
+        const int32_t my_pos = mine ? s.pos + static_cast<int32_t>(my_token) - s.row : -1;
+        // positions of the wavefront's rows
+        const int64_t wave_row = row0 + 32 * wave;
+        const int32_t wave_first = s.pos + static_cast<int32_t>(wave_row / a.group);
+        const int32_t wave_last = wave_row < rows ? s.pos + static_cast<int32_t>(min(wave_row + 31, rows - 1) / a.group) : -1;
+        half8 q[kParts][W / 16];
+        float q_factor;
+        {
+            const T *row = static_cast<const T *>(a.q) + my_token * a.q_token_stride + my_head * a.q_head_stride;
+            float most = 0.0f;
+#pragma unroll
+            for (int f = 0; f < W / 16; ++f) {
+                float x[8];
+                load_eight(row, 16 * f + 8 * h, p.head_dim, a.aligned, x);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(x[i]));
+            }
+            const int e = exponent_of(fmaxf(most, __shfl_xor(most, 32)));
+            const float sign = a.scale < 0.0f ? -1.0f : 1.0f;
+#pragma unroll
+            for (int f = 0; f < W / 16; ++f) {
+                float x[8];
+                load_eight(row, 16 * f + 8 * h, p.head_dim, a.aligned, x);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = ldexpf(x[i] * sign, 14 - e);
+                split_halves<kParts>(x, &q[0][f], &q[kParts - 1][f]);
+            }
+            q_factor = ldexpf(fabsf(a.scale) * kLog2e, e - 14);
+        }
+        constexpr int kDims = W / 32;
+        f32x16 o[kDims];
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) o[d] = f32x16{};
+        float m = -INFINITY, l = 0.0f;
+
+        int32_t k_page[kChunks], v_page[kChunks], s_page = -1;
+        u32x4 kc[kChunks], vc[kChunks];
+        float ks = 0.0f, vs = 0.0f;
+        int32_t s_ok = 0;
+        const auto ask_pages = [&](int32_t i) {
+            if (i >= end) return;
+            const int32_t t0 = tiles.at(i) * kTile;
+#pragma unroll
+            for (int n = 0; n < kChunks; ++n) {
+                const int32_t ch = n * kThreads + static_cast<int32_t>(tid);
+                if (kThreads * kChunks != W * 4 && ch >= W * 4) continue;
+                k_page[n] = page_of(p, b, (t0 + ch / (W / 16)) >> p.page_shift);
+                v_page[n] = page_of(p, b, (t0 + 16 * (ch & 3)) >> p.page_shift);
+            }
+            if (tid < 4) s_page = page_of(p, b, (t0 + 16 * static_cast<int32_t>(tid)) >> p.page_shift);
+        };
+        const auto ask_codes = [&](int32_t i) {
+            if (i >= end) return;
+            const int32_t t0 = tiles.at(i) * kTile;
+#pragma unroll
+            for (int n = 0; n < kChunks; ++n) {
+                const int32_t ch = n * kThreads + static_cast<int32_t>(tid);
+                if (kThreads * kChunks != W * 4 && ch >= W * 4) continue;
+                const uint32_t k_at = static_cast<uint32_t>(t0 + ch / (W / 16)), v_at = static_cast<uint32_t>(t0 + 16 * (ch & 3));
+                kc[n] = *reinterpret_cast<const u32x4 *>(k_head + static_cast<uint32_t>(max(k_page[n], 0)) * page_stride + (k_at & in_page) * W + 16 * (ch % (W / 16)));
+                vc[n] = *reinterpret_cast<const u32x4 *>(v_head + static_cast<uint32_t>(max(v_page[n], 0)) * page_stride + (static_cast<uint32_t>(ch >> 2) << p.page_shift) + (v_at & in_page));
+            }
+            if (tid < 4) {
+                const uint64_t at = uint64_t{static_cast<uint32_t>(max(s_page, 0))} * p.kv_heads + head;
+                ks = p.k_scale[at];
+                vs = p.v_scale[at];
+                s_ok = s_page >= 0;
+            }
+        };
+        const auto to_lds = [&](int half) {
+#pragma unroll
+            for (int n = 0; n < kChunks; ++n) {
+                const int32_t ch = n * kThreads + static_cast<int32_t>(tid);
+                if (kThreads * kChunks != W * 4 && ch >= W * 4) continue;
+                half8 *k = reinterpret_cast<half8 *>(lds + half * kHalf + (ch / (W / 16)) * kKeyRow + 32 * (ch % (W / 16)));
+                k[0] = eight_codes(kc[n][0], kc[n][1]);
+                k[1] = eight_codes(kc[n][2], kc[n][3]);
+                bf16x8 *v = reinterpret_cast<bf16x8 *>(lds + half * kHalf + kValues + (ch >> 2) * kValueRow + 32 * (ch & 3));
+                v[0] = eight_values(vc[n][0], vc[n][2]);
+                v[1] = eight_values(vc[n][1], vc[n][3]);
+            }
+            if (tid < 4) {
+                // a page without a token that is seen may hold anything as its scale
+                reinterpret_cast<float *>(&tile_ks[half])[tid] = fabsf(ks) < INFINITY ? ks : 0.0f;
+                reinterpret_cast<float *>(&tile_vs[half])[tid] = fabsf(vs) < INFINITY ? vs : 0.0f;
+                tile_ok[half][tid] = s_ok;
+            }
+        };
+        __syncthreads();                           // the last group's tiles have been read
+        ask_pages(begin);
+        ask_codes(begin);
+        ask_pages(begin + 1);
+        if (begin < end) to_lds(0);
+        ask_codes(begin + 1);
+        ask_pages(begin + 2);
+        __syncthreads();
+
+        for (int32_t i = begin; i < end; ++i) {
+            const int half = (i - begin) & 1;
+            const int32_t t0 = tiles.at(i) * kTile;
+            const uint8_t *at = lds + half * kHalf;
+            const bool work = t0 <= wave_last;      // a wavefront whose rows see nothing here only turns codes
+            f32x16 z[2];
+            if (work) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    z[t] = f32x16{};
+#pragma unroll
+                    for (int f = 0; f < W / 16; ++f) {
+                        const half8 k = *reinterpret_cast<const half8 *>(at + (32 * t + c) * kKeyRow + 32 * f + 16 * h);
+#pragma unroll
+                        for (int n = 0; n < kParts; ++n) z[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[n][f], z[t], 0, 0, 0);
+                    }
+                }
+            }
+            if (i + 1 < end) to_lds(half ^ 1);
+            ask_codes(i + 2);
+            ask_pages(i + 3);
+            if (work) {
+                const f32x4 kf = tile_ks[half] * q_factor, vf = tile_vs[half];
+                const bool all = t0 + kTile - 1 <= wave_first && (!a.window || static_cast<uint32_t>(wave_last - t0) < a.window) &&
+                                 (tile_ok[half][0] & tile_ok[half][1] & tile_ok[half][2] & tile_ok[half][3]);
+                float top = -INFINITY;
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        z[t][j] *= kf[2 * t + j / 8];
+                        if (!all) {
+                            const int32_t key = t0 + 32 * t + 8 * (j / 4) + 4 * static_cast<int32_t>(h) + (j & 3);
+                            const bool seen = tile_ok[half][2 * t + j / 8] && key <= my_pos &&
+                                              (!a.window || static_cast<uint32_t>(my_pos - key) < a.window || static_cast<uint32_t>(key) < a.sinks);
+                            z[t][j] = seen ? z[t][j] : -INFINITY;
+                        }
+                        top = fmaxf(top, z[t][j]);
+                    }
+                top = fmaxf(top, __shfl_xor(top, 32));
+                // sums may stand at 2^8 times their unit before they are brought to a new one
+                if (__any(top > m + 8.0f)) {
+                    const float now = fmaxf(m, top), by = __builtin_amdgcn_exp2f(m - (now == -INFINITY ? 0.0f : now));
+                    m = now;
+                    l *= by;
+#pragma unroll
+                    for (int d = 0; d < kDims; ++d) o[d] *= by;
+                }
+                const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) {     // 16 tokens
+                        float x[8];
+                        bf16x8 w[kWeights];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const float e = __builtin_amdgcn_exp2f(z[t][8 * g + j] - base);
+                            l += e;
+                            x[j] = e * vf[2 * t + g];
+                        }
+                        split_weights<kWeights>(x, w);
+#pragma unroll
+                        for (int d = 0; d < kDims; ++d) {
+                            const bf16x8 v = *reinterpret_cast<const bf16x8 *>(at + kValues + (32 * d + c) * kValueRow + 32 * (2 * t + g) + 16 * h);
+#pragma unroll
+                            for (int n = 0; n < kWeights; ++n) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[n], o[d], 0, 0, 0);
+                        }
+                    }
+            }
+            __syncthreads();
+        }
+        l += __shfl_xor(l, 32);
+        if (mine) {
+            const float inv = l > 0.0f ? 1.0f / l : 0.0f, base = m == -INFINITY ? 0.0f : m;
+            const float lse = l > 0.0f ? base + __builtin_amdgcn_logf(l) : l == l ? -INFINITY : l;
+            const uint64_t at = uint64_t{my_token} * a.q_heads + my_head;
+            T *out = static_cast<T *>(a.out) + my_token * a.out_token_stride + my_head * a.out_head_stride;
+            float *part = a.part_o + (at * a.splits + split) * W;
+#pragma unroll
+            for (int d = 0; d < kDims; ++d)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const uint32_t dim = 32 * d + 8 * (j / 4) + 4 * h + (j & 3);
+                    const float x = l == l ? o[d][j] * inv : l;
+                    if (a.splits > 1) part[dim] = x;
+                    else if (dim < p.head_dim) store_as(out + dim, x);
+                }
+            if (h == 0) {
+                if (a.splits > 1) a.part_lse[at * a.splits + split] = lse;
+                else if (a.lse) a.lse[at] = lse * kLn2;
+            }
+        }
+    }
+}
+
 // Joins the parts of rows whose tiles were split. A wavefront per row and head.
 template <int W, typename T>
 __global__ __launch_bounds__(kWG) void k_attend_join(Pool p, Query a, uint32_t rows_per_tile) {
@@ -398,7 +635,8 @@ entro_status check_query(const entro_cache *c, const entro_cache_query *q) {
 }
 
 struct Shape {
-    uint32_t splits, least;
+    uint32_t waves;                // 0: the kernel for few rows; otherwise wavefronts of the one for many
+    uint32_t row_tiles, splits, least;
     uint64_t bytes;
 };
 
@@ -408,38 +646,59 @@ int compute_units() {
     return cus > 0 ? cus : 256;
 }
 
+// Wavefronts of a workgroup of many rows: eight share a tile's codes best; where a wavefront's sums and queries take more than 256 registers, four.
+uint32_t many_waves(uint32_t width, uint32_t type) { return width > 128 || type == ENTRO_F32 ? 4 : 8; }
+
 // How far a call's tiles are split: as many workgroups as fill the chip, tiles of a workgroup not fewer than pay for the
 // join, which is a launch of its own.
 Shape shape_of(const entro_cache *c, const entro_cache_table *t, const entro_cache_query *q) {
-    Shape s = {1, 16, 0};
+    Shape s = {0, 1, 1, 16, 0};
+    const uint32_t width = entro_cache_width(c->head_dim);
+    const uint64_t rows = uint64_t{q->max_new} * (q->q_heads / c->kv_heads);
     uint64_t len = q->max_len;
     if (q->window && len > uint64_t{q->window} + q->sinks + q->max_new + 2 * kTile) len = uint64_t{q->window} + q->sinks + q->max_new + 2 * kTile;
     const uint64_t tiles = (len + kTile - 1) / kTile, units = uint64_t{t->seqs} * c->kv_heads;
-    const uint64_t want = (uint64_t(compute_units()) * 4 + units - 1) / units, can = (tiles + s.least - 1) / s.least;
+    uint64_t groups = units, per_cu = 4;
+    if (rows > 16) {
+        s.waves = rows > 64 ? many_waves(width, q->type) : 2;
+        const uint64_t row_tiles = (rows + 32 * s.waves - 1) / (32 * s.waves), most = 0x3fffffffull / units;
+        s.row_tiles = static_cast<uint32_t>(row_tiles < most ? row_tiles : (most ? most : 1));
+        groups *= s.row_tiles;
+        per_cu = s.waves == 2 ? 4 : 1;
+    }
+    const uint64_t want = (uint64_t(compute_units()) * per_cu + groups - 1) / groups, can = (tiles + s.least - 1) / s.least;
     s.splits = static_cast<uint32_t>(want < can ? want : can);
     if (s.splits < 1) s.splits = 1;
     if (s.splits > 256) s.splits = 256;
-    if (s.splits > 1) s.bytes = uint64_t{q->tokens} * q->q_heads * s.splits * (entro_cache_width(c->head_dim) + 1) * 4;
+    if (s.splits > 1) s.bytes = uint64_t{q->tokens} * q->q_heads * s.splits * (width + 1) * 4;
     return s;
 }
 
-template <typename T>
-void launch(const Pool &p, const Query &a, hipStream_t st) {
-    const dim3 grid(p.seqs * p.kv_heads * a.splits);
-    const dim3 join(static_cast<unsigned>((uint64_t{a.tokens} * a.q_heads + kWG / 64 - 1) / (kWG / 64)));
-#define ENTRO_WIDTH(W)                                                                                  \
-    case W:                                                                                             \
-        hipLaunchKernelGGL((k_attend_few<W, T>), grid, dim3(kWG), 0, st, p, a);                         \
-        if (a.splits > 1) hipLaunchKernelGGL((k_attend_join<W, T>), join, dim3(kWG), 0, st, p, a, 16u); \
-        break
-    switch (p.width) {
-        ENTRO_WIDTH(64);
-        ENTRO_WIDTH(96);
-        ENTRO_WIDTH(128);
-        ENTRO_WIDTH(192);
-        ENTRO_WIDTH(256);
+template <int W, typename T>
+void launch_width(const Pool &p, const Query &a, const Shape &s, hipStream_t st) {
+    constexpr int kMost = W > 128 || sizeof(T) == 4 ? 4 : 8;
+    const uint32_t units = p.seqs * p.kv_heads * a.splits;
+    if (s.waves == 0)
+        hipLaunchKernelGGL((k_attend_few<W, T>), dim3(units), dim3(kWG), 0, st, p, a);
+    else if (s.waves == 2)
+        hipLaunchKernelGGL((k_attend_many<W, T, 2>), dim3(units * s.row_tiles), dim3(128), 0, st, p, a, s.row_tiles);
+    else
+        hipLaunchKernelGGL((k_attend_many<W, T, kMost>), dim3(units * s.row_tiles), dim3(kMost * 64), 0, st, p, a, s.row_tiles);
+    if (a.splits > 1) {
+        const dim3 join(static_cast<unsigned>((uint64_t{a.tokens} * a.q_heads + kWG / 64 - 1) / (kWG / 64)));
+        hipLaunchKernelGGL((k_attend_join<W, T>), join, dim3(kWG), 0, st, p, a, s.waves ? 32 * s.waves : 16u);
     }
-#undef ENTRO_WIDTH
+}
+
+template <typename T>
+void launch(const Pool &p, const Query &a, const Shape &s, hipStream_t st) {
+    switch (p.width) {
+        case 64: return launch_width<64, T>(p, a, s, st);
+        case 96: return launch_width<96, T>(p, a, s, st);
+        case 128: return launch_width<128, T>(p, a, s, st);
+        case 192: return launch_width<192, T>(p, a, s, st);
+        case 256: return launch_width<256, T>(p, a, s, st);
+    }
 }
 
 }  // namespace
@@ -463,7 +722,7 @@ entro_status entro_cache_attend(const entro_cache *c, const entro_cache_table *t
         if (!aligned16(workspace)) return ENTRO_ERR_ALIGN;
         if (workspace_bytes < shape.bytes) return ENTRO_ERR_CAPACITY;
     }
-    if (uint64_t{t->seqs} * c->kv_heads * shape.splits > 0x7fffffffull || uint64_t{q->tokens} * q->q_heads > 0x1ffffffffull) return ENTRO_ERR_SIZE;
+    if (uint64_t{t->seqs} * c->kv_heads * shape.splits * shape.row_tiles > 0x7fffffffull || uint64_t{q->tokens} * q->q_heads > 0x1ffffffffull) return ENTRO_ERR_SIZE;
     const Pool p = pool_of(c, t, q->layer);
     const bool aligned = ((q->q_token_stride | q->q_head_stride) & 7u) == 0;
     float *part_lse = static_cast<float *>(workspace), *part_o = part_lse + uint64_t{q->tokens} * q->q_heads * shape.splits;
@@ -472,9 +731,9 @@ entro_status entro_cache_attend(const entro_cache *c, const entro_cache_table *t
                      part_o, part_lse};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (q->type == ENTRO_F32)
-        launch<float>(p, a, st);
+        launch<float>(p, a, shape, st);
     else
-        launch<uint16_t>(p, a, st);
+        launch<uint16_t>(p, a, shape, st);
     return hip_ok(hipGetLastError(), "entro_cache_attend") ? ENTRO_OK : ENTRO_ERR_DEVICE;
 }
 
