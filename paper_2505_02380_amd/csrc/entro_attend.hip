@@ -29,6 +29,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
+constexpr uint32_t kMostSplits = kWG;          // the join has a lane for each
 constexpr int kTile = 64;                      // tokens a wavefront takes at a time
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -92,6 +93,17 @@ __device__ inline float column_max(float v) {
 __device__ inline float column_sum(float v) {
     v += __shfl_xor(v, 16);
     return v + __shfl_xor(v, 32);
+}
+
+// A position's entry in the table, asked for without waiting for it; what it is worth is looked at where it is used. (A position past the
+// table's slots takes the last one's.)
+__device__ inline int32_t table_entry(const Pool &p, uint32_t b, int32_t at) {
+    return p.slots[uint64_t{b} * p.stride + min(static_cast<uint32_t>(at) >> p.page_shift, p.stride - 1)];
+}
+
+__device__ inline int32_t checked_page(const Pool &p, int32_t id, int32_t at) {
+    const bool there = (static_cast<uint32_t>(id) < p.pages) & (static_cast<uint32_t>(at) >> p.page_shift < p.stride);
+    return there ? id : -1;
 }
 
 // The tiles of kTile tokens that rows at positions first..last see: those of the first tokens, then those of the window.
@@ -169,7 +181,7 @@ __device__ inline void split_halves(const float *x, half8 *hi, half8 *lo) {
 // the probabilities. Keys, values and probabilities so go from memory through registers to the matrix units, with no
 // exchange between lanes but for the maximum. Matrix unit slots that a tile of 16 rows leaves empty cost nothing: the bytes bound it.
 template <int W, typename T>
-__global__ __launch_bounds__(kWG, 2) void k_attend_few(Pool p, Query a) {
+__global__ __launch_bounds__(kWG, W > 128 ? 1 : 2) void k_attend_few(Pool p, Query a) {
     constexpr int kParts = sizeof(T) == 2 ? 1 : 2;         // halves that make a factor of the first product
     constexpr int kWeights = sizeof(T) == 2 ? 2 : 3;       // bf16 numbers that make a weight of the second
     constexpr int kFull = W / 64, kRest = W % 64 ? 1 : 0;   // loads of 64 dimensions of 16 tokens, and of 32
@@ -177,9 +189,13 @@ __global__ __launch_bounds__(kWG, 2) void k_attend_few(Pool p, Query a) {
     __shared__ float merge_o[4][16][W + 4];
     __shared__ float merge_m[4][16], merge_l[4][16];
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6, g = lane >> 4, c = lane & 15u;
-    const uint32_t split = blockIdx.x % a.splits, unit = blockIdx.x / a.splits, head = unit % p.kv_heads, b = unit / p.kv_heads;
+    // Workgroups go to the XCDs in turn. Those of one XCD take the key heads of the same sequence and split, whose codes lie side by side, and
+    // the splits of a sequence go to different XCDs, so that long sequences do not meet on one.
+    const uint32_t r = p.seqs < 8 ? blockIdx.x : blockIdx.x / 8, head = r % p.kv_heads, split = r / p.kv_heads % a.splits, block = r / p.kv_heads / a.splits;
+    const uint32_t b = p.seqs < 8 ? block : 8 * block + ((blockIdx.x - split) & 7u);
+    if (b >= p.seqs) return;
     const Span s = span_of(a.start, p.lengths, b, a.tokens);
-    const uint64_t token_bytes = W, page_bytes = uint64_t{W} << p.page_shift, page_stride = page_bytes * p.kv_heads;
+    const uint64_t page_bytes = uint64_t{W} << p.page_shift, page_stride = page_bytes * p.kv_heads;
     const uint8_t *k_head = p.k + head * page_bytes, *v_head = p.v + head * page_bytes;
     const float *ks_head = p.k_scale + head, *vs_head = p.v_scale + head;
     const uint32_t in_page = (1u << p.page_shift) - 1;
@@ -190,119 +206,159 @@ __global__ __launch_bounds__(kWG, 2) void k_attend_few(Pool p, Query a) {
         const Tiles tiles = tiles_of(p, a, first, last);
         const int32_t per = tiles_per_split(a, tiles.count), begin = static_cast<int32_t>(split) * per, end = min(begin + per, tiles.count);
         if (begin >= end && split > 0) continue;
-        // the lane's row
-        const int64_t my_row = row0 + c;
-        const bool mine = my_row < rows;
-        const uint32_t my_token = static_cast<uint32_t>(s.row) + static_cast<uint32_t>((mine ? my_row : row0) / a.group);
-        const uint32_t my_head = head * a.group + static_cast<uint32_t>((mine ? my_row : row0) % a.group);
-        const int32_t my_pos = s.pos + static_cast<int32_t>(my_token) - s.row;
-        half8 q[kParts][W / 32];
-        float q_factor;
-        {
-            const T *row = static_cast<const T *>(a.q) + my_token * a.q_token_stride + my_head * a.q_head_stride;
-            float x[W / 32][8], most = 0.0f;
+    // A tile's codes and scales as this lane has them: keys of the tokens 16 (c / 4) .., values of the tokens 16 g ..  As soon as a
+    // tile's keys have been multiplied the next tile's are asked for, and so for the values; page numbers come a tile earlier
+    // still, so that nothing waits for them.  (A second set of registers for the codes does not fit.)
+    u32x4 kc[4][kFull], vc[kDims];
+    u32x2 kr[4];
+    float ks = 0.0f, vs = 0.0f;
+    int32_t page = -1, k_page = -1, v_page = -1, k_later = -1, v_later = -1;
+    const auto tile_at = [&](int32_t i) { return tiles.at(min(i, end - 1)) * kTile; };
+    const auto ask_pages = [&](int32_t i) {
+        k_later = table_entry(p, b, tile_at(i) + 16 * static_cast<int32_t>(c >> 2));
+        v_later = table_entry(p, b, tile_at(i) + 16 * static_cast<int32_t>(g));
+    };
+    const auto take_pages = [&](int32_t i) {
+        k_page = checked_page(p, k_later, tile_at(i) + 16 * static_cast<int32_t>(c >> 2));
+        v_page = checked_page(p, v_later, tile_at(i) + 16 * static_cast<int32_t>(g));
+    };
+    const auto ask_keys = [&](int32_t i) {
+        const uint32_t at = (static_cast<uint32_t>(tile_at(i)) + 16 * (c >> 2)) & in_page;
+        const uint8_t *kp = k_head + static_cast<uint32_t>(max(k_page, 0)) * page_stride + (at + (c & 3u)) * W;
 #pragma unroll
-            for (int f = 0; f < W / 32; ++f) {
-                load_eight(row, f < 2 * kFull ? (f / 2) * 64 + g * 16 + (f & 1) * 8 : kFull * 64 + g * 8, p.head_dim, a.aligned, x[f]);
+        for (int t = 0; t < 4; ++t) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(x[f][i]));
-            }
-            const int e = exponent_of(column_max(most));
-            const float sign = a.scale < 0.0f ? -1.0f : 1.0f;
-#pragma unroll
-            for (int f = 0; f < W / 32; ++f) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[f][i] = ldexpf(x[f][i] * sign, 14 - e);
-                split_halves<kParts>(x[f], &q[0][f], &q[kParts - 1][f]);
-            }
-            q_factor = ldexpf(fabsf(a.scale) * kLog2e, e - 14);
+            for (int f = 0; f < kFull; ++f) kc[t][f] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(kp + 4 * t * W + 64 * f + 16 * g));
+            if (kRest) kr[t] = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(kp + 4 * t * W + 64 * kFull + 8 * g));
         }
-        f32x4 o[kDims];
+        ks = ks_head[uint64_t{static_cast<uint32_t>(max(v_page, 0))} * p.kv_heads];
+    };
+    const auto ask_values = [&](int32_t i) {
+        const uint32_t at = (static_cast<uint32_t>(tile_at(i)) + 16 * g) & in_page;
+        const uint8_t *vp = v_head + static_cast<uint32_t>(max(v_page, 0)) * page_stride + (uint64_t{c} << p.page_shift) + at;
 #pragma unroll
-        for (int d = 0; d < kDims; ++d) o[d] = f32x4{0, 0, 0, 0};
-        float m = -INFINITY, l = 0.0f;
+        for (int d = 0; d < kDims; ++d) vc[d] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(vp + (uint64_t{16u * d} << p.page_shift)));
+        vs = vs_head[uint64_t{static_cast<uint32_t>(max(v_page, 0))} * p.kv_heads];
+    };
+    const int32_t i0 = begin + static_cast<int32_t>(wave);
+    // the lane's row
+    const int64_t my_row = row0 + c;
+    const bool mine = my_row < rows;
+    const uint32_t my_token = static_cast<uint32_t>(s.row) + static_cast<uint32_t>((mine ? my_row : row0) / a.group);
+    const uint32_t my_head = head * a.group + static_cast<uint32_t>((mine ? my_row : row0) % a.group);
+    const int32_t my_pos = s.pos + static_cast<int32_t>(my_token) - s.row;
+    
+    half8 q[kParts][W / 32];
+    float q_factor;
+    {
+        const T *row = static_cast<const T *>(a.q) + my_token * a.q_token_stride + my_head * a.q_head_stride;
+        float x[W / 32][8], most = 0.0f;
+        if (i0 < end) ask_pages(i0);
+#pragma unroll
+        for (int f = 0; f < W / 32; ++f)
+            load_eight(row, f < 2 * kFull ? (f / 2) * 64 + g * 16 + (f & 1) * 8 : kFull * 64 + g * 8, p.head_dim, a.aligned, x[f]);
+        if (i0 < end) {
+            take_pages(i0);
+            ask_pages(i0 + 4);
+            ask_keys(i0);
+            ask_values(i0);
+        }
+#pragma unroll
+        for (int f = 0; f < W / 32; ++f)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(x[f][i]));
+        const int e = exponent_of(column_max(most));
+        const float sign = a.scale < 0.0f ? -1.0f : 1.0f;
+#pragma unroll
+        for (int f = 0; f < W / 32; ++f) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[f][i] = ldexpf(x[f][i] * sign, 14 - e);
+            split_halves<kParts>(x[f], &q[0][f], &q[kParts - 1][f]);
+        }
+        q_factor = ldexpf(fabsf(a.scale) * kLog2e, e - 14);
+    }
+    f32x4 o[kDims];
+#pragma unroll
+    for (int d = 0; d < kDims; ++d) o[d] = f32x4{0, 0, 0, 0};
+    float m = -INFINITY, l = 0.0f;
 
-        for (int32_t i = begin + static_cast<int32_t>(wave); i < end; i += 4) {
-            const int32_t t0 = tiles.at(i) * kTile;
-            // this lane loads keys of the tokens 16 (c / 4) .. and values of the tokens 16 g ..
-            const int32_t k_at = t0 + 16 * static_cast<int32_t>(c >> 2), v_at = t0 + 16 * static_cast<int32_t>(g);
-            const int32_t k_page = page_of(p, b, k_at >> p.page_shift), v_page = page_of(p, b, v_at >> p.page_shift);
-            const uint8_t *kp = k_head + static_cast<uint32_t>(max(k_page, 0)) * page_stride + ((static_cast<uint32_t>(k_at) & in_page) + (c & 3u)) * token_bytes;
-            const uint8_t *vp = v_head + static_cast<uint32_t>(max(v_page, 0)) * page_stride + (uint64_t{c} << p.page_shift) + (static_cast<uint32_t>(v_at) & in_page);
-            const uint64_t scale_at = uint64_t{static_cast<uint32_t>(max(v_page, 0))} * p.kv_heads;
-            u32x4 kc[4][kFull + 0], vc[kDims];
-            u32x2 kr[4];
+    for (int32_t i = i0; i < end; i += 4) {
+        const int32_t t0 = tile_at(i);
+        page = v_page;
+        f32x4 z[4];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
+        for (int t = 0; t < 4; ++t) {
+            z[t] = f32x4{0, 0, 0, 0};
 #pragma unroll
-                for (int f = 0; f < kFull; ++f) kc[t][f] = *reinterpret_cast<const u32x4 *>(kp + 4 * t * W + 64 * f + 16 * g);
-                if (kRest) kr[t] = *reinterpret_cast<const u32x2 *>(kp + 4 * t * W + 64 * kFull + 8 * g);
-            }
+            for (int f = 0; f < kFull; ++f) {
+                const half8 k0 = eight_codes(kc[t][f][0], kc[t][f][1]), k1 = eight_codes(kc[t][f][2], kc[t][f][3]);
 #pragma unroll
-            for (int d = 0; d < kDims; ++d) vc[d] = *reinterpret_cast<const u32x4 *>(vp + (uint64_t{16u * d} << p.page_shift));
-            const float ks = ks_head[scale_at], vs = vs_head[scale_at];
-
-            f32x4 z[4];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                z[t] = f32x4{0, 0, 0, 0};
-#pragma unroll
-                for (int f = 0; f < kFull; ++f) {
-                    const half8 k0 = eight_codes(kc[t][f][0], kc[t][f][1]), k1 = eight_codes(kc[t][f][2], kc[t][f][3]);
-#pragma unroll
-                    for (int n = 0; n < kParts; ++n) {
-                        z[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[n][2 * f], z[t], 0, 0, 0);
-                        z[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q[n][2 * f + 1], z[t], 0, 0, 0);
-                    }
-                }
-                if (kRest) {
-                    const half8 k0 = eight_codes(kr[t][0], kr[t][1]);
-#pragma unroll
-                    for (int n = 0; n < kParts; ++n) z[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[n][2 * kFull], z[t], 0, 0, 0);
+                for (int n = 0; n < kParts; ++n) {
+                    z[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[n][2 * f], z[t], 0, 0, 0);
+                    z[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q[n][2 * f + 1], z[t], 0, 0, 0);
                 }
             }
-            // scores in units of log2
-            const float factor = ks * q_factor;
-            float top = -INFINITY;
+            if (kRest) {
+                const half8 k0 = eight_codes(kr[t][0], kr[t][1]);
+#pragma unroll
+                for (int n = 0; n < kParts; ++n) z[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[n][2 * kFull], z[t], 0, 0, 0);
+            }
+        }
+        // scores in units of log2; a page without a token that is seen may hold anything as its scale
+        const float factor = fmaxf(ks * q_factor, 1e-37f);
+        take_pages(i + 4);
+        ask_pages(i + 8);
+        ask_keys(i + 4);
+        if (!(t0 + kTile - 1 <= first && (!a.window || static_cast<uint32_t>(last - t0) < a.window) && __all(page >= 0))) {
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const int32_t key = v_at + 4 * t + j;
-                    const bool seen = v_page >= 0 && key <= my_pos && (!a.window || static_cast<uint32_t>(my_pos - key) < a.window || static_cast<uint32_t>(key) < a.sinks);
-                    z[t][j] = seen ? z[t][j] * factor : -INFINITY;
-                    top = fmaxf(top, z[t][j]);
+                    const int32_t key = t0 + 16 * static_cast<int32_t>(g) + 4 * t + j;
+                    const bool seen = (page >= 0) & (key <= my_pos) &
+                                      ((a.window == 0) | (static_cast<uint32_t>(my_pos - key) < a.window) | (static_cast<uint32_t>(key) < a.sinks));
+                    z[t][j] = seen ? z[t][j] : -INFINITY;
                 }
-            const float now = fmaxf(m, column_max(top)), base = now == -INFINITY ? 0.0f : now;
-            const float by = __builtin_amdgcn_exp2f(m - base);
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = fmaxf(top, z[t][j]);
+        const float scale = top > -INFINITY ? vs : 0.0f;
+        top = column_max(top * factor);
+        // sums may stand at 2^8 times their unit before they are brought to a new one
+        if (__any(top > m + 8.0f)) {
+            const float now = fmaxf(m, top), by = __builtin_amdgcn_exp2f(m - (now == -INFINITY ? 0.0f : now));
             m = now;
             l *= by;
 #pragma unroll
             for (int d = 0; d < kDims; ++d) o[d] *= by;
-            // a page without a token that is seen may hold anything as its scale
-            const float scale = top > -INFINITY ? vs : 0.0f;
-            bf16x8 w[2][kWeights];
+        }
+        const float base = m == -INFINITY ? 0.0f : m;
+        bf16x8 w[2][kWeights];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float x[8];
+        for (int h = 0; h < 2; ++h) {
+            float x[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float e = __builtin_amdgcn_exp2f(z[2 * h + j / 4][j & 3] - base);
-                    l += e;
-                    x[j] = e * scale;
-                }
-                split_weights<kWeights>(x, w[h]);
+            for (int j = 0; j < 8; ++j) {
+                const float e = __builtin_amdgcn_exp2f(fmaf(z[2 * h + j / 4][j & 3], factor, -base));
+                l += e;
+                x[j] = e * scale;
             }
+            split_weights<kWeights>(x, w[h]);
+        }
 #pragma unroll
-            for (int d = 0; d < kDims; ++d) {
-                const bf16x8 v0 = eight_values(vc[d][0], vc[d][1]), v1 = eight_values(vc[d][2], vc[d][3]);
+        for (int d = 0; d < kDims; ++d) {
+            const bf16x8 v0 = eight_values(vc[d][0], vc[d][1]), v1 = eight_values(vc[d][2], vc[d][3]);
 #pragma unroll
-                for (int n = 0; n < kWeights; ++n) {
-                    o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, w[0][n], o[d], 0, 0, 0);
-                    o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, w[1][n], o[d], 0, 0, 0);
-                }
+            for (int n = 0; n < kWeights; ++n) {
+                o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, w[0][n], o[d], 0, 0, 0);
+                o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, w[1][n], o[d], 0, 0, 0);
             }
         }
+        ask_values(i + 4);
+    }
         l = column_sum(l);
         // the four wavefronts' parts
         __syncthreads();
@@ -424,34 +480,30 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void k_attend_many(
         float ks = 0.0f, vs = 0.0f;
         int32_t s_ok = 0;
         const auto ask_pages = [&](int32_t i) {
-            if (i >= end) return;
-            const int32_t t0 = tiles.at(i) * kTile;
+            const int32_t t0 = tiles.at(min(i, end - 1)) * kTile;
 #pragma unroll
             for (int n = 0; n < kChunks; ++n) {
                 const int32_t ch = n * kThreads + static_cast<int32_t>(tid);
-                if (kThreads * kChunks != W * 4 && ch >= W * 4) continue;
-                k_page[n] = page_of(p, b, (t0 + ch / (W / 16)) >> p.page_shift);
-                v_page[n] = page_of(p, b, (t0 + 16 * (ch & 3)) >> p.page_shift);
+                k_page[n] = table_entry(p, b, t0 + min(ch / (W / 16), kTile - 1));
+                v_page[n] = table_entry(p, b, t0 + 16 * (ch & 3));
             }
-            if (tid < 4) s_page = page_of(p, b, (t0 + 16 * static_cast<int32_t>(tid)) >> p.page_shift);
+            s_page = table_entry(p, b, t0 + 16 * static_cast<int32_t>(tid & 3u));
         };
         const auto ask_codes = [&](int32_t i) {
-            if (i >= end) return;
-            const int32_t t0 = tiles.at(i) * kTile;
+            const int32_t t0 = tiles.at(min(i, end - 1)) * kTile;
 #pragma unroll
             for (int n = 0; n < kChunks; ++n) {
-                const int32_t ch = n * kThreads + static_cast<int32_t>(tid);
-                if (kThreads * kChunks != W * 4 && ch >= W * 4) continue;
-                const uint32_t k_at = static_cast<uint32_t>(t0 + ch / (W / 16)), v_at = static_cast<uint32_t>(t0 + 16 * (ch & 3));
-                kc[n] = *reinterpret_cast<const u32x4 *>(k_head + static_cast<uint32_t>(max(k_page[n], 0)) * page_stride + (k_at & in_page) * W + 16 * (ch % (W / 16)));
-                vc[n] = *reinterpret_cast<const u32x4 *>(v_head + static_cast<uint32_t>(max(v_page[n], 0)) * page_stride + (static_cast<uint32_t>(ch >> 2) << p.page_shift) + (v_at & in_page));
+                const int32_t ch = min(n * kThreads + static_cast<int32_t>(tid), W * 4 - 1);
+                const int32_t k_at = t0 + ch / (W / 16), v_at = t0 + 16 * (ch & 3);
+                const uint64_t k_id = static_cast<uint32_t>(max(checked_page(p, k_page[n], k_at), 0)), v_id = static_cast<uint32_t>(max(checked_page(p, v_page[n], v_at), 0));
+                kc[n] = *reinterpret_cast<const u32x4 *>(k_head + k_id * page_stride + (static_cast<uint32_t>(k_at) & in_page) * W + 16 * (ch % (W / 16)));
+                vc[n] = *reinterpret_cast<const u32x4 *>(v_head + v_id * page_stride + (static_cast<uint32_t>(ch >> 2) << p.page_shift) + (static_cast<uint32_t>(v_at) & in_page));
             }
-            if (tid < 4) {
-                const uint64_t at = uint64_t{static_cast<uint32_t>(max(s_page, 0))} * p.kv_heads + head;
-                ks = p.k_scale[at];
-                vs = p.v_scale[at];
-                s_ok = s_page >= 0;
-            }
+            const int32_t id = checked_page(p, s_page, t0 + 16 * static_cast<int32_t>(tid & 3u));
+            const uint64_t at = uint64_t{static_cast<uint32_t>(max(id, 0))} * p.kv_heads + head;
+            ks = p.k_scale[at];
+            vs = p.v_scale[at];
+            s_ok = id >= 0;
         };
         const auto to_lds = [&](int half) {
 #pragma unroll
@@ -473,12 +525,14 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void k_attend_many(
             }
         };
         __syncthreads();                           // the last group's tiles have been read
-        ask_pages(begin);
-        ask_codes(begin);
-        ask_pages(begin + 1);
-        if (begin < end) to_lds(0);
-        ask_codes(begin + 1);
-        ask_pages(begin + 2);
+        if (begin < end) {
+            ask_pages(begin);
+            ask_codes(begin);
+            ask_pages(begin + 1);
+            to_lds(0);
+            ask_codes(begin + 1);
+            ask_pages(begin + 2);
+        }
         __syncthreads();
 
         for (int32_t i = begin; i < end; ++i) {
@@ -577,44 +631,62 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void k_attend_many(
     }
 }
 
-// Joins the parts of rows whose tiles were split. A wavefront per row and head.
+// Joins the parts of rows whose tiles were split. A workgroup per row and head: its lanes stand for four dimensions each, and as often as
+// they cover a row they take parts in turn.
 template <int W, typename T>
 __global__ __launch_bounds__(kWG) void k_attend_join(Pool p, Query a, uint32_t rows_per_tile) {
-    const uint32_t lane = threadIdx.x & 63u;
-    const uint64_t at = uint64_t{blockIdx.x} * (kWG / 64) + (threadIdx.x >> 6);
-    if (at >= uint64_t{a.tokens} * a.q_heads) return;
-    const uint32_t token = static_cast<uint32_t>(at / a.q_heads), h = static_cast<uint32_t>(at % a.q_heads);
-    uint32_t lo = 0, hi = p.seqs;                // the last sequence that starts at or before the row
-    while (hi - lo > 1) {
-        const uint32_t mid = (lo + hi) / 2;
-        if (a.start[mid] <= static_cast<int32_t>(token)) lo = mid; else hi = mid;
-    }
-    const Span s = span_of(a.start, p.lengths, lo, a.tokens);
-    if (static_cast<int32_t>(token) < s.row || static_cast<int32_t>(token) >= s.row + s.count) return;
-    const int64_t rows = int64_t{s.count} * a.group, row = int64_t(token - static_cast<uint32_t>(s.row)) * a.group + h % a.group;
-    const int64_t row0 = row / rows_per_tile * rows_per_tile;
-    const Tiles tiles = tiles_of(p, a, s.pos + static_cast<int32_t>(row0 / a.group),
-                                 s.pos + static_cast<int32_t>(min(row0 + rows_per_tile - 1, rows - 1) / a.group));
-    const int32_t per = tiles_per_split(a, tiles.count);
-    const uint32_t parts = static_cast<uint32_t>(max((tiles.count + per - 1) / per, 1));
-    float most = -INFINITY;
-    for (uint32_t i = lane; i < parts; i += 64) most = fmaxf(most, a.part_lse[at * a.splits + i]);
-    for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
-    const float base = most == -INFINITY ? 0.0f : most;
-    float sum = 0.0f, x[W / 64 + 1] = {};
-    for (uint32_t i = 0; i < parts; ++i) {
-        const float by = __builtin_amdgcn_exp2f(a.part_lse[at * a.splits + i] - base);
-        sum += by;
+    constexpr int kLanes = W / 4, kSets = kWG / kLanes;
+    __shared__ f32x4 sums[kSets][kLanes];
+    __shared__ float wave_most[kWG / 64], wave_sum[kWG / 64], shares[kWG];
+    const uint32_t tid = threadIdx.x, set = tid / kLanes, d = tid % kLanes;
+    const uint32_t h = blockIdx.x % a.q_heads, b = blockIdx.x / a.q_heads;
+    const Span s = span_of(a.start, p.lengths, b, a.tokens);
+    for (int32_t nth = static_cast<int32_t>(blockIdx.y); nth < s.count; nth += static_cast<int32_t>(gridDim.y)) {
+        const uint32_t token = static_cast<uint32_t>(s.row + nth);
+        const uint64_t at = uint64_t{token} * a.q_heads + h;
+        const int64_t rows = int64_t{s.count} * a.group, row = int64_t{nth} * a.group + h % a.group;
+        const int64_t row0 = row / rows_per_tile * rows_per_tile;
+        const Tiles tiles = tiles_of(p, a, s.pos + static_cast<int32_t>(row0 / a.group),
+                                     s.pos + static_cast<int32_t>(min(row0 + rows_per_tile - 1, rows - 1) / a.group));
+        const int32_t per = tiles_per_split(a, tiles.count);
+        const uint32_t parts = static_cast<uint32_t>(max((tiles.count + per - 1) / per, 1));
+        const float *lse = a.part_lse + at * a.splits;
+        const f32x4 *part = reinterpret_cast<const f32x4 *>(a.part_o + at * a.splits * W);
+        // every part's share, a lane each (there are at most kMostSplits)
+        const float mine = tid < parts ? lse[tid] : -INFINITY;
+        float most = mine;
+        for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+        if ((tid & 63u) == 0) wave_most[tid >> 6] = most;
+        __syncthreads();
+        for (int i = 0; i < kWG / 64; ++i) most = fmaxf(most, wave_most[i]);
+        const float base = most == -INFINITY ? 0.0f : most;
+        const float share = __builtin_amdgcn_exp2f(mine - base);
+        shares[tid] = share;
+        float sum = share;
+        for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+        if ((tid & 63u) == 0) wave_sum[tid >> 6] = sum;
+        __syncthreads();
+        sum = 0.0f;
+        for (int i = 0; i < kWG / 64; ++i) sum += wave_sum[i];
+        f32x4 x = {0, 0, 0, 0};
+        if (set < kSets) {
+#pragma unroll 4
+            for (uint32_t i = set; i < parts; i += kSets) x += part[i * kLanes + d] * shares[i];
+            sums[set][d] = x;
+        }
+        __syncthreads();
+        if (set == 0) {
 #pragma unroll
-        for (int j = 0; j < (W + 63) / 64; ++j)
-            if (64 * j + lane < p.head_dim) x[j] += by * a.part_o[(at * a.splits + i) * W + 64 * j + lane];
-    }
-    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+            for (int i = 1; i < kSets; ++i) x += sums[i][d];
+            const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+            T *out = static_cast<T *>(a.out) + token * a.out_token_stride + h * a.out_head_stride;
 #pragma unroll
-    for (int j = 0; j < (W + 63) / 64; ++j)
-        if (64 * j + lane < p.head_dim)
-            store_as(static_cast<T *>(a.out) + token * a.out_token_stride + h * a.out_head_stride + 64 * j + lane, sum == sum ? x[j] * inv : sum);
-    if (lane == 0 && a.lse) a.lse[at] = sum > 0.0f ? (base + __builtin_amdgcn_logf(sum)) * kLn2 : (sum == sum ? -INFINITY : sum);
+            for (int j = 0; j < 4; ++j)
+                if (4 * d + j < p.head_dim) store_as(out + 4 * d + j, sum == sum ? x[j] * inv : sum);
+        }
+        if (tid == 0 && a.lse) a.lse[at] = sum > 0.0f ? (base + __builtin_amdgcn_logf(sum)) * kLn2 : (sum == sum ? -INFINITY : sum);
+        __syncthreads();
+    }
 }
 
 entro_status check_query_sizes(const entro_cache *c, const entro_cache_query *q) {
@@ -636,7 +708,7 @@ entro_status check_query(const entro_cache *c, const entro_cache_query *q) {
 
 struct Shape {
     uint32_t waves;                // 0: the kernel for few rows; otherwise wavefronts of the one for many
-    uint32_t row_tiles, splits, least;
+    uint32_t row_tiles, splits, least, join_rows;
     uint64_t bytes;
 };
 
@@ -652,13 +724,13 @@ uint32_t many_waves(uint32_t width, uint32_t type) { return width > 128 || type 
 // How far a call's tiles are split: as many workgroups as fill the chip, tiles of a workgroup not fewer than pay for the
 // join, which is a launch of its own.
 Shape shape_of(const entro_cache *c, const entro_cache_table *t, const entro_cache_query *q) {
-    Shape s = {0, 1, 1, 16, 0};
+    Shape s = {0, 1, 1, 16, q->max_new < 1 ? 1 : q->max_new > 65535 ? 65535 : q->max_new, 0};
     const uint32_t width = entro_cache_width(c->head_dim);
     const uint64_t rows = uint64_t{q->max_new} * (q->q_heads / c->kv_heads);
     uint64_t len = q->max_len;
     if (q->window && len > uint64_t{q->window} + q->sinks + q->max_new + 2 * kTile) len = uint64_t{q->window} + q->sinks + q->max_new + 2 * kTile;
     const uint64_t tiles = (len + kTile - 1) / kTile, units = uint64_t{t->seqs} * c->kv_heads;
-    uint64_t groups = units, per_cu = 4;
+    uint64_t groups = units, per_cu = 2;
     if (rows > 16) {
         s.waves = rows > 64 ? many_waves(width, q->type) : 2;
         const uint64_t row_tiles = (rows + 32 * s.waves - 1) / (32 * s.waves), most = 0x3fffffffull / units;
@@ -666,10 +738,25 @@ Shape shape_of(const entro_cache *c, const entro_cache_table *t, const entro_cac
         groups *= s.row_tiles;
         per_cu = s.waves == 2 ? 4 : 1;
     }
-    const uint64_t want = (uint64_t(compute_units()) * per_cu + groups - 1) / groups, can = (tiles + s.least - 1) / s.least;
+    const uint64_t cus = static_cast<uint64_t>(compute_units());
+    uint64_t want, can;
+    if (s.waves == 0 && units * 4 > cus * 2) {
+        // the heads of many sequences fill the chip; pieces of at most 96 tiles keep one long sequence from being the last
+        // alone (8192 tokens of 64 sequences in one, two, four pieces: 128, 130, 127 us; 4096 of 32 with 32 heads: 139, 147, 154)
+        want = can = (tiles + 95) / 96;
+    } else if (s.waves == 0) {
+        // two workgroups a compute unit are enough (131072 tokens, 8 heads: 64 pieces 55 us, 128 pieces 60 us); below 24 tiles the
+        // join costs more than it gives (9 tiles: 8.1 us in one piece, 11.3 in two)
+        want = cus * 2 / units;
+        can = tiles < 24 ? 1 : tiles / 8;
+    } else {
+        want = (cus * per_cu + groups - 1) / groups;
+        can = (tiles + s.least - 1) / s.least;
+    }
     s.splits = static_cast<uint32_t>(want < can ? want : can);
     if (s.splits < 1) s.splits = 1;
-    if (s.splits > 256) s.splits = 256;
+    if (s.splits > kMostSplits) s.splits = kMostSplits;
+    if (s.waves == 0 && tiles) s.least = static_cast<uint32_t>((tiles + s.splits - 1) / s.splits);
     if (s.splits > 1) s.bytes = uint64_t{q->tokens} * q->q_heads * s.splits * (width + 1) * 4;
     return s;
 }
@@ -679,13 +766,13 @@ void launch_width(const Pool &p, const Query &a, const Shape &s, hipStream_t st)
     constexpr int kMost = W > 128 || sizeof(T) == 4 ? 4 : 8;
     const uint32_t units = p.seqs * p.kv_heads * a.splits;
     if (s.waves == 0)
-        hipLaunchKernelGGL((k_attend_few<W, T>), dim3(units), dim3(kWG), 0, st, p, a);
+        hipLaunchKernelGGL((k_attend_few<W, T>), dim3(p.seqs < 8 ? units : (p.seqs + 7) / 8 * 8 * p.kv_heads * a.splits), dim3(kWG), 0, st, p, a);
     else if (s.waves == 2)
         hipLaunchKernelGGL((k_attend_many<W, T, 2>), dim3(units * s.row_tiles), dim3(128), 0, st, p, a, s.row_tiles);
     else
         hipLaunchKernelGGL((k_attend_many<W, T, kMost>), dim3(units * s.row_tiles), dim3(kMost * 64), 0, st, p, a, s.row_tiles);
     if (a.splits > 1) {
-        const dim3 join(static_cast<unsigned>((uint64_t{a.tokens} * a.q_heads + kWG / 64 - 1) / (kWG / 64)));
+        const dim3 join(p.seqs * a.q_heads, s.join_rows);
         hipLaunchKernelGGL((k_attend_join<W, T>), join, dim3(kWG), 0, st, p, a, s.waves ? 32 * s.waves : 16u);
     }
 }
@@ -722,10 +809,12 @@ entro_status entro_cache_attend(const entro_cache *c, const entro_cache_table *t
         if (!aligned16(workspace)) return ENTRO_ERR_ALIGN;
         if (workspace_bytes < shape.bytes) return ENTRO_ERR_CAPACITY;
     }
-    if (uint64_t{t->seqs} * c->kv_heads * shape.splits * shape.row_tiles > 0x7fffffffull || uint64_t{q->tokens} * q->q_heads > 0x1ffffffffull) return ENTRO_ERR_SIZE;
+    if (uint64_t{t->seqs} * c->kv_heads * shape.splits * shape.row_tiles > 0x7fffffffull ||
+        uint64_t{t->seqs} * q->q_heads > 0x7fffffffull || uint64_t{q->tokens} * q->q_heads > 0x7fffffffull)
+        return ENTRO_ERR_SIZE;
     const Pool p = pool_of(c, t, q->layer);
     const bool aligned = ((q->q_token_stride | q->q_head_stride) & 7u) == 0;
-    float *part_lse = static_cast<float *>(workspace), *part_o = part_lse + uint64_t{q->tokens} * q->q_heads * shape.splits;
+    float *part_o = static_cast<float *>(workspace), *part_lse = part_o + uint64_t{q->tokens} * q->q_heads * shape.splits * p.width;
     const Query a = {q->q, q->out, q->lse, q->q_token_stride, q->q_head_stride, q->out_token_stride, q->out_head_stride, q->start,
                      q->tokens, q->q_heads, q->q_heads / c->kv_heads, q->window, q->sinks, q->scale, aligned, shape.splits, shape.least,
                      part_o, part_lse};

@@ -210,6 +210,39 @@ def test_attend_with_extreme_queries_and_scales(kind, new):
     check_attend(pool, table, lengths, q, start, kind, out, lse, dim ** -0.5)
 
 
+@pytest.mark.parametrize("kind,new", [("bf16", 1), ("f32", 1), ("bf16", 20), ("f32", 70)])
+def test_attend_looks_at_no_page_without_seen_tokens(kind, new):
+    """Pages that a table names for tokens to come, and pages that have left the window: their scales may be NaN."""
+    rng = np.random.default_rng(16)
+    lengths, heads, dim, page = [200, 70], 2, 128, 16
+    pool, table = make(rng, 2, [360, 300], heads, dim, page)
+    pool.v_scale[:] = pool.k_scale[:] = np.nan
+    for b, n in enumerate(lengths):
+        for slot in range(-(-n // page)):
+            if slot == 0 or (slot + 1) * page > n - new - 40 or new > 1:
+                pool.k_scale[0, table[b, slot]], pool.v_scale[0, table[b, slot]] = 0.03, 0.02
+    start = starts([new, new])
+    q = rounded(rng.standard_normal((2 * new, 4, dim)), kind)
+    window = 40 if new == 1 else 0
+    out, lse = run_attend(cache_of(pool), table, lengths, q, start, kind, window=window, sinks=4, max_len=360)
+    pool.k_scale, pool.v_scale = np.nan_to_num(pool.k_scale, nan=1e30), np.nan_to_num(pool.v_scale, nan=1e30)
+    check_attend(pool, table, lengths, q, start, kind, out, lse, dim ** -0.5, window, 4)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("dim,lengths,new,group", [(256, [2100, 30], [1, 1], 2), (192, [1700], [1], 5), (256, [1300], [40], 2), (200, [1800, 900], [17, 3], 8),
+                                                   (64, [6300] + [40] * 70, [1] * 71, 1)])
+def test_attend_splits_of_every_width(kind, dim, lengths, new, group):
+    rng = np.random.default_rng(17)
+    heads, page = 2, 32
+    pool, table = make(rng, len(lengths), lengths, heads, dim, page)
+    scales(rng, pool, table)
+    start = starts(new)
+    q = rounded(rng.standard_normal((start[-1], heads * group, dim)) * 2, kind)
+    out, lse = run_attend(cache_of(pool), table, lengths, q, start, kind)
+    check_attend(pool, table, lengths, q, start, kind, out, lse, dim ** -0.5)
+
+
 def test_attend_long_context_splits_and_repeats():
     """A context long enough to be split over the chip; the same call again gives the same bits."""
     rng = np.random.default_rng(10)
