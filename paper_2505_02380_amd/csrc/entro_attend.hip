@@ -95,17 +95,6 @@ __device__ inline float column_sum(float v) {
     return v + __shfl_xor(v, 32);
 }
 
-// A position's entry in the table, asked for without waiting for it; what it is worth is looked at where it is used. (A position past the
-// table's slots takes the last one's.)
-__device__ inline int32_t table_entry(const Pool &p, uint32_t b, int32_t at) {
-    return p.slots[uint64_t{b} * p.stride + min(static_cast<uint32_t>(at) >> p.page_shift, p.stride - 1)];
-}
-
-__device__ inline int32_t checked_page(const Pool &p, int32_t id, int32_t at) {
-    const bool there = (static_cast<uint32_t>(id) < p.pages) & (static_cast<uint32_t>(at) >> p.page_shift < p.stride);
-    return there ? id : -1;
-}
-
 // The tiles of kTile tokens that rows at positions first..last see: those of the first tokens, then those of the window.
 struct Tiles {
     int32_t sinks, from, count;

@@ -97,11 +97,15 @@ __device__ inline Span span_of(const int32_t *start, const int32_t *lengths, uin
     return s;
 }
 
-// The page of a slot, or -1.
-__device__ inline int32_t page_of(const Pool &p, uint32_t b, int32_t slot) {
-    if (slot < 0 || slot >= static_cast<int32_t>(p.stride)) return -1;
-    const int32_t id = p.slots[uint64_t{b} * p.stride + static_cast<uint32_t>(slot)];
-    return static_cast<uint32_t>(id) < p.pages ? id : -1;
+// A position's entry in the table, asked for without waiting for it; what it is worth is looked at where it is used. (A position past the
+// table's slots takes the last one's.)
+__device__ inline int32_t table_entry(const Pool &p, uint32_t b, int32_t at) {
+    return p.slots[uint64_t{b} * p.stride + min(static_cast<uint32_t>(at) >> p.page_shift, p.stride - 1)];
+}
+
+__device__ inline int32_t checked_page(const Pool &p, int32_t id, int32_t at) {
+    const bool there = (static_cast<uint32_t>(id) < p.pages) & (static_cast<uint32_t>(at) >> p.page_shift < p.stride);
+    return there ? id : -1;
 }
 
 __device__ inline float bf16_to_f32(uint16_t b) { return __uint_as_float(uint32_t{b} << 16); }

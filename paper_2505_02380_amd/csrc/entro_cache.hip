@@ -16,9 +16,6 @@ constexpr int kScanWG = 1024;
 constexpr int32_t kNoOwner = 0x7fffffff;      // owner[page]: no row holds it
 constexpr int32_t kFullSomewhere = -1;        // owner[page]: to some row it is a full page
 
-template <typename T> __device__ inline float load_as_f32(const T *p);
-template <> __device__ inline float load_as_f32<float>(const float *p) { return *p; }
-template <> __device__ inline float load_as_f32<uint16_t>(const uint16_t *p) { return bf16_to_f32(*p); }
 template <typename T> __device__ inline T store_from_f32(float f);
 template <> __device__ inline float store_from_f32<float>(float f) { return f; }
 template <> __device__ inline uint16_t store_from_f32<uint16_t>(float f) { return f32_to_bf16(f); }
@@ -28,90 +25,286 @@ struct Rows {
     uint64_t token_stride[2], head_stride[2];
     const int32_t *start;
     uint32_t tokens;
+    bool aligned;                // rows begin at multiples of 16 bytes
 };
 
-// Eq. 1's grid map with z = 128: NaN to the zero-point, infinities to the ends.
-__device__ inline uint32_t grid_code(float x, float scale) {
-    if (!(scale > 0.0f)) return 128u;
-    float q = rintf(x / scale);
-    q = q == q ? fminf(fmaxf(q, -127.0f), 127.0f) : 0.0f;
-    return static_cast<uint32_t>(static_cast<int32_t>(q) + 128);
+// Eq. 1's grid map with z = 128. x / scale is its correctly rounded quotient: by the reciprocal (itself correctly rounded), the remainder, which
+// fma gives exactly, and one correction, where reciprocal and remainder are normal numbers, which they are for scales
+// of 2^-100 and more; smaller ones and blocks with elements that are no numbers divide. Adding 1.5 * 2^23 + 128 rounds the
+// quotient to the nearest even integer and leaves the code in the low byte.
+struct Grid {
+    float scale, inverse;
+    bool divide;
+};
+
+__device__ inline Grid grid_of(float scale, bool numbers) {
+    return {scale, 1.0f / scale, !numbers || scale < 7.9e-31f};
 }
 
-// One workgroup per block that a sequence writes to, and head; k and v one after the other.
+__device__ inline uint32_t code_by_division(float x, float scale) {
+    float q = rintf(x / scale);
+    q = q == q ? fminf(fmaxf(q, -127.0f), 127.0f) : 0.0f;   // NaN to the zero-point, infinities to the ends
+    return scale > 0.0f ? static_cast<uint32_t>(static_cast<int32_t>(q) + 128) : 128u;
+}
+
+// The code stands in the low byte.
+__device__ inline uint32_t code_by_inverse(float x, const Grid &g) {
+    const float q = x * g.inverse;
+    return __float_as_uint(fmaf(fmaf(-q, g.scale, x), g.inverse, q) + 12583040.0f);
+}
+
+__device__ inline uint32_t four_codes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
+}
+
+__device__ inline uint32_t byte_of(uint32_t w, uint32_t i) { return (w >> (8 * i)) & 0xffu; }
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// A block of a sequence and a head: what LANES lanes write or read together. They take it in patches of 4 tokens x 8 dimensions,
+// the smallest that is whole words of rows (16 bytes in bf16), of key codes (8 bytes of a token) and of value codes (4 bytes of a
+// dimension). Neighbouring lanes have neighbouring dimensions of the keys, but neighbouring tokens of the values, as the codes lie.
+struct Block {
+    int64_t row;                 // of the block's token 0 (it may lie before the tensor)
+    uint32_t t0, t1;             // tokens t0 .. t1 - 1 have rows
+    int32_t entry, at;           // of the table, and the position it stands for: checked_page's
+};
+
+struct Patch {
+    uint32_t t, d;               // its first token and dimension
+};
+
+// The `nth` of `patches` patches; kv: 0 keys, 1 values.
+__device__ inline Patch patch_of(const Pool &p, uint32_t nth, int kv) {
+    const uint32_t quads = 1u << (p.page_shift - 2), eights = (p.head_dim + 7) / 8;
+    if (kv) return {4 * (nth & (quads - 1)), 8 * (nth >> (p.page_shift - 2))};
+    return {4 * (nth / eights), 8 * (nth % eights)};
+}
+
+// The block with number w of `blocks` per sequence and kv_heads per block, then every `blocks`-th one after it; f is called with each.
+template <typename F>
+__device__ inline void each_block(const Pool &p, const Rows &r, uint32_t blocks, uint32_t w, F f) {
+    const uint32_t head = w % p.kv_heads, nth = w / p.kv_heads % blocks, b = w / p.kv_heads / blocks;
+    const Span s = span_of(r.start, p.lengths, b, r.tokens);
+    if (s.count == 0) return;
+    const int32_t first = max(s.pos, 0) >> p.page_shift, last = (s.length - 1) >> p.page_shift;
+    for (int32_t block = first + static_cast<int32_t>(nth); block <= last; block += static_cast<int32_t>(blocks)) {
+        const int32_t at = block << p.page_shift;
+        Block x;
+        x.entry = table_entry(p, b, at);
+        x.at = at;
+        x.row = int64_t{s.row} + at - s.pos;
+        x.t0 = static_cast<uint32_t>(max(s.pos - at, 0));
+        x.t1 = static_cast<uint32_t>(min(s.length - at, 1 << p.page_shift));
+        f(x, head);
+    }
+}
+
+// A patch's rows as they lie in memory: asked for all at once (rows that are not there: others in their place).
 template <typename T>
-__global__ __launch_bounds__(kWG) void k_append(Pool p, Rows r, uint32_t blocks_per_seq, uint32_t work) {
-    __shared__ uint32_t most[kWG / 64];
-    const uint32_t tid = threadIdx.x, pt = 1u << p.page_shift;
-    for (uint32_t w = blockIdx.x; w < work; w += gridDim.x) {
-        const uint32_t head = w % p.kv_heads, nth = w / p.kv_heads % blocks_per_seq, b = w / p.kv_heads / blocks_per_seq;
-        const Span s = span_of(r.start, p.lengths, b, r.tokens);
-        if (s.count == 0) continue;
-        const int32_t first = max(s.pos, 0) >> p.page_shift, last = (s.length - 1) >> p.page_shift;
-        for (int32_t block = first + static_cast<int32_t>(nth); block <= last; block += static_cast<int32_t>(blocks_per_seq)) {
-            const int32_t page = page_of(p, b, block);
-            if (page < 0) continue;
-            const int32_t at = block << p.page_shift;
-            const uint32_t t0 = static_cast<uint32_t>(max(s.pos - at, 0)), t1 = static_cast<uint32_t>(min(s.length - at, static_cast<int32_t>(pt)));
-            for (int kv = 0; kv < 2; ++kv) {
-                const uint64_t unit = uint64_t{static_cast<uint32_t>(page)} * p.kv_heads + head;
-                uint8_t *codes = (kv ? p.v : p.k) + unit * pt * p.width;
-                float *scale_at = (kv ? p.v_scale : p.k_scale) + unit;
-                const T *x = static_cast<const T *>(r.x[kv]) + uint64_t(int64_t{s.row} + at - s.pos) * r.token_stride[kv] + head * r.head_stride[kv];
-                const uint32_t n = (t1 - t0) * p.head_dim;
-                uint32_t m = 0;
-                for (uint32_t i = tid; i < n; i += kWG) {
-                    const uint32_t t = t0 + i / p.head_dim, d = i % p.head_dim;
-                    const uint32_t bits = __float_as_uint(load_as_f32(x + t * r.token_stride[kv] + d)) & 0x7fffffffu;
-                    m = max(m, bits < 0x7f800000u ? bits : 0u);
+struct RawPatch {
+    u32x4 w[4][sizeof(T) / 2];
+};
+
+template <typename T>
+__device__ inline RawPatch<T> ask_patch(const T *x, uint64_t token_stride, const Patch &a, const Block &b, uint32_t head_dim, bool aligned) {
+    RawPatch<T> r;
+    if (aligned && a.d + 8 <= head_dim) {
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            const u32x4 *row = reinterpret_cast<const u32x4 *>(x + min(max(a.t + j, b.t0), b.t1 - 1) * token_stride + a.d);
+#pragma unroll
+            for (uint32_t i = 0; i < sizeof(T) / 2; ++i) r.w[j][i] = row[i];
+        }
+    } else {
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            const T *row = x + min(max(a.t + j, b.t0), b.t1 - 1) * token_stride;
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) {
+                const T e = row[min(a.d + i, head_dim - 1)];
+                if (sizeof(T) == 2) {
+                    const uint32_t h = static_cast<uint32_t>(e) << (16 * (i & 1));
+                    r.w[j][0][i / 2] = i & 1 ? r.w[j][0][i / 2] | h : h;
+                } else {
+                    r.w[j][(i / 4) % (sizeof(T) / 2)][i & 3] = __builtin_bit_cast(uint32_t, static_cast<float>(e));
                 }
-                for (int o = 32; o; o >>= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), o)));
-                if ((tid & 63u) == 0) most[tid >> 6] = m;
-                const float old = t0 ? *scale_at : 0.0f;
-                __syncthreads();
-                for (int i = 0; i < kWG / 64; ++i) m = max(m, most[i]);
-                const float scale = fmaxf(old, __uint_as_float(m) / 127.0f);
-                if (scale > old) {
-                    for (uint32_t i = tid; i < t0 * p.head_dim; i += kWG) {
-                        const uint32_t t = i / p.head_dim, d = i % p.head_dim;
-                        uint8_t *c = codes + (kv ? d * pt + t : t * p.width + d);
-                        *c = static_cast<uint8_t>(static_cast<int32_t>(rintf(static_cast<float>(static_cast<int32_t>(*c) - 128) * old / scale)) + 128);
-                    }
-                }
-                for (uint32_t i = tid; i < n; i += kWG) {
-                    const uint32_t t = t0 + i / p.head_dim, d = i % p.head_dim;
-                    codes[kv ? d * pt + t : t * p.width + d] = static_cast<uint8_t>(grid_code(load_as_f32(x + t * r.token_stride[kv] + d), scale));
-                }
-                if (tid == 0) *scale_at = scale;
-                __syncthreads();                 // `most` is used again
             }
+        }
+    }
+    return r;
+}
+
+template <typename T>
+__device__ inline void patch_values(const RawPatch<T> &r, const Patch &a, const Block &b, uint32_t head_dim, float (*v)[8]) {
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j)
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) {
+            const uint32_t w = sizeof(T) == 2 ? r.w[j][0][i / 2] : r.w[j][(i / 4) % (sizeof(T) / 2)][i & 3];
+            const float x = __uint_as_float(sizeof(T) == 4 ? w : i & 1 ? w & 0xffff0000u : w << 16);
+            v[j][i] = a.t + j >= b.t0 && a.t + j < b.t1 && a.d + i < head_dim ? x : 0.0f;
+        }
+}
+
+// The bits of the largest |x| of a patch: of all elements, or of the finite ones.
+__device__ inline uint32_t largest(const float (*v)[8], bool finite) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t bits = __float_as_uint(v[j][i]) & 0x7fffffffu;
+            m = max(m, !finite || bits < 0x7f800000u ? bits : 0u);
+        }
+    return m;
+}
+
+// A patch's codes: new tokens' from v, older ones moved to the new grid if the scale has grown, others left as they are.
+__device__ inline void write_patch(const Pool &p, uint64_t unit, const Patch &a, const Block &b, const float (*v)[8], float old, const Grid &grid, int kv) {
+    const bool moved = grid.scale > old && a.t < b.t0;
+    if ((a.t + 4 <= b.t0 && !moved) || a.t >= b.t1) return;
+    const uint32_t pt = 1u << p.page_shift, step = kv ? pt : p.width;
+    uint8_t *at = kv ? p.v + (unit * p.width + a.d) * pt + a.t : p.k + (unit * pt + a.t) * p.width + a.d;
+    if (a.t >= b.t0 && a.t + 4 <= b.t1 && a.d + 8 <= p.head_dim && !grid.divide) {
+        uint32_t c[4][8];
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j)
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) c[j][i] = code_by_inverse(v[j][i], grid);
+        if (kv) {
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) *reinterpret_cast<uint32_t *>(at + i * step) = four_codes(c[0][i], c[1][i], c[2][i], c[3][i]);
+        } else {
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j)
+                *reinterpret_cast<u32x2 *>(at + j * step) = u32x2{four_codes(c[j][0], c[j][1], c[j][2], c[j][3]), four_codes(c[j][4], c[j][5], c[j][6], c[j][7])};
+        }
+        return;
+    }
+    // code by code: nothing has to be read first but codes that move
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) {
+        if (a.t + j >= b.t1 || (a.t + j < b.t0 && !moved)) continue;
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) {
+            if (a.d + i >= p.head_dim) break;
+            uint8_t *code = kv ? at + i * step + j : at + j * step + i;
+            if (a.t + j >= b.t0)
+                *code = static_cast<uint8_t>(grid.divide ? code_by_division(v[j][i], grid.scale) : code_by_inverse(v[j][i], grid));
+            else
+                *code = static_cast<uint8_t>(static_cast<int32_t>(rintf(static_cast<float>(static_cast<int32_t>(*code) - 128) * old / grid.scale)) + 128);
         }
     }
 }
 
-// A lane per row, head and dimension.
-template <typename T>
-__global__ __launch_bounds__(kWG) void k_read(Pool p, Rows r, uint64_t n) {
-    for (uint64_t i = uint64_t{blockIdx.x} * kWG + threadIdx.x; i < n; i += uint64_t{gridDim.x} * kWG) {
-        const uint32_t d = static_cast<uint32_t>(i % p.head_dim), head = static_cast<uint32_t>(i / p.head_dim % p.kv_heads);
-        const int32_t row = static_cast<int32_t>(i / p.head_dim / p.kv_heads);
-        uint32_t lo = 0, hi = p.seqs;            // the last sequence that starts at or before the row
-        while (hi - lo > 1) {
-            const uint32_t mid = (lo + hi) / 2;
-            if (r.start[mid] <= row) lo = mid; else hi = mid;
-        }
-        const Span s = span_of(r.start, p.lengths, lo, r.tokens);
-        if (row < s.row || row >= s.row + s.count) continue;
-        const int32_t pos = s.pos + row - s.row, page = pos < 0 ? -1 : page_of(p, lo, pos >> p.page_shift);
-        const uint32_t pt = 1u << p.page_shift, t = static_cast<uint32_t>(pos) & (pt - 1);
-        float k = 0.0f, v = 0.0f;
-        if (page >= 0) {
-            const uint64_t unit = uint64_t{static_cast<uint32_t>(page)} * p.kv_heads + head, at = unit * pt * p.width;
-            k = static_cast<float>(static_cast<int32_t>(p.k[at + t * p.width + d]) - 128) * p.k_scale[unit];
-            v = static_cast<float>(static_cast<int32_t>(p.v[at + d * pt + t]) - 128) * p.v_scale[unit];
-        }
-        static_cast<T *>(r.x[0])[static_cast<uint32_t>(row) * r.token_stride[0] + head * r.head_stride[0] + d] = store_from_f32<T>(k);
-        static_cast<T *>(r.x[1])[static_cast<uint32_t>(row) * r.token_stride[1] + head * r.head_stride[1] + d] = store_from_f32<T>(v);
+// LANES lanes to a block and head: a wavefront where that has few patches, else the workgroup. Rows are read once where every lane
+// has one patch (up to 64 tokens of 128 dimensions), else twice.  Bound by the bytes of the rows and codes for prompts, by
+// the latency of four dependent loads (row numbers, page, rows and scale, codes) for single tokens.
+template <typename T, int LANES>
+__global__ __launch_bounds__(kWG) void k_append(Pool p, Rows r, uint32_t blocks, uint32_t work) {
+    __shared__ uint32_t most[2][kWG / 64];
+    constexpr uint32_t kUnits = kWG / LANES;
+    const uint32_t lane = threadIdx.x % LANES, patches = ((p.head_dim + 7) / 8) << (p.page_shift - 2);
+    for (uint32_t w = blockIdx.x * kUnits + threadIdx.x / LANES; w < work; w += gridDim.x * kUnits) {
+        each_block(p, r, blocks, w, [&](const Block &b, uint32_t head) {
+            const T *x[2];
+            float v[2][4][8];
+            uint32_t m[2] = {0, 0};
+#pragma unroll
+            for (int kv = 0; kv < 2; ++kv) x[kv] = static_cast<const T *>(r.x[kv]) + static_cast<uint64_t>(b.row) * r.token_stride[kv] + head * r.head_stride[kv];
+            const auto look = [&](bool finite) {
+                m[0] = m[1] = 0;
+                for (uint32_t i = lane; i < patches; i += LANES) {
+                    const Patch a[2] = {patch_of(p, i, 0), patch_of(p, i, 1)};
+                    const RawPatch<T> k = ask_patch(x[0], r.token_stride[0], a[0], b, p.head_dim, r.aligned);
+                    const RawPatch<T> u = ask_patch(x[1], r.token_stride[1], a[1], b, p.head_dim, r.aligned);
+                    patch_values<T>(k, a[0], b, p.head_dim, v[0]);
+                    patch_values<T>(u, a[1], b, p.head_dim, v[1]);
+                    m[0] = max(m[0], largest(v[0], finite));
+                    m[1] = max(m[1], largest(v[1], finite));
+                }
+                for (int o = 32; o; o >>= 1) {
+                    m[0] = max(m[0], static_cast<uint32_t>(__shfl_xor(static_cast<int>(m[0]), o)));
+                    m[1] = max(m[1], static_cast<uint32_t>(__shfl_xor(static_cast<int>(m[1]), o)));
+                }
+                if (LANES > 64) {
+                    __syncthreads();
+                    if ((threadIdx.x & 63u) == 0) most[0][threadIdx.x >> 6] = m[0], most[1][threadIdx.x >> 6] = m[1];
+                    __syncthreads();
+                    for (int i = 0; i < kWG / 64; ++i) m[0] = max(m[0], most[0][i]), m[1] = max(m[1], most[1][i]);
+                }
+            };
+            look(false);
+            const bool numbers = max(m[0], m[1]) < 0x7f800000u;
+            if (!numbers) look(true);
+            const int32_t page = checked_page(p, b.entry, b.at);
+            if (page < 0) return;
+            const uint64_t unit = uint64_t{static_cast<uint32_t>(page)} * p.kv_heads + head;
+            const float old[2] = {b.t0 ? p.k_scale[unit] : 0.0f, b.t0 ? p.v_scale[unit] : 0.0f};
+            const Grid grid[2] = {grid_of(fmaxf(old[0], __uint_as_float(m[0]) / 127.0f), numbers), grid_of(fmaxf(old[1], __uint_as_float(m[1]) / 127.0f), numbers)};
+            for (uint32_t i = lane; i < patches; i += LANES) {
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv) {
+                    const Patch a = patch_of(p, i, kv);
+                    if (patches > LANES)
+                        patch_values<T>(ask_patch(x[kv], r.token_stride[kv], a, b, p.head_dim, r.aligned), a, b, p.head_dim, v[kv]);
+                    write_patch(p, unit, a, b, v[kv], old[kv], grid[kv], kv);
+                }
+            }
+            if (lane == 0) p.k_scale[unit] = grid[0].scale, p.v_scale[unit] = grid[1].scale;
+        });
+    }
+}
+
+template <typename T, int LANES>
+__global__ __launch_bounds__(kWG) void k_read(Pool p, Rows r, uint32_t blocks, uint32_t work) {
+    constexpr uint32_t kUnits = kWG / LANES;
+    const uint32_t lane = threadIdx.x % LANES, patches = ((p.head_dim + 7) / 8) << (p.page_shift - 2), pt = 1u << p.page_shift;
+    for (uint32_t w = blockIdx.x * kUnits + threadIdx.x / LANES; w < work; w += gridDim.x * kUnits) {
+        each_block(p, r, blocks, w, [&](const Block &b, uint32_t head) {
+            const int32_t page = checked_page(p, b.entry, b.at);
+            const uint64_t unit = uint64_t{static_cast<uint32_t>(max(page, 0))} * p.kv_heads + head;
+            const float scale[2] = {p.k_scale[unit], p.v_scale[unit]};
+            for (uint32_t i = lane; i < patches; i += LANES) {
+                const Patch a[2] = {patch_of(p, i, 0), patch_of(p, i, 1)};
+                uint32_t words[2][8];
+#pragma unroll
+                for (uint32_t j = 0; j < 4; ++j) {
+                    const u32x2 x = *reinterpret_cast<const u32x2 *>(p.k + (unit * pt + a[0].t + j) * p.width + a[0].d);
+                    words[0][2 * j] = x[0];
+                    words[0][2 * j + 1] = x[1];
+                }
+#pragma unroll
+                for (uint32_t d = 0; d < 8; ++d) words[1][d] = *reinterpret_cast<const uint32_t *>(p.v + (unit * p.width + a[1].d + d) * pt + a[1].t);
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv) {
+                    T *out = static_cast<T *>(r.x[kv]) + static_cast<uint64_t>(b.row) * r.token_stride[kv] + head * r.head_stride[kv];
+#pragma unroll
+                    for (uint32_t j = 0; j < 4; ++j) {
+                        const uint32_t t = a[kv].t + j;
+                        if (t < b.t0 || t >= b.t1) continue;
+                        T y[8];
+#pragma unroll
+                        for (uint32_t d = 0; d < 8; ++d) {
+                            const uint32_t code = kv ? byte_of(words[1][d], j) : byte_of(words[0][2 * j + d / 4], d & 3);
+                            y[d] = store_from_f32<T>(page < 0 ? 0.0f : static_cast<float>(static_cast<int32_t>(code) - 128) * scale[kv]);
+                        }
+                        T *row = out + t * r.token_stride[kv] + a[kv].d;
+                        if (r.aligned && a[kv].d + 8 <= p.head_dim) {
+#pragma unroll
+                            for (uint32_t d = 0; d < 8; d += 16 / sizeof(T)) *reinterpret_cast<u32x4 *>(row + d) = *reinterpret_cast<const u32x4 *>(y + d);
+                        } else {
+#pragma unroll
+                            for (uint32_t d = 0; d < 8; ++d)
+                                if (a[kv].d + d < p.head_dim) row[d] = y[d];
+                        }
+                    }
+                }
+            }
+        });
     }
 }
 
@@ -291,8 +484,6 @@ __global__ __launch_bounds__(kWG) void k_regroup_fill(Regroup g, PageWork w, con
     for (int32_t i = keep + static_cast<int32_t>(threadIdx.x); i < want; i += kWG) row[i] = fresh[copy + static_cast<uint32_t>(i - keep)];
 }
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
 struct Copies {
     uint8_t *codes[2];
     float *scale[2];
@@ -377,7 +568,35 @@ entro_status check_rows(const entro_cache *c, const entro_cache_rows *r) {
 }
 
 Rows rows_of(const entro_cache_rows *r) {
-    return {{r->k, r->v}, {r->k_token_stride, r->v_token_stride}, {r->k_head_stride, r->v_head_stride}, r->start, r->tokens};
+    const bool aligned = ((r->k_token_stride | r->v_token_stride | r->k_head_stride | r->v_head_stride) & 7u) == 0;
+    return {{r->k, r->v}, {r->k_token_stride, r->v_token_stride}, {r->k_head_stride, r->v_head_stride}, r->start, r->tokens, aligned};
+}
+
+template <typename T, int LANES>
+void launch_lanes(const Pool &p, const Rows &r, uint32_t blocks, uint32_t work, hipStream_t st, bool write) {
+    const uint32_t groups = (work + kWG / LANES - 1) / (kWG / LANES), grid = groups < 65536 ? groups : 65536;
+    if (write)
+        hipLaunchKernelGGL((k_append<T, LANES>), dim3(grid), dim3(kWG), 0, st, p, r, blocks, work);
+    else
+        hipLaunchKernelGGL((k_read<T, LANES>), dim3(grid), dim3(kWG), 0, st, p, r, blocks, work);
+}
+
+// entro_cache_append and entro_cache_read; false if there are too many blocks.
+bool launch_rows(const entro_cache *c, const entro_cache_table *t, const entro_cache_rows *rows, hipStream_t st, bool write) {
+    const Pool p = pool_of(c, t, rows->layer);
+    const Rows r = rows_of(rows);
+    // as many blocks as the most rows can touch, and no more than there are slots
+    const uint64_t touch = (uint64_t{rows->max_new} + c->page_tokens + (rows->max_new ? 0 : 1) - 2) / c->page_tokens + 1;
+    const uint32_t blocks = static_cast<uint32_t>(touch < t->stride ? touch : t->stride);
+    const uint64_t work = uint64_t{blocks} * c->kv_heads * t->seqs;
+    if (work > 0x7fffffffull) return false;
+    const bool few = ((c->head_dim + 7) / 8) * (c->page_tokens / 4) <= 64;
+    const uint32_t n = static_cast<uint32_t>(work);
+    if (rows->type == ENTRO_F32)
+        few ? launch_lanes<float, 64>(p, r, blocks, n, st, write) : launch_lanes<float, kWG>(p, r, blocks, n, st, write);
+    else
+        few ? launch_lanes<uint16_t, 64>(p, r, blocks, n, st, write) : launch_lanes<uint16_t, kWG>(p, r, blocks, n, st, write);
+    return true;
 }
 
 Copies copies_of(const entro_cache *c) {
@@ -437,19 +656,8 @@ entro_status entro_cache_append(const entro_cache *c, const entro_cache_table *t
     if (const entro_status s = check_cache(c)) return s;
     if (const entro_status s = check_table(t)) return s;
     if (const entro_status s = check_rows(c, r)) return s;
-    if (r->tokens == 0 || r->max_new == 0) return ENTRO_OK;
-    const Pool p = pool_of(c, t, r->layer);
-    // as many blocks as the most rows can touch, and no more than there are slots
-    const uint64_t touch = (uint64_t{r->max_new} + c->page_tokens - 2) / c->page_tokens + 1;
-    const uint32_t blocks = static_cast<uint32_t>(touch < t->stride ? touch : t->stride);
-    const uint64_t work = uint64_t{blocks} * c->kv_heads * t->seqs;
-    if (work > 0xffffffffull) return ENTRO_ERR_SIZE;
-    const unsigned grid = static_cast<unsigned>(work < 65536 ? work : 65536);
-    hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (r->type == ENTRO_F32)
-        hipLaunchKernelGGL(k_append<float>, dim3(grid), dim3(kWG), 0, st, p, rows_of(r), blocks, static_cast<uint32_t>(work));
-    else
-        hipLaunchKernelGGL(k_append<uint16_t>, dim3(grid), dim3(kWG), 0, st, p, rows_of(r), blocks, static_cast<uint32_t>(work));
+    if (r->tokens == 0) return ENTRO_OK;
+    if (!launch_rows(c, t, r, static_cast<hipStream_t>(hip_stream), true)) return ENTRO_ERR_SIZE;
     return hip_ok(hipGetLastError(), "entro_cache_append") ? ENTRO_OK : ENTRO_ERR_DEVICE;
 }
 
@@ -458,14 +666,7 @@ entro_status entro_cache_read(const entro_cache *c, const entro_cache_table *t, 
     if (const entro_status s = check_table(t)) return s;
     if (const entro_status s = check_rows(c, r)) return s;
     if (r->tokens == 0) return ENTRO_OK;
-    const Pool p = pool_of(c, t, r->layer);
-    const uint64_t n = uint64_t{r->tokens} * c->kv_heads * c->head_dim, wgs = (n + kWG - 1) / kWG;
-    const unsigned grid = static_cast<unsigned>(wgs < 16384 ? wgs : 16384);
-    hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (r->type == ENTRO_F32)
-        hipLaunchKernelGGL(k_read<float>, dim3(grid), dim3(kWG), 0, st, p, rows_of(r), n);
-    else
-        hipLaunchKernelGGL(k_read<uint16_t>, dim3(grid), dim3(kWG), 0, st, p, rows_of(r), n);
+    if (!launch_rows(c, t, r, static_cast<hipStream_t>(hip_stream), false)) return ENTRO_ERR_SIZE;
     return hip_ok(hipGetLastError(), "entro_cache_read") ? ENTRO_OK : ENTRO_ERR_DEVICE;
 }
 
