@@ -484,6 +484,146 @@ __global__ __launch_bounds__(kWG) void k_regroup_fill(Regroup g, PageWork w, con
     for (int32_t i = keep + static_cast<int32_t>(threadIdx.x); i < want; i += kWG) row[i] = fresh[copy + static_cast<uint32_t>(i - keep)];
 }
 
+// ------------------------------------------------------------------------------------- small tables: one workgroup for all of it
+//
+// Four launches in a row cost more than their work where the table is small: one workgroup then goes through the same steps with
+// its marks in LDS (a step of 64 rows and 660 pages: see k_regroup_plan for the steps).
+constexpr uint32_t kSmallPages = 16384, kSmallSlots = 65536;
+
+__global__ __launch_bounds__(kScanWG) void k_regroup_one(Regroup g, PageWork w, int32_t *status) {
+    __shared__ int32_t owner[kSmallPages];
+    __shared__ uint16_t fresh[kSmallPages];
+    const uint32_t pt = 1u << g.page_shift, slots = g.to.seqs * g.to.stride;
+    // what row b keeps in slot s
+    const auto kept_page = [&](const Row &r, uint32_t s) {
+        if (static_cast<int32_t>(s) >= slots_of(r.kept, g.page_shift) || s >= g.from.stride) return -1;
+        const int32_t id = g.from.slots[uint64_t{static_cast<uint32_t>(r.parent)} * g.from.stride + s];
+        const uint64_t at = uint64_t{s} << g.page_shift;
+        const bool left = g.window && at + pt + g.window <= static_cast<uint64_t>(r.kept) + 1 && at >= g.sinks;
+        return static_cast<uint32_t>(id) < g.pages && !left ? id : -1;
+    };
+    for (uint32_t p = threadIdx.x; p < g.pages; p += kScanWG) owner[p] = kNoOwner;
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < slots; i += kScanWG) {
+        const uint32_t b = i / g.to.stride, s = i % g.to.stride;
+        const Row r = regroup_row(g, b);
+        if (s == 0) g.to.lengths[b] = r.length;
+        const int32_t id = kept_page(r, s);
+        const bool open = open_at(r.kept, s, g.page_shift);
+        if (id >= 0) atomicMin(&owner[id], open ? static_cast<int32_t>(b) : kFullSomewhere);
+        // open slots and those of new pages are written below
+        if (!open && (static_cast<int32_t>(s) < slots_of(r.kept, g.page_shift) || static_cast<int32_t>(s) >= slots_of(r.length, g.page_shift)))
+            g.to.slots[i] = id;
+    }
+    __syncthreads();
+    uint32_t free_all = 0, total;
+    for (uint32_t p0 = 0; p0 < g.pages; p0 += kScanWG) {
+        const uint32_t p = p0 + threadIdx.x, is_free = p < g.pages && owner[p] == kNoOwner;
+        const uint32_t at = free_all + scan_before(is_free, &total);
+        free_all += total;
+        if (is_free) fresh[at] = static_cast<uint16_t>(p);
+    }
+    uint32_t need_all = 0, copies_all = 0;
+    bool too_long = false;
+    for (uint32_t b0 = 0; b0 < g.to.seqs; b0 += kScanWG) {
+        const uint32_t b = b0 + threadIdx.x;
+        uint32_t copy = 0, need = 0;
+        int32_t open_page = -1;
+        if (b < g.to.seqs) {
+            const Row r = regroup_row(g, b);
+            const int32_t want = slots_of(r.length, g.page_shift);
+            too_long |= want > static_cast<int32_t>(g.to.stride);
+            const uint32_t s = static_cast<uint32_t>(r.kept) >> g.page_shift;
+            if (s < g.to.stride && open_at(r.kept, s, g.page_shift)) open_page = kept_page(r, s);
+            copy = open_page >= 0 && owner[open_page] != static_cast<int32_t>(b);
+            need = copy + static_cast<uint32_t>(want - slots_of(r.kept, g.page_shift));
+        }
+        const uint32_t at = need_all + scan_before(need, &total);
+        need_all = min(need_all + total, 0x7fffffffu);
+        const uint32_t nth = copies_all + scan_before(copy, &total);
+        copies_all += total;
+        if (b < g.to.seqs) w.first[b] = static_cast<int32_t>(min(at, 0x3fffffffu) * 2 + copy);
+        if (copy) {
+            w.src[nth] = open_page;
+            w.dst[nth] = at < free_all ? static_cast<int32_t>(fresh[at]) : 0;
+        }
+    }
+    const bool fits = !__syncthreads_or(too_long) && need_all <= free_all;
+    __threadfence_block();
+    for (uint32_t i = threadIdx.x; i < slots; i += kScanWG) {
+        const uint32_t b = i / g.to.stride, s = i % g.to.stride;
+        const Row r = regroup_row(g, b);
+        const bool open = open_at(r.kept, s, g.page_shift);
+        const int32_t keep = slots_of(r.kept, g.page_shift);
+        if (!open && (static_cast<int32_t>(s) < keep || static_cast<int32_t>(s) >= slots_of(r.length, g.page_shift))) continue;
+        int32_t id = open ? kept_page(r, s) : -1;
+        if (fits) {
+            const uint32_t first = static_cast<uint32_t>(w.first[b]);
+            if (!open)
+                id = fresh[first / 2 + (first & 1u) + (s - static_cast<uint32_t>(keep))];
+            else if (first & 1u)
+                id = fresh[first / 2];
+        }
+        g.to.slots[i] = id;
+    }
+    if (threadIdx.x == 0) {
+        w.counts[0] = fits ? static_cast<int32_t>(copies_all) : 0;
+        status[0] = fits ? 0 : 1;
+        status[1] = static_cast<int32_t>(g.pages - free_all + (fits ? need_all : 0u));
+        status[2] = static_cast<int32_t>(free_all - (fits ? need_all : 0u));
+        status[3] = fits ? static_cast<int32_t>(copies_all) : 0;
+    }
+}
+
+__global__ __launch_bounds__(kScanWG) void k_compact_one(entro_cache_table t, entro_cache_table next, uint32_t pages, PageWork w, int32_t *status) {
+    __shared__ int32_t number[kSmallPages];           // of a page after the move
+    __shared__ uint16_t holes[kSmallPages], late[kSmallPages];
+    const uint32_t slots = t.seqs * t.stride;
+    for (uint32_t p = threadIdx.x; p < pages; p += kScanWG) number[p] = -1;
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < slots; i += kScanWG) {
+        const int32_t id = t.slots[i];
+        if (static_cast<uint32_t>(id) < pages) number[id] = id;
+    }
+    for (uint32_t b = threadIdx.x; b < t.seqs; b += kScanWG) next.lengths[b] = t.lengths[b];
+    __syncthreads();
+    uint32_t used = 0, total;
+    for (uint32_t p0 = 0; p0 < pages; p0 += kScanWG) {
+        const uint32_t p = p0 + threadIdx.x;
+        scan_before(p < pages && number[p] >= 0, &total);
+        used += total;
+    }
+    uint32_t free_below = 0, moves = 0;
+    for (uint32_t p0 = 0; p0 < pages; p0 += kScanWG) {
+        const uint32_t p = p0 + threadIdx.x;
+        const bool held = p < pages && number[p] >= 0, hole = p < used && !held, move = p >= used && held;
+        const uint32_t h = free_below + scan_before(hole, &total);
+        free_below += total;
+        const uint32_t m = moves + scan_before(move, &total);
+        moves += total;
+        if (hole) holes[h] = static_cast<uint16_t>(p);
+        if (move) late[m] = static_cast<uint16_t>(p);
+    }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < moves; i += kScanWG) {
+        w.src[i] = late[i];
+        w.dst[i] = holes[i];
+        number[late[i]] = holes[i];
+    }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < slots; i += kScanWG) {
+        const int32_t id = t.slots[i];
+        next.slots[i] = static_cast<uint32_t>(id) < pages ? number[id] : -1;
+    }
+    if (threadIdx.x == 0) {
+        w.counts[0] = static_cast<int32_t>(moves);
+        status[0] = 0;
+        status[1] = static_cast<int32_t>(used);
+        status[2] = static_cast<int32_t>(pages - used);
+        status[3] = static_cast<int32_t>(moves);
+    }
+}
+
 struct Copies {
     uint8_t *codes[2];
     float *scale[2];
@@ -631,6 +771,10 @@ dim3 rows_grid(uint32_t stride, uint32_t seqs) {
     return dim3(x < 64 ? x : 64, seqs);
 }
 
+unsigned fill_grid(uint32_t pages) { return pages < 1024 * kWG ? (pages + kWG - 1) / kWG : 1024; }
+
+bool small(const entro_cache *c, const entro_cache_table *t) { return c->pages <= kSmallPages && uint64_t{t->seqs} * t->stride <= kSmallSlots; }
+
 unsigned copy_grid(uint64_t most, uint32_t layers) {
     const uint64_t items = most * layers * 2;
     return static_cast<unsigned>(items < 4096 ? items : 4096);
@@ -684,11 +828,14 @@ entro_status entro_cache_regroup(const entro_cache *c, const entro_cache_table *
     pages_workspace(c, next, &w, workspace);
     const Regroup g = {*t, *next, parent, grow, c->pages, static_cast<uint32_t>(__builtin_ctz(c->page_tokens)), window, sinks};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    const unsigned fill = c->pages < 1024 * kWG ? (c->pages + kWG - 1) / kWG : 1024;
-    hipLaunchKernelGGL(k_page_fill, dim3(fill), dim3(kWG), 0, st, w.owner, c->pages, kNoOwner);
-    hipLaunchKernelGGL(k_regroup_rows, rows_grid(next->stride, next->seqs), dim3(kWG), 0, st, g, w.owner);
-    hipLaunchKernelGGL(k_regroup_plan, dim3(1), dim3(kScanWG), 0, st, g, w, status);
-    hipLaunchKernelGGL(k_regroup_fill, dim3(next->seqs), dim3(kWG), 0, st, g, w, static_cast<const int32_t *>(status));
+    if (small(c, next)) {
+        hipLaunchKernelGGL(k_regroup_one, dim3(1), dim3(kScanWG), 0, st, g, w, status);
+    } else {
+        hipLaunchKernelGGL(k_page_fill, dim3(fill_grid(c->pages)), dim3(kWG), 0, st, w.owner, c->pages, kNoOwner);
+        hipLaunchKernelGGL(k_regroup_rows, rows_grid(next->stride, next->seqs), dim3(kWG), 0, st, g, w.owner);
+        hipLaunchKernelGGL(k_regroup_plan, dim3(1), dim3(kScanWG), 0, st, g, w, status);
+        hipLaunchKernelGGL(k_regroup_fill, dim3(next->seqs), dim3(kWG), 0, st, g, w, static_cast<const int32_t *>(status));
+    }
     hipLaunchKernelGGL(k_copy_pages, dim3(copy_grid(next->seqs, c->layers)), dim3(kWG), 0, st, copies_of(c), static_cast<const int32_t *>(w.src),
                        static_cast<const int32_t *>(w.dst), static_cast<const int32_t *>(w.counts));
     return hip_ok(hipGetLastError(), "entro_cache_regroup") ? ENTRO_OK : ENTRO_ERR_DEVICE;
@@ -701,11 +848,14 @@ entro_status entro_cache_compact(const entro_cache *c, const entro_cache_table *
     PageWork w;
     pages_workspace(c, next, &w, workspace);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    const unsigned fill = c->pages < 1024 * kWG ? (c->pages + kWG - 1) / kWG : 1024;
-    hipLaunchKernelGGL(k_page_fill, dim3(fill), dim3(kWG), 0, st, w.owner, c->pages, kNoOwner);
-    hipLaunchKernelGGL(k_compact_mark, rows_grid(t->stride, t->seqs), dim3(kWG), 0, st, *t, c->pages, w.owner);
-    hipLaunchKernelGGL(k_compact_plan, dim3(1), dim3(kScanWG), 0, st, c->pages, w, status);
-    hipLaunchKernelGGL(k_compact_rows, rows_grid(t->stride, t->seqs), dim3(kWG), 0, st, *t, *next, c->pages, static_cast<const int32_t *>(w.owner));
+    if (small(c, next)) {
+        hipLaunchKernelGGL(k_compact_one, dim3(1), dim3(kScanWG), 0, st, *t, *next, c->pages, w, status);
+    } else {
+        hipLaunchKernelGGL(k_page_fill, dim3(fill_grid(c->pages)), dim3(kWG), 0, st, w.owner, c->pages, kNoOwner);
+        hipLaunchKernelGGL(k_compact_mark, rows_grid(t->stride, t->seqs), dim3(kWG), 0, st, *t, c->pages, w.owner);
+        hipLaunchKernelGGL(k_compact_plan, dim3(1), dim3(kScanWG), 0, st, c->pages, w, status);
+        hipLaunchKernelGGL(k_compact_rows, rows_grid(t->stride, t->seqs), dim3(kWG), 0, st, *t, *next, c->pages, static_cast<const int32_t *>(w.owner));
+    }
     hipLaunchKernelGGL(k_copy_pages, dim3(copy_grid(c->pages / 2 + 1, c->layers)), dim3(kWG), 0, st, copies_of(c),
                        static_cast<const int32_t *>(w.src), static_cast<const int32_t *>(w.dst), static_cast<const int32_t *>(w.counts));
     return hip_ok(hipGetLastError(), "entro_cache_compact") ? ENTRO_OK : ENTRO_ERR_DEVICE;

@@ -455,6 +455,26 @@ def test_compact_against_the_definition(case):
     check_pages(pool, *result, want, pool.pages)
 
 
+def test_large_tables():
+    """Tables and pools past what one workgroup takes: the same results."""
+    rng = np.random.default_rng(18)
+    page, seqs, stride = 16, 130, 600
+    lengths = rng.integers(0, 9000, seqs)
+    pool, table = make(rng, seqs, lengths, 1, 1, page, spare=3000, slots=stride)
+    pool.k_scale[:], pool.v_scale[:] = 1, 1
+    table[7], lengths[7] = table[3], lengths[3]                           # shared pages
+    parent, grow = rng.integers(-3, seqs, seqs), rng.integers(-300, 60, seqs)
+    want = ref.regroup(pool.pages, page, table, lengths, seqs, stride, parent, grow, 5000, 20)
+    assert want is not None and len(want[2]) > 20 and seqs * stride > 65536
+    twin = pool.copy()
+    result = run_pages(pool, table, lengths, seqs, stride, lambda c, t, n, status, ws: E.entro_cache_regroup(
+        c, t, n, status, ws, parent=ints(parent), grow=ints(grow), window=5000, sinks=20))
+    check_pages(pool, *result, want, pool.pages)
+    want = ref.compact(twin.pages, table, lengths.astype(np.int32))
+    result = run_pages(twin, table, lengths, *table.shape, lambda c, t, n, status, ws: E.entro_cache_compact(c, t, n, status, ws))
+    check_pages(twin, *result, want, twin.pages)
+
+
 def test_refusals_of_pages_that_do_not_suffice():
     rng = np.random.default_rng(14)
     pool, table = make(rng, 2, [20, 20], 1, 64, 16, spare=1)
