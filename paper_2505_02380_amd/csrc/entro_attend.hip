@@ -403,8 +403,9 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void k_attend_many(
     constexpr int kParts = sizeof(T) == 2 ? 1 : 2, kWeights = sizeof(T) == 2 ? 2 : 3;
     constexpr int kChunks = (W * 4 + kThreads - 1) / kThreads;      // pieces of 16 codes a thread turns, of keys and of values
     constexpr int kKeyRow = 2 * W + 16, kValueRow = 2 * kTile + 16;   // bytes
-    constexpr int kValues = kTile * kKeyRow, kHalf = kValues + W * kValueRow;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kHalf];
+    constexpr int kKeyTile = kTile * kKeyRow, kValueTile = W * kValueRow;
+    constexpr int kValueTiles = WAVES == 8 ? 3 : 2;
+    __shared__ __attribute__((aligned(16))) uint8_t key_lds[2][kKeyTile], value_lds[kValueTiles][kValueTile];
     __shared__ f32x4 tile_ks[2], tile_vs[2];
     __shared__ int32_t tile_ok[2][4];
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6, h = lane >> 5, c = lane & 31u;
@@ -494,15 +495,15 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void k_attend_many(
             vs = p.v_scale[at];
             s_ok = id >= 0;
         };
-        const auto to_lds = [&](int half) {
+        const auto to_lds = [&](int half, int place) {
 #pragma unroll
             for (int n = 0; n < kChunks; ++n) {
                 const int32_t ch = n * kThreads + static_cast<int32_t>(tid);
                 if (kThreads * kChunks != W * 4 && ch >= W * 4) continue;
-                half8 *k = reinterpret_cast<half8 *>(lds + half * kHalf + (ch / (W / 16)) * kKeyRow + 32 * (ch % (W / 16)));
+                half8 *k = reinterpret_cast<half8 *>(key_lds[half] + (ch / (W / 16)) * kKeyRow + 32 * (ch % (W / 16)));
                 k[0] = eight_codes(kc[n][0], kc[n][1]);
                 k[1] = eight_codes(kc[n][2], kc[n][3]);
-                bf16x8 *v = reinterpret_cast<bf16x8 *>(lds + half * kHalf + kValues + (ch >> 2) * kValueRow + 32 * (ch & 3));
+                bf16x8 *v = reinterpret_cast<bf16x8 *>(value_lds[place] + (ch >> 2) * kValueRow + 32 * (ch & 3));
                 v[0] = eight_values(vc[n][0], vc[n][2]);
                 v[1] = eight_values(vc[n][1], vc[n][3]);
             }
@@ -518,17 +519,33 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void k_attend_many(
             ask_pages(begin);
             ask_codes(begin);
             ask_pages(begin + 1);
-            to_lds(0);
+            to_lds(0, 0);
             ask_codes(begin + 1);
             ask_pages(begin + 2);
         }
         __syncthreads();
 
+        // the second product: weights of four times 16 tokens
+        const auto add_values = [&](const bf16x8 (*w)[kWeights], int place) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+#pragma unroll
+                for (int d = 0; d < kDims; ++d) {
+                    const bf16x8 v = *reinterpret_cast<const bf16x8 *>(value_lds[place] + (32 * d + c) * kValueRow + 32 * g + 16 * h);
+#pragma unroll
+                    for (int n = 0; n < kWeights; ++n) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[g][n], o[d], 0, 0, 0);
+                }
+        };
+        const bool late = WAVES == 8 && wave >= 4;
+        bool owed = false;
+        bf16x8 w[4][kWeights];
+        int place = 0, place_before = 0;            // of the tile's values, and of the last tile's
         for (int32_t i = begin; i < end; ++i) {
-            const int half = (i - begin) & 1;
+            const int half = (i - begin) & 1, place_next = place + 1 < kValueTiles ? place + 1 : 0;
             const int32_t t0 = tiles.at(i) * kTile;
-            const uint8_t *at = lds + half * kHalf;
             const bool work = t0 <= wave_last;      // a wavefront whose rows see nothing here only turns codes
+            if (owed) add_values(w, place_before);
+            owed = false;
             f32x16 z[2];
             if (work) {
 #pragma unroll
@@ -536,33 +553,40 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void k_attend_many(
                     z[t] = f32x16{};
 #pragma unroll
                     for (int f = 0; f < W / 16; ++f) {
-                        const half8 k = *reinterpret_cast<const half8 *>(at + (32 * t + c) * kKeyRow + 32 * f + 16 * h);
+                        const half8 k = *reinterpret_cast<const half8 *>(key_lds[half] + (32 * t + c) * kKeyRow + 32 * f + 16 * h);
 #pragma unroll
                         for (int n = 0; n < kParts; ++n) z[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[n][f], z[t], 0, 0, 0);
                     }
                 }
             }
-            if (i + 1 < end) to_lds(half ^ 1);
+            if (i + 1 < end) to_lds(half ^ 1, place_next);
             ask_codes(i + 2);
             ask_pages(i + 3);
             if (work) {
-                const f32x4 kf = tile_ks[half] * q_factor, vf = tile_vs[half];
+                f32x4 kf = tile_ks[half] * q_factor;
+                const f32x4 vf = tile_vs[half];
                 const bool all = t0 + kTile - 1 <= wave_first && (!a.window || static_cast<uint32_t>(wave_last - t0) < a.window) &&
                                  (tile_ok[half][0] & tile_ok[half][1] & tile_ok[half][2] & tile_ok[half][3]);
-                float top = -INFINITY;
+                if (!all) {
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                    for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        z[t][j] *= kf[2 * t + j / 8];
-                        if (!all) {
+                        for (int j = 0; j < 16; ++j) {
                             const int32_t key = t0 + 32 * t + 8 * (j / 4) + 4 * static_cast<int32_t>(h) + (j & 3);
-                            const bool seen = tile_ok[half][2 * t + j / 8] && key <= my_pos &&
-                                              (!a.window || static_cast<uint32_t>(my_pos - key) < a.window || static_cast<uint32_t>(key) < a.sinks);
+                            const bool seen = (tile_ok[half][2 * t + j / 8] != 0) & (key <= my_pos) &
+                                              ((a.window == 0) | (static_cast<uint32_t>(my_pos - key) < a.window) | (static_cast<uint32_t>(key) < a.sinks));
                             z[t][j] = seen ? z[t][j] : -INFINITY;
                         }
-                        top = fmaxf(top, z[t][j]);
-                    }
+                }
+                float top = -INFINITY;
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    kf[g] = fmaxf(kf[g], 1e-37f);   // minus infinity stays that
+                    float most = z[g / 2][8 * (g & 1)];
+#pragma unroll
+                    for (int j = 1; j < 8; ++j) most = fmaxf(most, z[g / 2][8 * (g & 1) + j]);
+                    top = fmaxf(top, most * kf[g]);
+                }
                 top = fmaxf(top, __shfl_xor(top, 32));
                 // sums may stand at 2^8 times their unit before they are brought to a new one
                 if (__any(top > m + 8.0f)) {
@@ -574,28 +598,24 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void k_attend_many(
                 }
                 const float base = m == -INFINITY ? 0.0f : m;
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                for (int g = 0; g < 4; ++g) {       // 16 tokens
+                    float x[8];
 #pragma unroll
-                    for (int g = 0; g < 2; ++g) {     // 16 tokens
-                        float x[8];
-                        bf16x8 w[kWeights];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const float e = __builtin_amdgcn_exp2f(z[t][8 * g + j] - base);
-                            l += e;
-                            x[j] = e * vf[2 * t + g];
-                        }
-                        split_weights<kWeights>(x, w);
-#pragma unroll
-                        for (int d = 0; d < kDims; ++d) {
-                            const bf16x8 v = *reinterpret_cast<const bf16x8 *>(at + kValues + (32 * d + c) * kValueRow + 32 * (2 * t + g) + 16 * h);
-#pragma unroll
-                            for (int n = 0; n < kWeights; ++n) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[n], o[d], 0, 0, 0);
-                        }
+                    for (int j = 0; j < 8; ++j) {
+                        const float e = __builtin_amdgcn_exp2f(fmaf(z[g / 2][8 * (g & 1) + j], kf[g], -base));
+                        l += e;
+                        x[j] = e * vf[g];
                     }
+                    split_weights<kWeights>(x, w[g]);
+                }
+                if (!late) add_values(w, place);
+                owed = late;
             }
+            place_before = place;
+            place = place_next;
             __syncthreads();
         }
+        if (owed) add_values(w, place_before);
         l += __shfl_xor(l, 32);
         if (mine) {
             const float inv = l > 0.0f ? 1.0f / l : 0.0f, base = m == -INFINITY ? 0.0f : m;
