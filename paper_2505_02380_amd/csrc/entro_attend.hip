@@ -398,14 +398,13 @@ __global__ __launch_bounds__(kWG, W > 128 ? 1 : 2) void k_attend_few(Pool p, Que
 // of each 32, h being the lane's half. The values' tokens lie in LDS in the order 0-3, 8-11, 4-7, 12-15 of each 16, so that what a
 // lane reads of them for the second product are the tokens whose weights it has.
 template <int W, typename T, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void k_attend_many(Pool p, Query a, uint32_t row_tiles) {
+__global__ __launch_bounds__(WAVES * 64, WAVES == 4 && sizeof(T) == 2 && W <= 128 ? 2 : 1) void k_attend_many(Pool p, Query a, uint32_t row_tiles) {
     constexpr int kThreads = WAVES * 64, kRows = WAVES * 32;
     constexpr int kParts = sizeof(T) == 2 ? 1 : 2, kWeights = sizeof(T) == 2 ? 2 : 3;
     constexpr int kChunks = (W * 4 + kThreads - 1) / kThreads;      // pieces of 16 codes a thread turns, of keys and of values
     constexpr int kKeyRow = 2 * W + 16, kValueRow = 2 * kTile + 16;   // bytes
     constexpr int kKeyTile = kTile * kKeyRow, kValueTile = W * kValueRow;
-    constexpr int kValueTiles = WAVES == 8 ? 3 : 2;
-    __shared__ __attribute__((aligned(16))) uint8_t key_lds[2][kKeyTile], value_lds[kValueTiles][kValueTile];
+    __shared__ __attribute__((aligned(16))) uint8_t key_lds[2][kKeyTile], value_lds[2][kValueTile];
     __shared__ f32x4 tile_ks[2], tile_vs[2];
     __shared__ int32_t tile_ok[2][4];
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6, h = lane >> 5, c = lane & 31u;
@@ -495,7 +494,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void k_attend_many(
             vs = p.v_scale[at];
             s_ok = id >= 0;
         };
-        const auto to_lds = [&](int half, int place) {
+        const auto to_lds = [&](int half) {
 #pragma unroll
             for (int n = 0; n < kChunks; ++n) {
                 const int32_t ch = n * kThreads + static_cast<int32_t>(tid);
@@ -503,7 +502,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void k_attend_many(
                 half8 *k = reinterpret_cast<half8 *>(key_lds[half] + (ch / (W / 16)) * kKeyRow + 32 * (ch % (W / 16)));
                 k[0] = eight_codes(kc[n][0], kc[n][1]);
                 k[1] = eight_codes(kc[n][2], kc[n][3]);
-                bf16x8 *v = reinterpret_cast<bf16x8 *>(value_lds[place] + (ch >> 2) * kValueRow + 32 * (ch & 3));
+                bf16x8 *v = reinterpret_cast<bf16x8 *>(value_lds[half] + (ch >> 2) * kValueRow + 32 * (ch & 3));
                 v[0] = eight_values(vc[n][0], vc[n][2]);
                 v[1] = eight_values(vc[n][1], vc[n][3]);
             }
@@ -519,47 +518,53 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void k_attend_many(
             ask_pages(begin);
             ask_codes(begin);
             ask_pages(begin + 1);
-            to_lds(0, 0);
+            to_lds(0);
             ask_codes(begin + 1);
             ask_pages(begin + 2);
         }
         __syncthreads();
 
+        // What the matrix units take from LDS is asked for kAhead pieces before it is used.
+        constexpr int kAhead = 4;
         // the second product: weights of four times 16 tokens
-        const auto add_values = [&](const bf16x8 (*w)[kWeights], int place) {
+        const auto add_values = [&](const bf16x8 (*w)[kWeights], int half) {
+            const uint8_t *at = value_lds[half] + c * kValueRow + 16 * h;
+            const auto piece = [&](int i) { return *reinterpret_cast<const bf16x8 *>(at + 32 * (i % kDims) * kValueRow + 32 * (i / kDims)); };
+            bf16x8 v[kAhead];
 #pragma unroll
-            for (int g = 0; g < 4; ++g)
+            for (int i = 0; i < kAhead; ++i) v[i] = piece(i);
 #pragma unroll
-                for (int d = 0; d < kDims; ++d) {
-                    const bf16x8 v = *reinterpret_cast<const bf16x8 *>(value_lds[place] + (32 * d + c) * kValueRow + 32 * g + 16 * h);
+            for (int i = 0; i < 4 * kDims; ++i) {
+                const bf16x8 now = v[i % kAhead];
+                if (i + kAhead < 4 * kDims) v[i % kAhead] = piece(i + kAhead);
 #pragma unroll
-                    for (int n = 0; n < kWeights; ++n) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[g][n], o[d], 0, 0, 0);
-                }
+                for (int n = 0; n < kWeights; ++n) o[i % kDims] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(now, w[i / kDims][n], o[i % kDims], 0, 0, 0);
+                
+            }
         };
-        const bool late = WAVES == 8 && wave >= 4;
-        bool owed = false;
-        bf16x8 w[4][kWeights];
-        int place = 0, place_before = 0;            // of the tile's values, and of the last tile's
         for (int32_t i = begin; i < end; ++i) {
-            const int half = (i - begin) & 1, place_next = place + 1 < kValueTiles ? place + 1 : 0;
+            const int half = (i - begin) & 1;
             const int32_t t0 = tiles.at(i) * kTile;
             const bool work = t0 <= wave_last;      // a wavefront whose rows see nothing here only turns codes
-            if (owed) add_values(w, place_before);
-            owed = false;
             f32x16 z[2];
             if (work) {
+                z[0] = z[1] = f32x16{};
+                const uint8_t *at = key_lds[half] + c * kKeyRow + 16 * h;
+                // two tokens' groups in turn, so that a product does not wait for the one before it
+                const auto piece = [&](int j) { return *reinterpret_cast<const half8 *>(at + 32 * (j & 1) * kKeyRow + 32 * (j >> 1)); };
+                half8 k[kAhead];
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    z[t] = f32x16{};
+                for (int j = 0; j < kAhead; ++j) k[j] = piece(j);
 #pragma unroll
-                    for (int f = 0; f < W / 16; ++f) {
-                        const half8 k = *reinterpret_cast<const half8 *>(key_lds[half] + (32 * t + c) * kKeyRow + 32 * f + 16 * h);
+                for (int j = 0; j < W / 8; ++j) {
+                    const half8 now = k[j % kAhead];
+                    if (j + kAhead < W / 8) k[j % kAhead] = piece(j + kAhead);
 #pragma unroll
-                        for (int n = 0; n < kParts; ++n) z[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[n][f], z[t], 0, 0, 0);
-                    }
+                    for (int n = 0; n < kParts; ++n) z[j & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now, q[n][j >> 1], z[j & 1], 0, 0, 0);
+                    
                 }
             }
-            if (i + 1 < end) to_lds(half ^ 1, place_next);
+            if (i + 1 < end) to_lds(half ^ 1);
             ask_codes(i + 2);
             ask_pages(i + 3);
             if (work) {
@@ -597,6 +602,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void k_attend_many(
                     for (int d = 0; d < kDims; ++d) o[d] *= by;
                 }
                 const float base = m == -INFINITY ? 0.0f : m;
+                bf16x8 w[4][kWeights];
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {       // 16 tokens
                     float x[8];
@@ -608,14 +614,10 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void k_attend_many(
                     }
                     split_weights<kWeights>(x, w[g]);
                 }
-                if (!late) add_values(w, place);
-                owed = late;
+                add_values(w, half);
             }
-            place_before = place;
-            place = place_next;
             __syncthreads();
         }
-        if (owed) add_values(w, place_before);
         l += __shfl_xor(l, 32);
         if (mine) {
             const float inv = l > 0.0f ? 1.0f / l : 0.0f, base = m == -INFINITY ? 0.0f : m;
@@ -727,9 +729,6 @@ int compute_units() {
     return cus > 0 ? cus : 256;
 }
 
-// Wavefronts of a workgroup of many rows: eight share a tile's codes best; where a wavefront's sums and queries take more than 256 registers, four.
-uint32_t many_waves(uint32_t width, uint32_t type) { return width > 128 || type == ENTRO_F32 ? 4 : 8; }
-
 // How far a call's tiles are split: as many workgroups as fill the chip, tiles of a workgroup not fewer than pay for the
 // join, which is a launch of its own.
 Shape shape_of(const entro_cache *c, const entro_cache_table *t, const entro_cache_query *q) {
@@ -741,11 +740,11 @@ Shape shape_of(const entro_cache *c, const entro_cache_table *t, const entro_cac
     const uint64_t tiles = (len + kTile - 1) / kTile, units = uint64_t{t->seqs} * c->kv_heads;
     uint64_t groups = units, per_cu = 2;
     if (rows > 16) {
-        s.waves = rows > 64 ? many_waves(width, q->type) : 2;
+        s.waves = rows > 64 ? 4 : 2;
         const uint64_t row_tiles = (rows + 32 * s.waves - 1) / (32 * s.waves), most = 0x3fffffffull / units;
         s.row_tiles = static_cast<uint32_t>(row_tiles < most ? row_tiles : (most ? most : 1));
         groups *= s.row_tiles;
-        per_cu = s.waves == 2 ? 4 : 1;
+        per_cu = s.waves == 2 ? 4 : 2;
     }
     const uint64_t cus = static_cast<uint64_t>(compute_units());
     uint64_t want, can;
@@ -772,14 +771,13 @@ Shape shape_of(const entro_cache *c, const entro_cache_table *t, const entro_cac
 
 template <int W, typename T>
 void launch_width(const Pool &p, const Query &a, const Shape &s, hipStream_t st) {
-    constexpr int kMost = W > 128 || sizeof(T) == 4 ? 4 : 8;
     const uint32_t units = p.seqs * p.kv_heads * a.splits;
     if (s.waves == 0)
         hipLaunchKernelGGL((k_attend_few<W, T>), dim3(p.seqs < 8 ? units : (p.seqs + 7) / 8 * 8 * p.kv_heads * a.splits), dim3(kWG), 0, st, p, a);
     else if (s.waves == 2)
         hipLaunchKernelGGL((k_attend_many<W, T, 2>), dim3(units * s.row_tiles), dim3(128), 0, st, p, a, s.row_tiles);
     else
-        hipLaunchKernelGGL((k_attend_many<W, T, kMost>), dim3(units * s.row_tiles), dim3(kMost * 64), 0, st, p, a, s.row_tiles);
+        hipLaunchKernelGGL((k_attend_many<W, T, 4>), dim3(units * s.row_tiles), dim3(256), 0, st, p, a, s.row_tiles);
     if (a.splits > 1) {
         const dim3 join(p.seqs * a.q_heads, s.join_rows);
         hipLaunchKernelGGL((k_attend_join<W, T>), join, dim3(kWG), 0, st, p, a, s.waves ? 32 * s.waves : 16u);
