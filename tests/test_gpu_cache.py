@@ -537,3 +537,32 @@ def test_a_step_in_a_graph_follows_lengths_that_change():
         assert torch.equal(out, out_twin) and torch.equal(cache.k, twin.k) and torch.equal(cache.v, twin.v)
         pool.k, pool.v, pool.k_scale, pool.v_scale = (x.cpu().numpy() for x in (cache.k, cache.v, cache.k_scale, cache.v_scale))
         check_attend(pool, table, list(lengths + step), q.float().cpu().numpy(), np.arange(4), "bf16", out, None, dim ** -0.5)
+
+
+def test_the_example_s_steps_against_the_definition():
+    """Products over compressed weights, page tables, rows, attention and the output's product together: the last step of a few, in
+    beams that fork, against the definitions on what the steps before it left."""
+    from examples import token_step as ex
+    cfg, heads, kv_heads, dim = ex.LAYERS["smol"]
+    beams, window, sinks = 3, 40, 4
+    layer = ex.Layer(cfg, beams)
+    g = ex.Generation(layer, heads, kv_heads, dim, beams, 120, page=16, window=window, sinks=sinks)
+    torch.manual_seed(5)
+    g.prompt(*(torch.randn(70, kv_heads, dim, device=DEV).to(torch.bfloat16) for _ in "kv"))
+    parents = [[0, 0, 0], [2, 0, 2], [0, 1, 1], [1, 1, 0], [0, 1, 2]]
+    for parent in parents:
+        layer.x.copy_(torch.randn(layer.x.shape, device=DEV))
+        g.step(ints(parent))
+    torch.cuda.synchronize()
+    assert g.status.tolist()[0] == 0 and g.table.lengths.tolist() == [75] * beams
+    pool = ref.Pool(np.random.default_rng(0), 1, 1, kv_heads, 16, dim)
+    pool.pages = g.cache.pages
+    pool.k, pool.v, pool.k_scale, pool.v_scale = (x.cpu().numpy() for x in (g.cache.k, g.cache.v, g.cache.k_scale, g.cache.v_scale))
+    table = g.table.slots.cpu().numpy()
+    assert (table[:, 1] == -1).all() and (table[:, 0] >= 0).all()          # positions 16..31 have left the window, those of the first tokens have not
+    q = layer.q.view(beams, heads, dim).float().cpu().numpy()
+    check_attend(pool, table, [75] * beams, q, np.arange(beams + 1), "bf16", layer.attended.view(beams, heads, dim), None, dim ** -0.5, window, sinks)
+    k, v = ref.read(pool, table, [75] * beams, np.arange(beams + 1), beams)
+    for got, fresh, scale in ((k, layer.k, pool.k_scale), (v, layer.v, pool.v_scale)):
+        step = scale[0, table[:, 74 // 16]][..., None]
+        assert np.all(np.abs(got - fresh.view(beams, kv_heads, dim).float().cpu().numpy()) <= step * 0.5 * (1 + 2.0 ** -16))
