@@ -5,7 +5,7 @@ namespace {
 
 using namespace entro_detail;
 
-constexpr int kWG = 256;
+constexpr int kWG = 256;                       // four wavefronts
 
 struct Query {
     const void *q;
@@ -30,6 +30,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr uint32_t kMostSplits = kWG;          // the join has a lane for each
+constexpr uint32_t kManyRows = 128;            // of a workgroup for many rows
 constexpr int kTile = 64;                      // tokens a wavefront takes at a time
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -164,11 +165,17 @@ __device__ inline void split_halves(const float *x, half8 *hi, half8 *lo) {
 // ------------------------------------------------------------------------------------------------- few rows: token generation
 //
 // A wavefront multiplies 64 tokens at a time with up to 16 rows (tokens of a sequence and query heads that share a key head) on
-// v_mfma_f32_16x16x32_f16. It computes scores transposed, tokens x rows: a lane then holds 16 tokens of one row, and by the
+// v_mfma_f32_16x16x32. It computes scores transposed, tokens x rows: a lane then holds 16 tokens of one row, and by the
 // choice of which key goes to which matrix row these are 16 tokens side by side in memory (lane group g: tokens 16 g ..
 // 16 g + 15), which is also what it loads of the values (16 bytes of one dimension) and what the second product wants of
 // the probabilities. Keys, values and probabilities so go from memory through registers to the matrix units, with no
-// exchange between lanes but for the maximum. Matrix unit slots that a tile of 16 rows leaves empty cost nothing: the bytes bound it.
+// exchange between lanes but for the maximum. Matrix unit slots that a tile of 16 rows leaves empty cost nothing.
+//
+// Bound by the bytes of the codes. The softmax and the turning of codes into numbers take about 500 vector instructions a
+// tile, a third of the time its 16 KB (128 dimensions) take to arrive; so what counts is that loads are always on their way: page numbers are
+// asked for two tiles ahead, a tile's codes as soon as the last tile's have been used. Measured: 131072 tokens of 8 heads of 128
+// 55 us with the join (4.9 TB/s; loads alone 51 to 56), 32 sequences in a window of 4096 with 32 heads of 96 139 us (5.5 TB/s), 64 sequences of
+// up to 8192 tokens 130 us (4.3 TB/s: sequences of different lengths, see shape_of).
 template <int W, typename T>
 __global__ __launch_bounds__(kWG, W > 128 ? 1 : 2) void k_attend_few(Pool p, Query a) {
     constexpr int kParts = sizeof(T) == 2 ? 1 : 2;         // halves that make a factor of the first product
@@ -397,9 +404,14 @@ __global__ __launch_bounds__(kWG, W > 128 ? 1 : 2) void k_attend_few(Pool p, Que
 // v_mfma_f32_32x32x16, scores transposed as above: a lane holds 32 of a tile's scores of one row, tokens 8 i + 4 h + (0..3)
 // of each 32, h being the lane's half. The values' tokens lie in LDS in the order 0-3, 8-11, 4-7, 12-15 of each 16, so that what a
 // lane reads of them for the second product are the tokens whose weights it has.
-template <int W, typename T, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, WAVES == 4 && sizeof(T) == 2 && W <= 128 ? 2 : 1) void k_attend_many(Pool p, Query a, uint32_t row_tiles) {
-    constexpr int kThreads = WAVES * 64, kRows = WAVES * 32;
+//
+// Bound by issue: of a wavefront's time, matrix instructions take 40 % and vector instructions 50 %, and the two of different
+// wavefronts overlap little. 4096 rows of 32 heads of 128 over 8192 tokens: 650 us, 0.63 PFLOP/s of the definition's operations (0.95 of the
+// matrix units', as weights are two bf16 numbers); of that, about 280 us go with the second product, 180 with the first, 140 with the
+// softmax, 110 with codes on their way to LDS.
+template <int W, typename T>
+__global__ __launch_bounds__(kWG, sizeof(T) == 2 && W <= 128 ? 2 : 1) void k_attend_many(Pool p, Query a, uint32_t row_tiles) {
+    constexpr int kThreads = kWG, kRows = kManyRows;
     constexpr int kParts = sizeof(T) == 2 ? 1 : 2, kWeights = sizeof(T) == 2 ? 2 : 3;
     constexpr int kChunks = (W * 4 + kThreads - 1) / kThreads;      // pieces of 16 codes a thread turns, of keys and of values
     constexpr int kKeyRow = 2 * W + 16, kValueRow = 2 * kTile + 16;   // bytes
@@ -539,7 +551,6 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 && sizeof(T) == 2 && W <= 12
                 if (i + kAhead < 4 * kDims) v[i % kAhead] = piece(i + kAhead);
 #pragma unroll
                 for (int n = 0; n < kWeights; ++n) o[i % kDims] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(now, w[i / kDims][n], o[i % kDims], 0, 0, 0);
-                
             }
         };
         for (int32_t i = begin; i < end; ++i) {
@@ -561,7 +572,6 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 && sizeof(T) == 2 && W <= 12
                     if (j + kAhead < W / 8) k[j % kAhead] = piece(j + kAhead);
 #pragma unroll
                     for (int n = 0; n < kParts; ++n) z[j & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now, q[n][j >> 1], z[j & 1], 0, 0, 0);
-                    
                 }
             }
             if (i + 1 < end) to_lds(half ^ 1);
@@ -718,7 +728,7 @@ entro_status check_query(const entro_cache *c, const entro_cache_query *q) {
 }
 
 struct Shape {
-    uint32_t waves;                // 0: the kernel for few rows; otherwise wavefronts of the one for many
+    bool many;                     // the kernel for many rows
     uint32_t row_tiles, splits, least, join_rows;
     uint64_t bytes;
 };
@@ -732,39 +742,40 @@ int compute_units() {
 // How far a call's tiles are split: as many workgroups as fill the chip, tiles of a workgroup not fewer than pay for the
 // join, which is a launch of its own.
 Shape shape_of(const entro_cache *c, const entro_cache_table *t, const entro_cache_query *q) {
-    Shape s = {0, 1, 1, 16, q->max_new < 1 ? 1 : q->max_new > 65535 ? 65535 : q->max_new, 0};
+    Shape s = {false, 1, 1, 16, q->max_new < 1 ? 1 : q->max_new > 65535 ? 65535 : q->max_new, 0};
     const uint32_t width = entro_cache_width(c->head_dim);
     const uint64_t rows = uint64_t{q->max_new} * (q->q_heads / c->kv_heads);
     uint64_t len = q->max_len;
     if (q->window && len > uint64_t{q->window} + q->sinks + q->max_new + 2 * kTile) len = uint64_t{q->window} + q->sinks + q->max_new + 2 * kTile;
     const uint64_t tiles = (len + kTile - 1) / kTile, units = uint64_t{t->seqs} * c->kv_heads;
-    uint64_t groups = units, per_cu = 2;
-    if (rows > 16) {
-        s.waves = rows > 64 ? 4 : 2;
-        const uint64_t row_tiles = (rows + 32 * s.waves - 1) / (32 * s.waves), most = 0x3fffffffull / units;
+    uint64_t groups = units;
+    // up to 32 rows in groups of 16, one after the other (32 and 48 rows of 128 dimensions over 4096 tokens of 8 sequences: 45 and 66 us,
+    // by the kernel for many 56 and 61)
+    if (rows > 32) {
+        s.many = true;
+        const uint64_t row_tiles = (rows + kManyRows - 1) / kManyRows, most = 0x3fffffffull / units;
         s.row_tiles = static_cast<uint32_t>(row_tiles < most ? row_tiles : (most ? most : 1));
         groups *= s.row_tiles;
-        per_cu = s.waves == 2 ? 4 : 2;
     }
     const uint64_t cus = static_cast<uint64_t>(compute_units());
     uint64_t want, can;
-    if (s.waves == 0 && units * 4 > cus * 2) {
+    if (!s.many && units * 4 > cus * 2) {
         // the heads of many sequences fill the chip; pieces of at most 96 tiles keep one long sequence from being the last
         // alone (8192 tokens of 64 sequences in one, two, four pieces: 128, 130, 127 us; 4096 of 32 with 32 heads: 139, 147, 154)
         want = can = (tiles + 95) / 96;
-    } else if (s.waves == 0) {
+    } else if (!s.many) {
         // two workgroups a compute unit are enough (131072 tokens, 8 heads: 64 pieces 55 us, 128 pieces 60 us); below 24 tiles the
         // join costs more than it gives (9 tiles: 8.1 us in one piece, 11.3 in two)
         want = cus * 2 / units;
         can = tiles < 24 ? 1 : tiles / 8;
     } else {
-        want = (cus * per_cu + groups - 1) / groups;
+        want = (cus * 2 + groups - 1) / groups;
         can = (tiles + s.least - 1) / s.least;
     }
     s.splits = static_cast<uint32_t>(want < can ? want : can);
     if (s.splits < 1) s.splits = 1;
     if (s.splits > kMostSplits) s.splits = kMostSplits;
-    if (s.waves == 0 && tiles) s.least = static_cast<uint32_t>((tiles + s.splits - 1) / s.splits);
+    if (!s.many && tiles) s.least = static_cast<uint32_t>((tiles + s.splits - 1) / s.splits);
     if (s.splits > 1) s.bytes = uint64_t{q->tokens} * q->q_heads * s.splits * (width + 1) * 4;
     return s;
 }
@@ -772,15 +783,13 @@ Shape shape_of(const entro_cache *c, const entro_cache_table *t, const entro_cac
 template <int W, typename T>
 void launch_width(const Pool &p, const Query &a, const Shape &s, hipStream_t st) {
     const uint32_t units = p.seqs * p.kv_heads * a.splits;
-    if (s.waves == 0)
+    if (!s.many)
         hipLaunchKernelGGL((k_attend_few<W, T>), dim3(p.seqs < 8 ? units : (p.seqs + 7) / 8 * 8 * p.kv_heads * a.splits), dim3(kWG), 0, st, p, a);
-    else if (s.waves == 2)
-        hipLaunchKernelGGL((k_attend_many<W, T, 2>), dim3(units * s.row_tiles), dim3(128), 0, st, p, a, s.row_tiles);
     else
-        hipLaunchKernelGGL((k_attend_many<W, T, 4>), dim3(units * s.row_tiles), dim3(256), 0, st, p, a, s.row_tiles);
+        hipLaunchKernelGGL((k_attend_many<W, T>), dim3(units * s.row_tiles), dim3(kWG), 0, st, p, a, s.row_tiles);
     if (a.splits > 1) {
         const dim3 join(p.seqs * a.q_heads, s.join_rows);
-        hipLaunchKernelGGL((k_attend_join<W, T>), join, dim3(kWG), 0, st, p, a, s.waves ? 32 * s.waves : 16u);
+        hipLaunchKernelGGL((k_attend_join<W, T>), join, dim3(kWG), 0, st, p, a, s.many ? kManyRows : 16u);
     }
 }
 

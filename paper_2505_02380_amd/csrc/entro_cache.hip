@@ -202,7 +202,8 @@ __device__ inline void write_patch(const Pool &p, uint64_t unit, const Patch &a,
 
 // LANES lanes to a block and head: a wavefront where that has few patches, else the workgroup. Rows are read once where every lane
 // has one patch (up to 64 tokens of 128 dimensions), else twice.  Bound by the bytes of the rows and codes for prompts, by
-// the latency of four dependent loads (row numbers, page, rows and scale, codes) for single tokens.
+// the latency of dependent loads (row numbers, page and rows, scale) for single tokens.  24700 rows of 8 heads of 128: 44 us written,
+// 31 us read back as bf16 (3.5 and 4.9 TB/s); a row of each of 64 sequences 7.6 us.
 template <typename T, int LANES>
 __global__ __launch_bounds__(kWG) void k_append(Pool p, Rows r, uint32_t blocks, uint32_t work) {
     __shared__ uint32_t most[2][kWG / 64];
@@ -486,9 +487,11 @@ __global__ __launch_bounds__(kWG) void k_regroup_fill(Regroup g, PageWork w, con
 
 // ------------------------------------------------------------------------------------- small tables: one workgroup for all of it
 //
-// Four launches in a row cost more than their work where the table is small: one workgroup then goes through the same steps with
-// its marks in LDS (a step of 64 rows and 660 pages: see k_regroup_plan for the steps).
-constexpr uint32_t kSmallPages = 16384, kSmallSlots = 65536;
+// Four launches in a row cost more than their work where the table is small: one workgroup then goes through the same steps with its
+// marks in LDS.  The whole call, by one workgroup and by four launches: 2112 slots and 1100 pages 11.7 and 19.7 us, 4096 and 3000 13.9 and
+// 21.2, 8192 and 7000 23.3 and 20.6; compaction 4096 and 3000 12.6 and 20.1, 16384 and 9000 29.2 and 32.6, 65536 and 15000
+// 56.8 and 47.4.
+constexpr uint32_t kSmallPages = 8192, kSmallRegroup = 6144, kSmallCompact = 16384;   // pages; slots of the next table
 
 __global__ __launch_bounds__(kScanWG) void k_regroup_one(Regroup g, PageWork w, int32_t *status) {
     __shared__ int32_t owner[kSmallPages];
@@ -631,7 +634,8 @@ struct Copies {
     uint32_t heads, layers, pages;
 };
 
-// Pages src[i] -> dst[i], i < counts[0], in all layers. A work item is a page of k or v of a layer.
+// Pages src[i] -> dst[i], i < counts[0], in all layers. A work item is a page of k or v of a layer. 1.1 GB moved in
+// 450 us: 5.0 TB/s read and written, what a large copy reaches (4.7).
 __global__ __launch_bounds__(kWG) void k_copy_pages(Copies c, const int32_t *src, const int32_t *dst, const int32_t *counts) {
     const uint64_t items = uint64_t{static_cast<uint32_t>(counts[0])} * c.layers * 2;
     const uint32_t vecs = static_cast<uint32_t>(c.page_bytes / 16);
@@ -773,7 +777,7 @@ dim3 rows_grid(uint32_t stride, uint32_t seqs) {
 
 unsigned fill_grid(uint32_t pages) { return pages < 1024 * kWG ? (pages + kWG - 1) / kWG : 1024; }
 
-bool small(const entro_cache *c, const entro_cache_table *t) { return c->pages <= kSmallPages && uint64_t{t->seqs} * t->stride <= kSmallSlots; }
+bool small(const entro_cache *c, const entro_cache_table *t, uint32_t slots) { return c->pages <= kSmallPages && uint64_t{t->seqs} * t->stride <= slots; }
 
 unsigned copy_grid(uint64_t most, uint32_t layers) {
     const uint64_t items = most * layers * 2;
@@ -828,7 +832,7 @@ entro_status entro_cache_regroup(const entro_cache *c, const entro_cache_table *
     pages_workspace(c, next, &w, workspace);
     const Regroup g = {*t, *next, parent, grow, c->pages, static_cast<uint32_t>(__builtin_ctz(c->page_tokens)), window, sinks};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (small(c, next)) {
+    if (small(c, next, kSmallRegroup)) {
         hipLaunchKernelGGL(k_regroup_one, dim3(1), dim3(kScanWG), 0, st, g, w, status);
     } else {
         hipLaunchKernelGGL(k_page_fill, dim3(fill_grid(c->pages)), dim3(kWG), 0, st, w.owner, c->pages, kNoOwner);
@@ -848,7 +852,7 @@ entro_status entro_cache_compact(const entro_cache *c, const entro_cache_table *
     PageWork w;
     pages_workspace(c, next, &w, workspace);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (small(c, next)) {
+    if (small(c, next, kSmallCompact)) {
         hipLaunchKernelGGL(k_compact_one, dim3(1), dim3(kScanWG), 0, st, *t, *next, c->pages, w, status);
     } else {
         hipLaunchKernelGGL(k_page_fill, dim3(fill_grid(c->pages)), dim3(kWG), 0, st, w.owner, c->pages, kNoOwner);
