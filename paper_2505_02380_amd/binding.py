@@ -625,6 +625,11 @@ class CacheQuery:
                              _rows_type(q, "q"), layer, window, sinks, q.shape[2] ** -0.5 if scale is None else scale, 0)
 
 
+def _on_gpu(*tensors):
+    device = tensors[0].device
+    _need(device.type == "cuda" and all(t.device == device for t in tensors), "all tensors of a call lie on one GPU")
+
+
 def _same_heads(cache: Cache, table: CacheTable, x, start):
     _need(x.shape[2] == cache.head_dim, f"rows have {cache.head_dim} dimensions")
     _need(start.numel() == table.c.seqs + 1, f"start is [{table.c.seqs} + 1]")
@@ -633,12 +638,14 @@ def _same_heads(cache: Cache, table: CacheTable, x, start):
 def entro_cache_append(cache: Cache, table: CacheTable, rows: CacheRows, stream=None):
     _same_heads(cache, table, rows.k, rows.start)
     _need(rows.k.shape[1] == cache.kv_heads, f"rows have {cache.kv_heads} heads")
+    _on_gpu(cache.k, table.slots, rows.k, rows.v, rows.start)
     _check(lib().entro_cache_append(C.byref(cache.c), C.byref(table.c), C.byref(rows.c), _stream_ptr(stream)), "entro_cache_append")
 
 
 def entro_cache_read(cache: Cache, table: CacheTable, rows: CacheRows, stream=None):
     _same_heads(cache, table, rows.k, rows.start)
     _need(rows.k.shape[1] == cache.kv_heads, f"rows have {cache.kv_heads} heads")
+    _on_gpu(cache.k, table.slots, rows.k, rows.v, rows.start)
     _check(lib().entro_cache_read(C.byref(cache.c), C.byref(table.c), C.byref(rows.c), _stream_ptr(stream)), "entro_cache_read")
 
 
@@ -653,6 +660,7 @@ def _workspace(ws):
 
 def entro_cache_attend(cache: Cache, table: CacheTable, query: CacheQuery, workspace=None, stream=None):
     _same_heads(cache, table, query.q, query.start)
+    _on_gpu(cache.k, table.slots, query.q, query.out, query.start)
     _check(lib().entro_cache_attend(C.byref(cache.c), C.byref(table.c), C.byref(query.c), *_workspace(workspace), _stream_ptr(stream)),
            "entro_cache_attend")
 
@@ -665,12 +673,14 @@ def entro_cache_regroup(cache: Cache, table: CacheTable, following: CacheTable, 
                         window: int = 0, sinks: int = 0, stream=None):
     """`following` receives the table of the next step; status: int32 device tensor of 4 (entro_cache_status reads its first word)."""
     n = following.c.seqs
+    _on_gpu(cache.k, table.slots, following.slots, status, workspace)
     _check(lib().entro_cache_regroup(C.byref(cache.c), C.byref(table.c), None if parent is None else _ints(parent, n, "parent"),
                                      None if grow is None else _ints(grow, n, "grow"), window, sinks, C.byref(following.c),
                                      _ints(status, 4, "status"), *_workspace(workspace), _stream_ptr(stream)), "entro_cache_regroup")
 
 
 def entro_cache_compact(cache: Cache, table: CacheTable, following: CacheTable, status, workspace, stream=None):
+    _on_gpu(cache.k, table.slots, following.slots, status, workspace)
     _check(lib().entro_cache_compact(C.byref(cache.c), C.byref(table.c), C.byref(following.c), _ints(status, 4, "status"),
                                      *_workspace(workspace), _stream_ptr(stream)), "entro_cache_compact")
 

@@ -265,6 +265,14 @@ __global__ __launch_bounds__(kWG) void k_read(Pool p, Rows r, uint32_t blocks, u
     constexpr uint32_t kUnits = kWG / LANES;
     const uint32_t lane = threadIdx.x % LANES, patches = ((p.head_dim + 7) / 8) << (p.page_shift - 2), pt = 1u << p.page_shift;
     for (uint32_t w = blockIdx.x * kUnits + threadIdx.x / LANES; w < work; w += gridDim.x * kUnits) {
+        if (w / p.kv_heads % blocks == 0) {           // rows before position 0: zeros
+            const Span s = span_of(r.start, p.lengths, w / p.kv_heads / blocks, r.tokens);
+            for (int32_t j = 0; j < min(-s.pos, s.count); ++j)
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv)
+                    for (uint32_t d = lane; d < p.head_dim; d += LANES)
+                        static_cast<T *>(r.x[kv])[static_cast<uint32_t>(s.row + j) * r.token_stride[kv] + w % p.kv_heads * r.head_stride[kv] + d] = 0;
+        }
         each_block(p, r, blocks, w, [&](const Block &b, uint32_t head) {
             const int32_t page = checked_page(p, b.entry, b.at);
             const uint64_t unit = uint64_t{static_cast<uint32_t>(max(page, 0))} * p.kv_heads + head;

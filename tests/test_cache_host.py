@@ -151,6 +151,32 @@ def test_the_binding_looks_at_shapes_and_types():
             bad()
 
 
+def test_calls_refuse_tensors_that_lie_in_host_memory():
+    k, v, s = torch.zeros(1, 4, 2, 16, 64, dtype=torch.uint8), torch.zeros(1, 4, 2, 64, 16, dtype=torch.uint8), torch.zeros(1, 4, 2)
+    cache, table, other = E.Cache(k, v, s, s, 16, 40), E.CacheTable.empty(3, 5, device="cpu"), E.CacheTable.empty(3, 5, device="cpu")
+    start, x = torch.zeros(4, dtype=torch.int32), torch.zeros(7, 2, 40)
+    status, ws = torch.zeros(4, dtype=torch.int32), torch.zeros(1 << 16, dtype=torch.uint8)
+    for call in (lambda: E.entro_cache_append(cache, table, E.CacheRows(x, x, start, 1)), lambda: E.entro_cache_read(cache, table, E.CacheRows(x, x, start, 1)),
+                 lambda: E.entro_cache_attend(cache, table, E.CacheQuery(x, x, start, 1, 1), ws),
+                 lambda: E.entro_cache_regroup(cache, table, other, status, ws), lambda: E.entro_cache_compact(cache, table, other, status, ws)):
+        with pytest.raises(ValueError):
+            call()
+
+
+def test_attend_refuses_a_workspace_that_is_none_or_too_small():
+    L = B.lib()
+    cache, table, _, query = good()
+    table.seqs, query.max_new, query.max_len = 1, 1, 1 << 17
+    c, t, q = C.byref(cache), C.byref(table), C.byref(query)
+    need = L.entro_cache_attend_workspace_bytes(c, t, q)
+    assert need > 0
+    assert L.entro_cache_attend(c, t, q, None, need, None) == B.ENTRO_ERR_NULL
+    assert L.entro_cache_attend(c, t, q, PTR + 8, need, None) == B.ENTRO_ERR_ALIGN
+    assert L.entro_cache_attend(c, t, q, PTR, need - 1, None) == B.ENTRO_ERR_CAPACITY
+    query.max_len = 100
+    assert L.entro_cache_attend_workspace_bytes(c, t, q) == 0
+
+
 def test_the_reference_s_regroup_by_hand():
     """Three rows of one sequence of 20 tokens in blocks of 16: they share the full block; the lowest keeps the open one."""
     table = np.array([[5, 2]], np.int32)

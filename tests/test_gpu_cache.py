@@ -361,6 +361,24 @@ def test_append_leaves_all_else_alone():
         assert np.array_equal(got.cpu().numpy(), want.astype(np.float32))
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("page,dim", [(16, 24), (64, 128)])
+def test_read_writes_all_rows_of_its_sequences_and_no_others(kind, page, dim):
+    """Zeros for positions before 0, in sequences without tokens, past the table and without a page; other rows stay."""
+    rng = np.random.default_rng(19)
+    lengths, counts, heads = [3, 0, 2 * page + 5, 7], [page + 9, 4, page + 7, 0], 2
+    pool, table = make(rng, 4, lengths, heads, dim, page)
+    scales(rng, pool, table)
+    table = np.ascontiguousarray(table[:, :2])
+    table[2, 1] = -1
+    start = starts(counts) + 2
+    back = [torch.full((start[-1] + 3, heads, dim), 7.0, dtype=TYPES[kind], device=DEV) for _ in "kv"]
+    E.entro_cache_read(cache_of(pool), E.CacheTable(dev(table), ints(lengths)), E.CacheRows(*back, ints(start), 3))
+    for got, want in zip(back, ref.read(pool, table, lengths, start, start[-1] + 3)):
+        want[:2] = want[start[-1]:] = 7
+        assert torch.equal(got.cpu(), torch.from_numpy(want.astype(np.float32)).to(TYPES[kind]))
+
+
 # ----------------------------------------------------------------------------------------------------------------- page tables
 def run_pages(pool, table, lengths, seqs, stride, call):
     cache = cache_of(pool)
