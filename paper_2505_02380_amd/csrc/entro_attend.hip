@@ -175,7 +175,7 @@ __device__ inline void split_halves(const float *x, half8 *hi, half8 *lo) {
 // tile, a third of the time its 16 KB (128 dimensions) take to arrive; so what counts is that loads are always on their way: page numbers are
 // asked for two tiles ahead, a tile's codes as soon as the last tile's have been used. Measured: 131072 tokens of 8 heads of 128
 // 55 us with the join (4.9 TB/s; loads alone 51 to 56), 32 sequences in a window of 4096 with 32 heads of 96 139 us (5.5 TB/s), 64 sequences of
-// up to 8192 tokens 130 us (4.3 TB/s: sequences of different lengths, see shape_of).
+// up to 8192 tokens 127 us (4.4 TB/s: sequences of different lengths, see shape_of).
 template <int W, typename T>
 __global__ __launch_bounds__(kWG, W > 128 ? 1 : 2) void k_attend_few(Pool p, Query a) {
     constexpr int kParts = sizeof(T) == 2 ? 1 : 2;         // halves that make a factor of the first product
@@ -184,7 +184,7 @@ __global__ __launch_bounds__(kWG, W > 128 ? 1 : 2) void k_attend_few(Pool p, Que
     constexpr int kDims = W / 16;
     __shared__ float merge_o[4][16][W + 4];
     __shared__ float merge_m[4][16], merge_l[4][16];
-    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6, g = lane >> 4, c = lane & 15u;
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15u;
     // Workgroups go to the XCDs in turn. Those of one XCD take the key heads of the same sequence and split, whose codes lie side by side, and
     // the splits of a sequence go to different XCDs, so that long sequences do not meet on one.
     const uint32_t r = p.seqs < 8 ? blockIdx.x : blockIdx.x / 8, head = r % p.kv_heads, split = r / p.kv_heads % a.splits, block = r / p.kv_heads / a.splits;
@@ -419,7 +419,7 @@ __global__ __launch_bounds__(kWG, sizeof(T) == 2 && W <= 128 ? 2 : 1) void k_att
     __shared__ __attribute__((aligned(16))) uint8_t key_lds[2][kKeyTile], value_lds[2][kValueTile];
     __shared__ f32x4 tile_ks[2], tile_vs[2];
     __shared__ int32_t tile_ok[2][4];
-    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6, h = lane >> 5, c = lane & 31u;
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, c = lane & 31u;
     // workgroups of one key head follow each other at multiples of the number of heads: with 8 heads, on one XCD and its L2
     const uint32_t units = p.seqs * p.kv_heads, unit = blockIdx.x % units, head = unit % p.kv_heads, b = unit / p.kv_heads;
     const uint32_t split = blockIdx.x / units % a.splits, tile_from_end = blockIdx.x / units / a.splits;
@@ -488,7 +488,7 @@ __global__ __launch_bounds__(kWG, sizeof(T) == 2 && W <= 128 ? 2 : 1) void k_att
                 k_page[n] = table_entry(p, b, t0 + min(ch / (W / 16), kTile - 1));
                 v_page[n] = table_entry(p, b, t0 + 16 * (ch & 3));
             }
-            s_page = table_entry(p, b, t0 + 16 * static_cast<int32_t>(tid & 3u));
+            if (wave == 0) s_page = table_entry(p, b, t0 + 16 * static_cast<int32_t>(tid & 3u));
         };
         const auto ask_codes = [&](int32_t i) {
             const int32_t t0 = tiles.at(min(i, end - 1)) * kTile;
@@ -500,11 +500,13 @@ __global__ __launch_bounds__(kWG, sizeof(T) == 2 && W <= 128 ? 2 : 1) void k_att
                 kc[n] = *reinterpret_cast<const u32x4 *>(k_head + k_id * page_stride + (static_cast<uint32_t>(k_at) & in_page) * W + 16 * (ch % (W / 16)));
                 vc[n] = *reinterpret_cast<const u32x4 *>(v_head + v_id * page_stride + (static_cast<uint32_t>(ch >> 2) << p.page_shift) + (static_cast<uint32_t>(v_at) & in_page));
             }
-            const int32_t id = checked_page(p, s_page, t0 + 16 * static_cast<int32_t>(tid & 3u));
-            const uint64_t at = uint64_t{static_cast<uint32_t>(max(id, 0))} * p.kv_heads + head;
-            ks = p.k_scale[at];
-            vs = p.v_scale[at];
-            s_ok = id >= 0;
+            if (wave == 0) {
+                const int32_t id = checked_page(p, s_page, t0 + 16 * static_cast<int32_t>(tid & 3u));
+                const uint64_t at = uint64_t{static_cast<uint32_t>(max(id, 0))} * p.kv_heads + head;
+                ks = p.k_scale[at];
+                vs = p.v_scale[at];
+                s_ok = id >= 0;
+            }
         };
         const auto to_lds = [&](int half) {
 #pragma unroll
