@@ -657,7 +657,7 @@ __global__ __launch_bounds__(kWG, sizeof(T) == 2 && W <= 128 ? 2 : 1) void k_att
 // Joins the parts of rows whose tiles were split. A workgroup per row and head: its lanes stand for four dimensions each, and as often as
 // they cover a row they take parts in turn.
 template <int W, typename T>
-__global__ __launch_bounds__(kWG) void k_attend_join(Pool p, Query a, uint32_t rows_per_tile) {
+__global__ __launch_bounds__(kWG) void k_attend_join(Pool p, Query a) {
     constexpr int kLanes = W / 4, kSets = kWG / kLanes;
     __shared__ f32x4 sums[kSets][kLanes];
     __shared__ float wave_most[kWG / 64], wave_sum[kWG / 64], shares[kWG];
@@ -668,9 +668,9 @@ __global__ __launch_bounds__(kWG) void k_attend_join(Pool p, Query a, uint32_t r
         const uint32_t token = static_cast<uint32_t>(s.row + nth);
         const uint64_t at = uint64_t{token} * a.q_heads + h;
         const int64_t rows = int64_t{s.count} * a.group, row = int64_t{nth} * a.group + h % a.group;
-        const int64_t row0 = row / rows_per_tile * rows_per_tile;
+        const int64_t row0 = row / 16 * 16;
         const Tiles tiles = tiles_of(p, a, s.pos + static_cast<int32_t>(row0 / a.group),
-                                     s.pos + static_cast<int32_t>(min(row0 + rows_per_tile - 1, rows - 1) / a.group));
+                                     s.pos + static_cast<int32_t>(min(row0 + 15, rows - 1) / a.group));
         const int32_t per = tiles_per_split(a, tiles.count);
         const uint32_t parts = static_cast<uint32_t>(max((tiles.count + per - 1) / per, 1));
         const float *lse = a.part_lse + at * a.splits;
@@ -712,6 +712,53 @@ __global__ __launch_bounds__(kWG) void k_attend_join(Pool p, Query a, uint32_t r
     }
 }
 
+// The same for many rows in a few parts: a wavefront per row and head, no more than a lane a part.
+template <int W, typename T>
+__global__ __launch_bounds__(kWG) void k_attend_join_rows(Pool p, Query a) {
+    constexpr uint32_t kLanes = W / 4, kSets = 64 / kLanes;
+    const uint32_t lane = threadIdx.x & 63u, set = lane / kLanes, d = lane % kLanes;
+    const uint32_t unit = blockIdx.x * (kWG / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = unit % a.q_heads, b = unit / a.q_heads;
+    if (b >= p.seqs) return;
+    const Span s = span_of(a.start, p.lengths, b, a.tokens);
+    const int64_t rows = int64_t{s.count} * a.group;
+    for (int32_t nth = static_cast<int32_t>(blockIdx.y); nth < s.count; nth += static_cast<int32_t>(gridDim.y)) {
+        const uint32_t token = static_cast<uint32_t>(s.row + nth);
+        const uint64_t at = uint64_t{token} * a.q_heads + h;
+        const int64_t row0 = (int64_t{nth} * a.group + h % a.group) / kManyRows * kManyRows;
+        const Tiles tiles = tiles_of(p, a, s.pos + static_cast<int32_t>(row0 / a.group),
+                                     s.pos + static_cast<int32_t>(min(row0 + kManyRows - 1, rows - 1) / a.group));
+        const int32_t per = tiles_per_split(a, tiles.count);
+        const uint32_t parts = static_cast<uint32_t>(max((tiles.count + per - 1) / per, 1));
+        const float mine = lane < parts ? a.part_lse[at * a.splits + lane] : -INFINITY;
+        float most = mine;
+        for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+        const float base = most == -INFINITY ? 0.0f : most, share = __builtin_amdgcn_exp2f(mine - base);
+        float sum = share;
+        for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+        const f32x4 *part = reinterpret_cast<const f32x4 *>(a.part_o + at * a.splits * W);
+        f32x4 x = {0, 0, 0, 0};
+        for (uint32_t i0 = 0; i0 < parts; i0 += kSets) {
+            const uint32_t i = i0 + set;
+            const float by = __shfl(share, static_cast<int>(min(i, 63u)));
+            if (set < kSets && i < parts) x += part[i * kLanes + d] * by;
+        }
+#pragma unroll
+        for (uint32_t i = 1; i < kSets; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float other = __shfl(x[j], static_cast<int>(d + i * kLanes));
+                if (set == 0) x[j] += other;
+            }
+        const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+        T *out = static_cast<T *>(a.out) + token * a.out_token_stride + h * a.out_head_stride;
+        if (set == 0)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (4 * d + j < p.head_dim) store_as(out + 4 * d + j, sum == sum ? x[j] * inv : sum);
+        if (lane == 0 && a.lse) a.lse[at] = sum > 0.0f ? (base + __builtin_amdgcn_logf(sum)) * kLn2 : (sum == sum ? -INFINITY : sum);
+    }
+}
+
 entro_status check_query_sizes(const entro_cache *c, const entro_cache_query *q) {
     if (!q) return ENTRO_ERR_NULL;
     if (q->type != ENTRO_F32 && q->type != ENTRO_BF16) return ENTRO_ERR_SCHEME;
@@ -744,7 +791,7 @@ int compute_units() {
 // How far a call's tiles are split: as many workgroups as fill the chip, tiles of a workgroup not fewer than pay for the
 // join, which is a launch of its own.
 Shape shape_of(const entro_cache *c, const entro_cache_table *t, const entro_cache_query *q) {
-    Shape s = {false, 1, 1, 16, q->max_new < 1 ? 1 : q->max_new > 65535 ? 65535 : q->max_new, 0};
+    Shape s = {false, 1, 1, 1, q->max_new < 1 ? 1 : q->max_new > 65535 ? 65535 : q->max_new, 0};
     const uint32_t width = entro_cache_width(c->head_dim);
     const uint64_t rows = uint64_t{q->max_new} * (q->q_heads / c->kv_heads);
     uint64_t len = q->max_len;
@@ -771,13 +818,14 @@ Shape shape_of(const entro_cache *c, const entro_cache_table *t, const entro_cac
         want = cus * 2 / units;
         can = tiles < 24 ? 1 : tiles / 8;
     } else {
+        // two workgroups a compute unit (64 tokens of 32 heads over 8192: 49 us, 1024 over 16384: 487 us in two pieces, 516 in one, 513 in four)
         want = (cus * 2 + groups - 1) / groups;
-        can = (tiles + s.least - 1) / s.least;
+        can = tiles / 8;
     }
     s.splits = static_cast<uint32_t>(want < can ? want : can);
     if (s.splits < 1) s.splits = 1;
-    if (s.splits > kMostSplits) s.splits = kMostSplits;
-    if (!s.many && tiles) s.least = static_cast<uint32_t>((tiles + s.splits - 1) / s.splits);
+    if (s.splits > (s.many ? 64 : kMostSplits)) s.splits = s.many ? 64 : kMostSplits;
+    if (tiles) s.least = static_cast<uint32_t>((tiles + s.splits - 1) / s.splits);
     if (s.splits > 1) s.bytes = uint64_t{q->tokens} * q->q_heads * s.splits * (width + 1) * 4;
     return s;
 }
@@ -790,8 +838,10 @@ void launch_width(const Pool &p, const Query &a, const Shape &s, hipStream_t st)
     else
         hipLaunchKernelGGL((k_attend_many<W, T>), dim3(units * s.row_tiles), dim3(kWG), 0, st, p, a, s.row_tiles);
     if (a.splits > 1) {
-        const dim3 join(p.seqs * a.q_heads, s.join_rows);
-        hipLaunchKernelGGL((k_attend_join<W, T>), join, dim3(kWG), 0, st, p, a, s.many ? kManyRows : 16u);
+        if (s.many)
+            hipLaunchKernelGGL((k_attend_join_rows<W, T>), dim3((p.seqs * a.q_heads + kWG / 64 - 1) / (kWG / 64), s.join_rows), dim3(kWG), 0, st, p, a);
+        else
+            hipLaunchKernelGGL((k_attend_join<W, T>), dim3(p.seqs * a.q_heads, s.join_rows), dim3(kWG), 0, st, p, a);
     }
 }
 
