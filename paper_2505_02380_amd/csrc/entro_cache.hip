@@ -255,6 +255,11 @@ __global__ __launch_bounds__(kWG) void k_append(Pool p, Rows r, uint32_t blocks,
                     write_patch(p, unit, a, b, v[kv], old[kv], grid[kv], kv);
                 }
             }
+            // everybody has read the old scales
+            if (LANES > 64)
+                __syncthreads();
+            else
+                __builtin_amdgcn_wave_barrier();
             if (lane == 0) p.k_scale[unit] = grid[0].scale, p.v_scale[unit] = grid[1].scale;
         });
     }

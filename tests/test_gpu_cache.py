@@ -316,6 +316,22 @@ def test_append_and_read_against_the_definition(case):
             assert torch.equal(got.cpu(), torch.from_numpy(want.astype(np.float32)).to(TYPES[out_kind]))
 
 
+@pytest.mark.parametrize("kind,heads,page,dim", [("bf16", 8, 64, 128), ("f32", 2, 256, 256), ("bf16", 5, 32, 80)])
+def test_append_token_by_token_with_a_scale_that_rises(kind, heads, page, dim):
+    """Every token of a block raises its scale: code for code, in blocks that several wavefronts share."""
+    rng = np.random.default_rng(20)
+    seqs, tokens = 6, min(page, 64)
+    pool, table = make(rng, seqs, [page] * seqs, heads, dim, page)
+    cache, table_dev, start = cache_of(pool), dev(table), starts([1] * seqs)
+    for n in range(1, tokens + 1):
+        k, v = (rounded(rng.standard_normal((seqs, heads, dim)) * 1.1 ** n, kind) for _ in "kv")
+        k[..., 0], v[..., 1] = rounded(np.array(6 * 1.1 ** n), kind), rounded(np.array(-7 * 1.1 ** n), kind)
+        E.entro_cache_append(cache, E.CacheTable(table_dev, ints([n] * seqs)), E.CacheRows(dev(k).to(TYPES[kind]), dev(v).to(TYPES[kind]), ints(start), 1))
+        near = ref.append(pool, table, [n] * seqs, k, v, start)
+        compare_pool(pool, cache, near, np.unique(table))
+        pool.k, pool.v = cache.k.cpu().numpy(), cache.v.cpu().numpy()
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
 def test_append_takes_values_that_are_no_numbers(kind):
     """NaN, infinities, a block of zeros, values too small for a scale of their own, the largest finite ones."""
