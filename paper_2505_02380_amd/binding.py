@@ -547,6 +547,12 @@ def _ints(x, n: Optional[int], what: str):
     return x.data_ptr()
 
 
+def _device_of(*tensors):
+    """The device of all tensors (None: left out), or None where they lie on several."""
+    devices = {x.device for x in tensors if x is not None}
+    return devices.pop() if len(devices) == 1 else None
+
+
 class Cache:
     """A pool of pages (include/entro.h has the layouts): the tensors, and the descriptor that the calls take."""
 
@@ -562,7 +568,7 @@ class Cache:
         for x in (k_scale, v_scale):
             _need(tuple(x.shape) == (layers, pages, heads) and x.dtype == torch.float32 and x.is_contiguous(),
                   "scales are float32 [layers][pages][kv_heads]")
-        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.k, self.v, self.k_scale, self.v_scale, self.device = k, v, k_scale, v_scale, _device_of(k, v, k_scale, v_scale)
         self.layers, self.pages, self.kv_heads, self.page_tokens, self.head_dim, self.width = layers, pages, heads, page_tokens, head_dim, width
         self.c = CCache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), layers, pages, page_tokens, heads, head_dim, 0)
 
@@ -583,7 +589,7 @@ class CacheTable:
 
     def __init__(self, slots, lengths):
         _need(slots.dim() == 2, "slots is [seqs][slots]")
-        self.slots, self.lengths = slots, lengths
+        self.slots, self.lengths, self.device = slots, lengths, _device_of(slots, lengths)
         self.c = CCacheTable(_ints(slots, None, "slots"), _ints(lengths, slots.shape[0], "lengths"), slots.shape[0], slots.shape[1])
 
     @classmethod
@@ -598,12 +604,17 @@ def _row_strides(x, what: str):
     return x.stride(0), x.stride(1)
 
 
+def _own_places(x) -> bool:
+    """Whether a tensor that a call writes is none that was expanded."""
+    return not any(n > 1 and s == 0 for n, s in zip(x.shape, x.stride()))
+
+
 class CacheRows:
     """Keys and values [tokens][kv_heads][head_dim] of the last tokens of sequences; start: int32 [seqs + 1]."""
 
     def __init__(self, k, v, start, max_new: int, layer: int = 0):
         _need(k.shape == v.shape and k.dtype == v.dtype, "k and v have one shape and type")
-        self.k, self.v, self.start = k, v, start
+        self.k, self.v, self.start, self.device = k, v, start, _device_of(k, v, start)
         self.c = CCacheRows(k.data_ptr(), v.data_ptr(), *_row_strides(k, "k"), *_row_strides(v, "v"), _ints(start, None, "start"),
                             k.shape[0], max_new, _rows_type(k, "k"), layer)
 
@@ -618,16 +629,17 @@ class CacheQuery:
         _need(q.shape == out.shape and q.dtype == out.dtype, "q and out have one shape and type")
         _need(lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == tuple(q.shape[:2])),
               "lse is float32 [tokens][q_heads]")
-        _need(q.dim() == 3 and not any(n > 1 and s == 0 for n, s in zip(out.shape, out.stride())), "out's elements have places of their own")
-        self.q, self.out, self.start, self.lse = q, out, start, lse
+        _need(q.dim() == 3 and _own_places(out), "out's elements have places of their own")
+        self.q, self.out, self.start, self.lse, self.device = q, out, start, lse, _device_of(q, out, start, lse)
         self.c = CCacheQuery(q.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(), *_row_strides(q, "q"),
                              *_row_strides(out, "out"), _ints(start, None, "start"), q.shape[0], max_new, max_len, q.shape[1],
                              _rows_type(q, "q"), layer, window, sinks, q.shape[2] ** -0.5 if scale is None else scale, 0)
 
 
-def _on_gpu(*tensors):
-    device = tensors[0].device
-    _need(device.type == "cuda" and all(t.device == device for t in tensors), "all tensors of a call lie on one GPU")
+def _on_gpu(cache: Cache, *given):
+    """Every tensor whose address a call takes lies on the pool's GPU; given: descriptors, tensors, None for what is left out."""
+    device = cache.device
+    _need(device is not None and device.type == "cuda" and all(x is None or x.device == device for x in given), "all tensors of a call lie on one GPU")
 
 
 def _same_heads(cache: Cache, table: CacheTable, x, start):
@@ -638,14 +650,15 @@ def _same_heads(cache: Cache, table: CacheTable, x, start):
 def entro_cache_append(cache: Cache, table: CacheTable, rows: CacheRows, stream=None):
     _same_heads(cache, table, rows.k, rows.start)
     _need(rows.k.shape[1] == cache.kv_heads, f"rows have {cache.kv_heads} heads")
-    _on_gpu(cache.k, table.slots, rows.k, rows.v, rows.start)
+    _on_gpu(cache, table, rows)
     _check(lib().entro_cache_append(C.byref(cache.c), C.byref(table.c), C.byref(rows.c), _stream_ptr(stream)), "entro_cache_append")
 
 
 def entro_cache_read(cache: Cache, table: CacheTable, rows: CacheRows, stream=None):
     _same_heads(cache, table, rows.k, rows.start)
+    _need(_own_places(rows.k) and _own_places(rows.v), "the elements of k and v that are written have places of their own")
     _need(rows.k.shape[1] == cache.kv_heads, f"rows have {cache.kv_heads} heads")
-    _on_gpu(cache.k, table.slots, rows.k, rows.v, rows.start)
+    _on_gpu(cache, table, rows)
     _check(lib().entro_cache_read(C.byref(cache.c), C.byref(table.c), C.byref(rows.c), _stream_ptr(stream)), "entro_cache_read")
 
 
@@ -660,7 +673,7 @@ def _workspace(ws):
 
 def entro_cache_attend(cache: Cache, table: CacheTable, query: CacheQuery, workspace=None, stream=None):
     _same_heads(cache, table, query.q, query.start)
-    _on_gpu(cache.k, table.slots, query.q, query.out, query.start)
+    _on_gpu(cache, table, query, workspace)
     _check(lib().entro_cache_attend(C.byref(cache.c), C.byref(table.c), C.byref(query.c), *_workspace(workspace), _stream_ptr(stream)),
            "entro_cache_attend")
 
@@ -673,14 +686,14 @@ def entro_cache_regroup(cache: Cache, table: CacheTable, following: CacheTable, 
                         window: int = 0, sinks: int = 0, stream=None):
     """`following` receives the table of the next step; status: int32 device tensor of 4 (entro_cache_status reads its first word)."""
     n = following.c.seqs
-    _on_gpu(cache.k, table.slots, following.slots, status, workspace)
+    _on_gpu(cache, table, following, status, workspace, parent, grow)
     _check(lib().entro_cache_regroup(C.byref(cache.c), C.byref(table.c), None if parent is None else _ints(parent, n, "parent"),
                                      None if grow is None else _ints(grow, n, "grow"), window, sinks, C.byref(following.c),
                                      _ints(status, 4, "status"), *_workspace(workspace), _stream_ptr(stream)), "entro_cache_regroup")
 
 
 def entro_cache_compact(cache: Cache, table: CacheTable, following: CacheTable, status, workspace, stream=None):
-    _on_gpu(cache.k, table.slots, following.slots, status, workspace)
+    _on_gpu(cache, table, following, status, workspace)
     _check(lib().entro_cache_compact(C.byref(cache.c), C.byref(table.c), C.byref(following.c), _ints(status, 4, "status"),
                                      *_workspace(workspace), _stream_ptr(stream)), "entro_cache_compact")
 

@@ -200,3 +200,69 @@ def test_the_reference_s_grid_by_hand():
     ref.append(pool, np.zeros((1, 1), int), [2], k[1:], k[1:], [0, 1])
     assert pool.k[0, 0, 0, :2, :2].tolist() == [[192, 103], [255, 129]]         # 63.5 is even at 64; -25; 127; 1
     assert np.isclose(pool.k_scale[0, 0, 0], 0.02)
+
+
+class Placed(torch.Tensor):
+    """A tensor in host memory that says it lies on a GPU."""
+    device = property(lambda self: torch.device("cuda:0"))
+
+
+@pytest.fixture
+def calls_made(monkeypatch):
+    """Names of the C calls that the binding makes; none of them runs."""
+    made = []
+
+    class Library:
+        def __getattr__(self, name):
+            return getattr(real, name) if name.endswith(("_bytes", "_width")) else lambda *args: made.append(name) or 0
+    real = B.lib()
+    monkeypatch.setattr(B, "lib", lambda: Library())
+    monkeypatch.setattr(B, "_stream_ptr", lambda stream: None)
+    return made
+
+
+OF_EVERY_CALL = ["pool.k", "pool.v", "pool.k_scale", "pool.v_scale", "slots", "lengths"]
+
+
+@pytest.mark.parametrize("call,tensor", [
+    (call, tensor) for call, more in [("append", ["k", "v", "start"]), ("read", ["k", "v", "start"]), ("attend", ["q", "out", "lse", "start", "workspace"]),
+                                      ("regroup", ["next.slots", "next.lengths", "status", "workspace", "parent", "grow"]),
+                                      ("compact", ["next.slots", "next.lengths", "status", "workspace"])]
+    for tensor in [None] + OF_EVERY_CALL + more])
+def test_calls_refuse_any_one_tensor_in_host_memory(calls_made, call, tensor):
+    """Everything on the GPU but one tensor: the call is not made. (With all of them there it is.)"""
+    def at(name, *shape, dtype=torch.int32):
+        x = torch.zeros(*shape, dtype=dtype)
+        return x if name == tensor else x.as_subclass(Placed)
+    pool = [at("pool.k", 1, 4, 2, 16, 64, dtype=torch.uint8), at("pool.v", 1, 4, 2, 64, 16, dtype=torch.uint8)]
+    cache = E.Cache(*pool, *(at(name, 1, 4, 2, dtype=torch.float32) for name in ("pool.k_scale", "pool.v_scale")), 16, 40)
+    table = E.CacheTable(at("slots", 3, 5), at("lengths", 3))
+    following, status = E.CacheTable(at("next.slots", 3, 5), at("next.lengths", 3)), at("status", 4)
+    start, room = at("start", 4), at("workspace", 1 << 16, dtype=torch.uint8)
+    rows = [at(name, 7, 2, 40, dtype=torch.float32) for name in "kv"]
+    run = {"append": lambda: E.entro_cache_append(cache, table, E.CacheRows(*rows, start, 1)),
+           "read": lambda: E.entro_cache_read(cache, table, E.CacheRows(*rows, start, 1)),
+           "attend": lambda: E.entro_cache_attend(cache, table, E.CacheQuery(*(at(n, 7, 4, 40, dtype=torch.float32) for n in ("q", "out")), start, 1, 9,
+                                                                             lse=at("lse", 7, 4, dtype=torch.float32)), room),
+           "regroup": lambda: E.entro_cache_regroup(cache, table, following, status, room, parent=at("parent", 3), grow=at("grow", 3)),
+           "compact": lambda: E.entro_cache_compact(cache, table, following, status, room)}[call]
+    if tensor is None:
+        run()
+        assert calls_made == ["entro_cache_" + call]
+    else:
+        with pytest.raises(ValueError, match="one GPU"):
+            run()
+        assert calls_made == []
+
+
+def test_read_refuses_rows_that_share_their_places(calls_made):
+    placed = lambda *shape, dtype=torch.int32: torch.zeros(*shape, dtype=dtype).as_subclass(Placed)  # noqa: E731
+    s = placed(1, 4, 2, dtype=torch.float32)
+    cache = E.Cache(placed(1, 4, 2, 16, 64, dtype=torch.uint8), placed(1, 4, 2, 64, 16, dtype=torch.uint8), s, s, 16, 40)
+    table, start, x = E.CacheTable(placed(3, 5), placed(3)), placed(4), placed(7, 2, 40, dtype=torch.float32)
+    for shared in (x[:1].expand(7, 2, 40), x[:, :1].expand(7, 2, 40)):
+        for k, v in ((x, shared), (shared, x)):
+            with pytest.raises(ValueError, match="places of their own"):
+                E.entro_cache_read(cache, table, E.CacheRows(k, v, start, 1))
+            E.entro_cache_append(cache, table, E.CacheRows(k, v, start, 1))         # rows that are only read may
+    assert calls_made == ["entro_cache_append"] * 4
