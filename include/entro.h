@@ -415,7 +415,12 @@ entro_status entro_encode_device_status(uint32_t status_word);
  *     and seen by no query (entro_cache_attend).
  *   - max_new and max_len bound how many rows and tokens a sequence has.  They size
  *     the launch and choose between kernels; results do not depend on them beyond
- *     the order of sums, and they may be exceeded.
+ *     the order of sums.  They may be exceeded, and may be any number where no
+ *     bound is known (then the rows and slots there are bound the launch).
+ *   - Sizes that no launch takes are ENTRO_ERR_SIZE: sequences times kv_heads of 2^31
+ *     and more (of 2^24 and more for entro_cache_attend, with the sequences rounded up
+ *     to a multiple of 8 where there are 8 or more), tokens times q_heads of 2^31
+ *     and more, 65536 and more sequences in entro_cache_regroup and entro_cache_compact.
  *   - Tables, lengths and starts are device memory that the kernels read, so that
  *     a captured HIP graph can be replayed as they change.  All calls only enqueue
  *     kernels.

@@ -31,6 +31,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr uint32_t kMostSplits = kWG;          // the join has a lane for each
 constexpr uint32_t kManyRows = 128;            // of a workgroup for many rows
+constexpr uint64_t kMostGroups = (1u << 24) - 1;   // workgroups of a launch: it has less than 2^32 lanes along x
 constexpr int kTile = 64;                      // tokens a wavefront takes at a time
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -788,21 +789,26 @@ int compute_units() {
     return cus > 0 ? cus : 256;
 }
 
+// Sequences and key heads of k_attend_few's grid, which takes eight sequences at a time.
+uint64_t units_of(uint32_t seqs, uint32_t kv_heads) { return (seqs < 8 ? seqs : (uint64_t{seqs} + 7) / 8 * 8) * kv_heads; }
+
 // How far a call's tiles are split: as many workgroups as fill the chip, tiles of a workgroup not fewer than pay for the
-// join, which is a launch of its own.
+// join, which is a launch of its own. A sequence has no more new tokens than there are rows and no more tokens than slots, whatever
+// the hints say, and the kernels' own loops cover what a grid of kMostGroups does not.
 Shape shape_of(const entro_cache *c, const entro_cache_table *t, const entro_cache_query *q) {
-    Shape s = {false, 1, 1, 1, q->max_new < 1 ? 1 : q->max_new > 65535 ? 65535 : q->max_new, 0};
+    const uint32_t max_new = q->max_new < q->tokens ? q->max_new : q->tokens;
+    Shape s = {false, 1, 1, 1, max_new < 1 ? 1 : max_new > 65535 ? 65535 : max_new, 0};
     const uint32_t width = entro_cache_width(c->head_dim);
-    const uint64_t rows = uint64_t{q->max_new} * (q->q_heads / c->kv_heads);
-    uint64_t len = q->max_len;
-    if (q->window && len > uint64_t{q->window} + q->sinks + q->max_new + 2 * kTile) len = uint64_t{q->window} + q->sinks + q->max_new + 2 * kTile;
+    const uint64_t rows = uint64_t{max_new} * (q->q_heads / c->kv_heads), room = uint64_t{t->stride} * c->page_tokens;
+    uint64_t len = q->max_len < room ? q->max_len : room;
+    if (q->window && len > uint64_t{q->window} + q->sinks + max_new + 2 * kTile) len = uint64_t{q->window} + q->sinks + max_new + 2 * kTile;
     const uint64_t tiles = (len + kTile - 1) / kTile, units = uint64_t{t->seqs} * c->kv_heads;
     uint64_t groups = units;
     // up to 32 rows in groups of 16, one after the other (32 and 48 rows of 128 dimensions over 4096 tokens of 8 sequences: 45 and 66 us,
     // by the kernel for many 56 and 61)
     if (rows > 32) {
         s.many = true;
-        const uint64_t row_tiles = (rows + kManyRows - 1) / kManyRows, most = 0x3fffffffull / units;
+        const uint64_t row_tiles = (rows + kManyRows - 1) / kManyRows, most = kMostGroups / units;
         s.row_tiles = static_cast<uint32_t>(row_tiles < most ? row_tiles : (most ? most : 1));
         groups *= s.row_tiles;
     }
@@ -823,8 +829,10 @@ Shape shape_of(const entro_cache *c, const entro_cache_table *t, const entro_cac
         can = tiles / 8;
     }
     s.splits = static_cast<uint32_t>(want < can ? want : can);
-    if (s.splits < 1) s.splits = 1;
+    const uint64_t fit = uint64_t{t->seqs} * q->q_heads > kMostGroups ? 1 : kMostGroups / (units_of(t->seqs, c->kv_heads) * s.row_tiles);
     if (s.splits > (s.many ? 64 : kMostSplits)) s.splits = s.many ? 64 : kMostSplits;
+    if (s.splits > fit) s.splits = static_cast<uint32_t>(fit);
+    if (s.splits < 1) s.splits = 1;
     if (tiles) s.least = static_cast<uint32_t>((tiles + s.splits - 1) / s.splits);
     if (s.splits > 1) s.bytes = uint64_t{q->tokens} * q->q_heads * s.splits * (width + 1) * 4;
     return s;
@@ -832,11 +840,10 @@ Shape shape_of(const entro_cache *c, const entro_cache_table *t, const entro_cac
 
 template <int W, typename T>
 void launch_width(const Pool &p, const Query &a, const Shape &s, hipStream_t st) {
-    const uint32_t units = p.seqs * p.kv_heads * a.splits;
     if (!s.many)
-        hipLaunchKernelGGL((k_attend_few<W, T>), dim3(p.seqs < 8 ? units : (p.seqs + 7) / 8 * 8 * p.kv_heads * a.splits), dim3(kWG), 0, st, p, a);
+        hipLaunchKernelGGL((k_attend_few<W, T>), dim3(static_cast<uint32_t>(units_of(p.seqs, p.kv_heads)) * a.splits), dim3(kWG), 0, st, p, a);
     else
-        hipLaunchKernelGGL((k_attend_many<W, T>), dim3(units * s.row_tiles), dim3(kWG), 0, st, p, a, s.row_tiles);
+        hipLaunchKernelGGL((k_attend_many<W, T>), dim3(p.seqs * p.kv_heads * a.splits * s.row_tiles), dim3(kWG), 0, st, p, a, s.row_tiles);
     if (a.splits > 1) {
         if (s.many)
             hipLaunchKernelGGL((k_attend_join_rows<W, T>), dim3((p.seqs * a.q_heads + kWG / 64 - 1) / (kWG / 64), s.join_rows), dim3(kWG), 0, st, p, a);
@@ -871,15 +878,13 @@ entro_status entro_cache_attend(const entro_cache *c, const entro_cache_table *t
     if (const entro_status s = check_table(t)) return s;
     if (const entro_status s = check_query(c, q)) return s;
     if (q->tokens == 0) return ENTRO_OK;
+    if (units_of(t->seqs, c->kv_heads) > kMostGroups || uint64_t{q->tokens} * q->q_heads > 0x7fffffffull) return ENTRO_ERR_SIZE;
     const Shape shape = shape_of(c, t, q);
     if (shape.bytes) {
         if (!workspace) return ENTRO_ERR_NULL;
         if (!aligned16(workspace)) return ENTRO_ERR_ALIGN;
         if (workspace_bytes < shape.bytes) return ENTRO_ERR_CAPACITY;
     }
-    if (uint64_t{t->seqs} * c->kv_heads * shape.splits * shape.row_tiles > 0x7fffffffull ||
-        uint64_t{t->seqs} * q->q_heads > 0x7fffffffull || uint64_t{q->tokens} * q->q_heads > 0x7fffffffull)
-        return ENTRO_ERR_SIZE;
     const Pool p = pool_of(c, t, q->layer);
     const bool aligned = ((q->q_token_stride | q->q_head_stride) & 7u) == 0;
     float *part_o = static_cast<float *>(workspace), *part_lse = part_o + uint64_t{q->tokens} * q->q_heads * shape.splits * p.width;

@@ -738,15 +738,16 @@ void launch_lanes(const Pool &p, const Rows &r, uint32_t blocks, uint32_t work, 
         hipLaunchKernelGGL((k_read<T, LANES>), dim3(grid), dim3(kWG), 0, st, p, r, blocks, work);
 }
 
-// entro_cache_append and entro_cache_read; false if there are too many blocks.
+// entro_cache_append and entro_cache_read; false if there are too many sequences and heads.
 bool launch_rows(const entro_cache *c, const entro_cache_table *t, const entro_cache_rows *rows, hipStream_t st, bool write) {
     const Pool p = pool_of(c, t, rows->layer);
     const Rows r = rows_of(rows);
-    // as many blocks as the most rows can touch, and no more than there are slots
-    const uint64_t touch = (uint64_t{rows->max_new} + c->page_tokens + (rows->max_new ? 0 : 1) - 2) / c->page_tokens + 1;
-    const uint32_t blocks = static_cast<uint32_t>(touch < t->stride ? touch : t->stride);
-    const uint64_t work = uint64_t{blocks} * c->kv_heads * t->seqs;
-    if (work > 0x7fffffffull) return false;
+    // as many blocks as the most rows can touch, and no more than there are slots; the kernels' own loops cover what 31 bits do not
+    const uint64_t most_new = rows->max_new < rows->tokens ? rows->max_new : rows->tokens, units = uint64_t{c->kv_heads} * t->seqs, fit = 0x7fffffffull / units;
+    const uint64_t touch = (most_new + c->page_tokens + (most_new ? 0 : 1) - 2) / c->page_tokens + 1, wanted = touch < t->stride ? touch : t->stride;
+    const uint32_t blocks = static_cast<uint32_t>(wanted < fit ? wanted : fit);
+    const uint64_t work = blocks * units;
+    if (work == 0) return false;
     const bool few = ((c->head_dim + 7) / 8) * (c->page_tokens / 4) <= 64;
     const uint32_t n = static_cast<uint32_t>(work);
     if (rows->type == ENTRO_F32)

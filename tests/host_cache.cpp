@@ -24,14 +24,18 @@ struct dim3 {
 typedef int hipError_t;
 typedef void *hipStream_t;
 constexpr hipError_t hipSuccess = 0;
+constexpr int hipDeviceAttributeMultiprocessorCount = 1;
 inline hipError_t hipGetLastError() { return hipSuccess; }
+inline hipError_t hipGetDevice(int *device) { return *device = 0, hipSuccess; }
+inline hipError_t hipDeviceGetAttribute(int *value, int, int) { return *value = 256, hipSuccess; }
 
 namespace {
 
 thread_local struct { uint32_t x; } threadIdx;
 thread_local dim3 blockIdx(0, 0);
 dim3 gridDim(0, 0);
-std::vector<dim3> launches;                      // the grids of the last call
+std::vector<uint64_t> launches;                  // lanes along x, workgroups along x and y of every launch
+bool only_noted;                                 // launches are noted, nothing runs
 
 constexpr uint32_t kMostWaves = 16;
 uint32_t waves, first_wave;
@@ -114,7 +118,8 @@ uint32_t perm(uint32_t a, uint32_t b, uint32_t select) {
 
 template <typename F>
 void host_launch(dim3 grid, dim3 block, F kernel) {
-    launches.push_back(grid);
+    launches.insert(launches.end(), {uint64_t{grid.x} * block.x, grid.x, grid.y});
+    if (only_noted) return;
     gridDim = grid;
     waves = block.x / 64;
     for (uint32_t i = 0; i < waves; ++i) wave_meets[i] = std::make_unique<std::barrier<>>(64);
@@ -135,6 +140,12 @@ void host_launch(dim3 grid, dim3 block, F kernel) {
         }
 }
 
+// Attention's matrix instructions have no host form: its launches are only noted.
+template <int W, typename T, typename... A> void k_attend_few(const A &...) {}
+template <int W, typename T, typename... A> void k_attend_many(const A &...) {}
+template <int W, typename T, typename... A> void k_attend_join(const A &...) {}
+template <int W, typename T, typename... A> void k_attend_join_rows(const A &...) {}
+
 }  // namespace
 
 #define hipLaunchKernelGGL(kernel, grid, block, lds, stream, ...) host_launch(grid, block, [&] { kernel(__VA_ARGS__); })
@@ -145,3 +156,14 @@ void entro_detail_note_hip_error(const char *, int) {}
 
 // The wavefront that runs first from here on.
 extern "C" void host_first_wave(uint32_t wave) { first_wave = wave; }
+
+// From here on launches are only noted.
+extern "C" void host_only_note(int yes) { only_noted = yes != 0; }
+
+// Lanes along x, workgroups along x and y of the launches since the last time, `most` numbers at most; returns how many.
+extern "C" int host_launches(uint64_t *out, int most) {
+    const int n = std::min(most, static_cast<int>(launches.size()));
+    std::copy_n(launches.begin(), n, out);
+    launches.clear();
+    return n;
+}

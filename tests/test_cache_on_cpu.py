@@ -31,9 +31,19 @@ def compiled(build, main, text):
 
 @pytest.fixture(scope="module")
 def host(tmp_path_factory):
-    L = compiled(tmp_path_factory.mktemp("host_cache"), "host_cache.cpp", source("entro_cache.h") + source("entro_cache.hip").replace('#include "entro_cache.h"', ""))
-    for call in (L.entro_cache_append, L.entro_cache_read):
-        call.argtypes = [C.POINTER(B.CCache), C.POINTER(B.CCacheTable), C.POINTER(B.CCacheRows), C.c_void_p]
+    include, attend = '#include "entro_cache.h"', source("entro_attend.hip")
+
+    def part(begin, end=None):
+        at = attend.index(begin)
+        return attend[at: attend.index(end, at) if end else None]
+
+    L = compiled(tmp_path_factory.mktemp("host_cache"), "host_cache.cpp", "\n".join([
+        source("entro_cache.h"), source("entro_cache.hip").replace(include, ""), "namespace {", part("struct Query {", "typedef"),
+        part("constexpr uint32_t kMostSplits", "constexpr float"), part("entro_status check_query_sizes")]))
+    for name in ("append", "read", "attend"):
+        call, twin = getattr(L, "entro_cache_" + name), getattr(B.lib(), "entro_cache_" + name)
+        call.argtypes = twin.argtypes
+    L.entro_cache_attend_workspace_bytes.restype = C.c_uint64
     return L
 
 
@@ -89,3 +99,48 @@ def test_append_moves_older_codes_whichever_wavefront_comes_first(host, first_wa
             away = getattr(pool, name) != getattr(twin, name)
             assert not np.any(away & ~near[name]), (n, np.argwhere(away & ~near[name])[:4])
         twin.k[...], twin.v[...] = pool.k, pool.v
+
+
+def launched(host):
+    out = (C.c_uint64 * 3000)()
+    n = host.host_launches(out, 3000)
+    return [tuple(out[i: i + 3]) for i in range(0, n, 3)]
+
+
+HINTS = [1, 5, 1000, 1 << 20, (1 << 31) - 1, (1 << 32) - 1]
+
+
+@pytest.mark.parametrize("seqs,stride,kv_heads,group,tokens", [
+    (64, 128, 8, 4, 64), (64, 128, 8, 4, 3000), (1, 8, 1, 1, 1), (1, 1 << 20, 8, 8, 1 << 20), (4096, 4096, 32, 1, 4096), (60000, 30000, 64, 1, 60000), (7, 100, 2, 16, 40)])
+def test_hints_of_any_size_make_launches_that_a_gpu_takes(host, seqs, stride, kv_heads, group, tokens):
+    """Hints bound the work and nothing else: whatever they say, a launch has less than 2^32 lanes along x and less than 2^16 workgroups along
+    y, and the call succeeds."""
+    at = 1 << 16
+    cache, table = B.CCache(at, at, at, at, 1, 1 << 20, 64, kv_heads, 64, 0), B.CCacheTable(at, at, seqs, stride)
+    row = kv_heads * 64
+    host.host_only_note(1)
+    launched(host)
+    for max_new in HINTS:
+        rows = B.CCacheRows(at, at, row, 64, row, 64, at, tokens, max_new, E.ENTRO_BF16, 0)
+        for call in (host.entro_cache_append, host.entro_cache_read):
+            assert call(C.byref(cache), C.byref(table), C.byref(rows), None) == B.ENTRO_OK
+        for max_len in HINTS:
+            for window in (0, 1, 1 << 20):
+                query = B.CCacheQuery(at, at, at, row * group, 64, row * group, 64, at, tokens, max_new, max_len, kv_heads * group, E.ENTRO_BF16, 0, window, 4, 0.1, 0)
+                need = host.entro_cache_attend_workspace_bytes(C.byref(cache), C.byref(table), C.byref(query))
+                assert host.entro_cache_attend(C.byref(cache), C.byref(table), C.byref(query), at, need, None) == B.ENTRO_OK
+        for lanes, x, y in launched(host):
+            assert 0 < lanes < 1 << 32 and 0 < x and 0 < y < 1 << 16, (max_new, lanes, x, y)
+    host.host_only_note(0)
+
+
+def test_attend_refuses_more_sequences_and_heads_than_a_launch_takes(host):
+    at = 1 << 16
+    cache, table = B.CCache(at, at, at, at, 1, 100, 16, 64, 64, 0), B.CCacheTable(at, at, 1 << 18, 1)
+    query = B.CCacheQuery(at, at, None, 64, 64, 64, 64, at, 5, 1, 16, 64, E.ENTRO_BF16, 0, 0, 0, 0.1, 0)
+    host.host_only_note(1)
+    launched(host)
+    assert host.entro_cache_attend(C.byref(cache), C.byref(table), C.byref(query), None, 0, None) == B.ENTRO_ERR_SIZE and not launched(host)
+    table.seqs = (1 << 18) - 8
+    assert host.entro_cache_attend(C.byref(cache), C.byref(table), C.byref(query), None, 0, None) == B.ENTRO_OK and len(launched(host)) == 1
+    host.host_only_note(0)

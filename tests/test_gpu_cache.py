@@ -230,6 +230,34 @@ def test_attend_looks_at_no_page_without_seen_tokens(kind, new):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [[1] * 9, [3, 0, 50, 1, 1, 20, 1, 1, 2]])
+def test_calls_with_hints_that_bound_nothing(kind, new):
+    """The largest numbers as hints, which no launch could follow, in append, read and attend: the results of the definition."""
+    rng = np.random.default_rng(21)
+    lengths, heads, dim, page = [90, 33, 200, 1, 64, 40, 7, 300, 16], 4, 64, 16
+    pool, table = make(rng, 9, lengths, heads, dim, page, slots=40)
+    scales(rng, pool, table)
+    start = starts(new)
+    k, v = (rounded(rng.standard_normal((start[-1], heads, dim)), kind) for _ in "kv")
+    cache, t = cache_of(pool), E.CacheTable(dev(table), ints(lengths))
+    named = np.unique(table[table >= 0])
+    for hint in ((1 << 31) - 1, (1 << 32) - 1):
+        E.entro_cache_append(cache, t, E.CacheRows(dev(k).to(TYPES[kind]), dev(v).to(TYPES[kind]), ints(start), hint))
+        near = ref.append(pool, table, lengths, k, v, start)
+        torch.cuda.synchronize()
+        compare_pool(pool, cache, near, named)
+        pool.k, pool.v = cache.k.cpu().numpy(), cache.v.cpu().numpy()
+        back = [torch.full((start[-1], heads, dim), 7.0, dtype=TYPES[kind], device=DEV) for _ in "kv"]
+        E.entro_cache_read(cache, t, E.CacheRows(*back, ints(start), hint))
+        for got, want in zip(back, ref.read(pool, table, lengths, start, start[-1])):
+            assert torch.equal(got.cpu(), torch.from_numpy(want.astype(np.float32)).to(TYPES[kind]))
+        q = rounded(rng.standard_normal((start[-1], 4 * heads, dim)) * 2, kind)
+        for window in (0, 50):
+            out, lse = run_attend(cache, table, lengths, q, start, kind, window=window, sinks=3, max_new=hint, max_len=hint)
+            check_attend(pool, table, lengths, q, start, kind, out, lse, dim ** -0.5, window, 3)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
 @pytest.mark.parametrize("dim,lengths,new,group", [(256, [2100, 30], [1, 1], 2), (192, [1700], [1], 5), (256, [1300], [40], 2), (200, [1800, 900], [17, 3], 8),
                                                    (64, [6300] + [40] * 70, [1] * 71, 1)])
 def test_attend_splits_of_every_width(kind, dim, lengths, new, group):
