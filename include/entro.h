@@ -416,7 +416,7 @@ entro_status entro_encode_device_status(uint32_t status_word);
  *   - max_new and max_len bound how many rows and tokens a sequence has.  They size
  *     the launch and choose between kernels; results do not depend on them beyond
  *     the order of sums.  They may be exceeded, and may be any number where no
- *     bound is known (then the rows and slots there are bound the launch).
+ *     bound is known.
  *   - Sizes that no launch takes are ENTRO_ERR_SIZE: sequences times kv_heads of 2^31
  *     and more (of 2^24 and more for entro_cache_attend, with the sequences rounded up
  *     to a multiple of 8 where there are 8 or more), tokens times q_heads of 2^31

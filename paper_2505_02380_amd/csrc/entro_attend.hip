@@ -793,14 +793,14 @@ int compute_units() {
 uint64_t units_of(uint32_t seqs, uint32_t kv_heads) { return (seqs < 8 ? seqs : (uint64_t{seqs} + 7) / 8 * 8) * kv_heads; }
 
 // How far a call's tiles are split: as many workgroups as fill the chip, tiles of a workgroup not fewer than pay for the
-// join, which is a launch of its own. A sequence has no more new tokens than there are rows and no more tokens than slots, whatever
-// the hints say, and the kernels' own loops cover what a grid of kMostGroups does not.
+// join, which is a launch of its own. A sequence has no more new tokens than there are rows, whatever the hint says, and the
+// kernels' own loops cover what a grid of kMostGroups does not.
 Shape shape_of(const entro_cache *c, const entro_cache_table *t, const entro_cache_query *q) {
     const uint32_t max_new = q->max_new < q->tokens ? q->max_new : q->tokens;
     Shape s = {false, 1, 1, 1, max_new < 1 ? 1 : max_new > 65535 ? 65535 : max_new, 0};
     const uint32_t width = entro_cache_width(c->head_dim);
-    const uint64_t rows = uint64_t{max_new} * (q->q_heads / c->kv_heads), room = uint64_t{t->stride} * c->page_tokens;
-    uint64_t len = q->max_len < room ? q->max_len : room;
+    const uint64_t rows = uint64_t{max_new} * (q->q_heads / c->kv_heads);
+    uint64_t len = q->max_len;
     if (q->window && len > uint64_t{q->window} + q->sinks + max_new + 2 * kTile) len = uint64_t{q->window} + q->sinks + max_new + 2 * kTile;
     const uint64_t tiles = (len + kTile - 1) / kTile, units = uint64_t{t->seqs} * c->kv_heads;
     uint64_t groups = units;
