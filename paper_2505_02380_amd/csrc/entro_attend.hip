@@ -33,6 +33,9 @@ constexpr uint32_t kMostSplits = kWG;          // the join has a lane for each
 constexpr uint32_t kManyRows = 128;            // of a workgroup for many rows
 constexpr uint64_t kMostGroups = (1u << 24) - 1;   // workgroups of a launch: it has less than 2^32 lanes along x
 constexpr int kTile = 64;                      // tokens a wavefront takes at a time
+// A row's maximum may have risen by 2^kRise before its sums are brought to a new unit; that unit is 2^kRise times the last maximum, so that no
+// weight is above 1 and sums stay as far from the largest number as those of the definition.
+constexpr float kRise = 8.0f, kUnit = 256.0f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // Four codes c as halves c - 128: 0x6400 + c is 1024 + c, exactly.
@@ -324,15 +327,14 @@ __global__ __launch_bounds__(kWG, W > 128 ? 1 : 2) void k_attend_few(Pool p, Que
             for (int j = 0; j < 4; ++j) top = fmaxf(top, z[t][j]);
         const float scale = top > -INFINITY ? vs : 0.0f;
         top = column_max(top * factor);
-        // sums may stand at 2^8 times their unit before they are brought to a new one
-        if (__any(top > m + 8.0f)) {
+        if (__any(top > m + kRise)) {
             const float now = fmaxf(m, top), by = __builtin_amdgcn_exp2f(m - (now == -INFINITY ? 0.0f : now));
             m = now;
             l *= by;
 #pragma unroll
             for (int d = 0; d < kDims; ++d) o[d] *= by;
         }
-        const float base = m == -INFINITY ? 0.0f : m;
+        const float base = m == -INFINITY ? 0.0f : m + kRise;
         bf16x8 w[2][kWeights];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -375,7 +377,7 @@ __global__ __launch_bounds__(kWG, W > 128 ? 1 : 2) void k_attend_few(Pool p, Que
             const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
             const uint32_t token = static_cast<uint32_t>(s.row) + static_cast<uint32_t>((row0 + r) / a.group);
             const uint32_t q_head = head * a.group + static_cast<uint32_t>((row0 + r) % a.group);
-            const float lse = sum > 0.0f ? base + __builtin_amdgcn_logf(sum) : sum == sum ? -INFINITY : sum;
+            const float lse = sum > 0.0f ? base + __builtin_amdgcn_logf(sum * kUnit) : sum == sum ? -INFINITY : sum;
             const uint64_t at = uint64_t{token} * a.q_heads + q_head;
             for (uint32_t d = d0; d < p.head_dim; d += 16) {
                 float x = 0.0f;
@@ -606,15 +608,14 @@ __global__ __launch_bounds__(kWG, sizeof(T) == 2 && W <= 128 ? 2 : 1) void k_att
                     top = fmaxf(top, most * kf[g]);
                 }
                 top = fmaxf(top, __shfl_xor(top, 32));
-                // sums may stand at 2^8 times their unit before they are brought to a new one
-                if (__any(top > m + 8.0f)) {
+                if (__any(top > m + kRise)) {
                     const float now = fmaxf(m, top), by = __builtin_amdgcn_exp2f(m - (now == -INFINITY ? 0.0f : now));
                     m = now;
                     l *= by;
 #pragma unroll
                     for (int d = 0; d < kDims; ++d) o[d] *= by;
                 }
-                const float base = m == -INFINITY ? 0.0f : m;
+                const float base = m == -INFINITY ? 0.0f : m + kRise;
                 bf16x8 w[4][kWeights];
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {       // 16 tokens
@@ -634,7 +635,7 @@ __global__ __launch_bounds__(kWG, sizeof(T) == 2 && W <= 128 ? 2 : 1) void k_att
         l += __shfl_xor(l, 32);
         if (mine) {
             const float inv = l > 0.0f ? 1.0f / l : 0.0f, base = m == -INFINITY ? 0.0f : m;
-            const float lse = l > 0.0f ? base + __builtin_amdgcn_logf(l) : l == l ? -INFINITY : l;
+            const float lse = l > 0.0f ? base + __builtin_amdgcn_logf(l * kUnit) : l == l ? -INFINITY : l;
             const uint64_t at = uint64_t{my_token} * a.q_heads + my_head;
             T *out = static_cast<T *>(a.out) + my_token * a.out_token_stride + my_head * a.out_head_stride;
             float *part = a.part_o + (at * a.splits + split) * W;

@@ -210,6 +210,32 @@ def test_attend_with_extreme_queries_and_scales(kind, new):
     check_attend(pool, table, lengths, q, start, kind, out, lse, dim ** -0.5)
 
 
+@pytest.mark.parametrize("kind,new", [("bf16", 1), ("f32", 1), ("bf16", 40), ("f32", 40)])
+def test_attend_with_values_near_the_largest_number(kind, new):
+    """Values of 3e38 at one token, whose weight is 2^7 times that of the tokens before it: the result is as large, its sums no larger."""
+    rng = np.random.default_rng(22)
+    lengths, heads, dim, page = [256 + new], 2, 64, 16
+    pool, table = make(rng, 1, lengths, heads, dim, page)
+    scales(rng, pool, table)
+    last = 15                                                             # the block of tokens 240..255
+    for h in range(heads):
+        for slot in range(len(table[0])):
+            codes = pool.at("k", 0, table[0, slot], h)[0]
+            codes[:] = 128
+            pool.k_scale[0, table[0, slot], h] = 7 * np.log(2) / 100
+            if slot == last:
+                codes[0, 0] = 228                                         # a score 7 log 2 above all others, at a q of 1
+                values = pool.at("v", 0, table[0, slot], h)[0]
+                values[:] = 128
+                values[0] = rng.integers(1, 256, dim)
+                pool.v_scale[0, table[0, slot], h] = 3e38 / 127
+    start = starts([new])
+    q = np.zeros((new, 4, dim))
+    q[..., 0] = 1
+    out, lse = run_attend(cache_of(pool), table, lengths, q, start, kind, scale=1.0)
+    check_attend(pool, table, lengths, q, start, kind, out, lse, 1.0)
+
+
 @pytest.mark.parametrize("kind,new", [("bf16", 1), ("f32", 1), ("bf16", 20), ("f32", 70)])
 def test_attend_looks_at_no_page_without_seen_tokens(kind, new):
     """Pages that a table names for tokens to come, and pages that have left the window: their scales may be NaN."""
