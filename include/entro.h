@@ -503,7 +503,8 @@ uint64_t entro_cache_attend_workspace_bytes(const entro_cache *c, const entro_ca
  *   out = sum_j p_j v_j, p = softmax_j(scale * q . k_j), lse = log(sum_j exp(scale * q . k_j)), over the positions j <= i that have a
  *   page and, if window > 0, i - j < window or j < sinks.
  * A query that sees nothing gets out 0 and lse -inf.  Sums are held in fp32.  bf16: q is taken exactly, probabilities
- * keep 16 bits in their product; fp32: q keeps 22 bits, probabilities 24.
+ * keep 16 bits in their product; fp32: q and probabilities keep 24 bits.  (Elements of q below 2^-100 of their row's largest one, and
+ * probabilities below 2^-100 of the largest, may lose bits.)
  * The order of sums depends on sizes, never on the run. */
 entro_status entro_cache_attend(const entro_cache *c, const entro_cache_table *t, const entro_cache_query *q, void *workspace,
                                 uint64_t workspace_bytes, void *hip_stream);

@@ -22,8 +22,6 @@ struct Query {
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef _Float16 half2 __attribute__((ext_vector_type(2)));
-typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -37,20 +35,6 @@ constexpr int kTile = 64;                      // tokens a wavefront takes at a 
 // weight is above 1 and sums stay as far from the largest number as those of the definition.
 constexpr float kRise = 8.0f, kUnit = 256.0f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-
-// Four codes c as halves c - 128: 0x6400 + c is 1024 + c, exactly.
-__device__ inline void codes_to_halves(uint32_t codes, half2 *lo, half2 *hi) {
-    const half2 off = {(_Float16)-1152.0f, (_Float16)-1152.0f};
-    *lo = __builtin_bit_cast(half2, __builtin_amdgcn_perm(0x64646464u, codes, 0x04010400u)) + off;
-    *hi = __builtin_bit_cast(half2, __builtin_amdgcn_perm(0x64646464u, codes, 0x04030402u)) + off;
-}
-
-__device__ inline half8 eight_codes(uint32_t a, uint32_t b) {
-    half2 h[4];
-    codes_to_halves(a, h, h + 1);
-    codes_to_halves(b, h + 2, h + 3);
-    return {h[0].x, h[0].y, h[1].x, h[1].y, h[2].x, h[2].y, h[3].x, h[3].y};
-}
 
 // The upper halves of two fp32 numbers: cut off to bf16.
 __device__ inline uint32_t upper_halves(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); }
@@ -69,10 +53,10 @@ __device__ inline bf16x8 eight_values(uint32_t a, uint32_t b) {
     return __builtin_bit_cast(bf16x8, r);
 }
 
-// Eight weights of the second product as the sum of N bf16 numbers: 16 or 24 bits of each, at any size. (A half holds 11 bits in one
-// piece, but loses weights that are 2^-40 of the largest one; where the heavier tokens' codes are 0 those are the result.)
+// Eight factors of a product as sums of N bf16 numbers: 8, 16 or 24 bits of each, at any size. (A half holds 11 bits in one piece, but
+// loses what is 2^-40 of the largest factor; where the larger ones meet codes of 0 that is the result.)
 template <int N>
-__device__ inline void split_weights(const float *x, bf16x8 *w) {
+__device__ inline void split_factors(const float *x, bf16x8 *w) {
     u32x4 r[N];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -154,17 +138,8 @@ __device__ inline void load_eight(const T *row, uint32_t d, uint32_t head_dim, b
     for (int i = 0; i < 8; ++i) x[i] = d + i < head_dim ? load_as_f32(row + d + i) : 0.0f;
 }
 
-// A query row's exponent e with |x| < 2^(e + 1): x * 2^(14 - e) is taken as halves, in one piece (exact for 11 bits) or two.
+// A query row's exponent e with |x| < 2^(e + 1): x * 2^-e is taken into the product, so that scores do not overflow before they are scaled.
 __device__ inline int exponent_of(float most) { return max(static_cast<int>((__float_as_uint(most) >> 23) & 0xffu) - 127, -126); }
-
-template <int N>
-__device__ inline void split_halves(const float *x, half8 *hi, half8 *lo) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        (*hi)[i] = (_Float16)x[i];
-        if (N == 2) (*lo)[i] = (_Float16)(x[i] - (float)(*hi)[i]);
-    }
-}
 
 // ------------------------------------------------------------------------------------------------- few rows: token generation
 //
@@ -182,7 +157,7 @@ __device__ inline void split_halves(const float *x, half8 *hi, half8 *lo) {
 // up to 8192 tokens 127 us (4.4 TB/s: sequences of different lengths, see shape_of).
 template <int W, typename T>
 __global__ __launch_bounds__(kWG, W > 128 ? 1 : 2) void k_attend_few(Pool p, Query a) {
-    constexpr int kParts = sizeof(T) == 2 ? 1 : 2;         // halves that make a factor of the first product
+    constexpr int kParts = sizeof(T) == 2 ? 1 : 3;         // bf16 numbers that make an element of q in the first product
     constexpr int kWeights = sizeof(T) == 2 ? 2 : 3;       // bf16 numbers that make a weight of the second
     constexpr int kFull = W / 64, kRest = W % 64 ? 1 : 0;   // loads of 64 dimensions of 16 tokens, and of 32
     constexpr int kDims = W / 16;
@@ -248,7 +223,7 @@ __global__ __launch_bounds__(kWG, W > 128 ? 1 : 2) void k_attend_few(Pool p, Que
     const uint32_t my_head = head * a.group + static_cast<uint32_t>((mine ? my_row : row0) % a.group);
     const int32_t my_pos = s.pos + static_cast<int32_t>(my_token) - s.row;
     
-    half8 q[kParts][W / 32];
+    bf16x8 q[W / 32][kParts];
     float q_factor;
     {
         const T *row = static_cast<const T *>(a.q) + my_token * a.q_token_stride + my_head * a.q_head_stride;
@@ -272,10 +247,10 @@ __global__ __launch_bounds__(kWG, W > 128 ? 1 : 2) void k_attend_few(Pool p, Que
 #pragma unroll
         for (int f = 0; f < W / 32; ++f) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[f][i] = ldexpf(x[f][i] * sign, 14 - e);
-            split_halves<kParts>(x[f], &q[0][f], &q[kParts - 1][f]);
+            for (int i = 0; i < 8; ++i) x[f][i] = ldexpf(x[f][i] * sign, -e);
+            split_factors<kParts>(x[f], q[f]);
         }
-        q_factor = ldexpf(fabsf(a.scale) * kLog2e, e - 14);
+        q_factor = ldexpf(fabsf(a.scale) * kLog2e, e);
     }
     f32x4 o[kDims];
 #pragma unroll
@@ -291,17 +266,17 @@ __global__ __launch_bounds__(kWG, W > 128 ? 1 : 2) void k_attend_few(Pool p, Que
             z[t] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int f = 0; f < kFull; ++f) {
-                const half8 k0 = eight_codes(kc[t][f][0], kc[t][f][1]), k1 = eight_codes(kc[t][f][2], kc[t][f][3]);
+                const bf16x8 k0 = eight_values(kc[t][f][0], kc[t][f][1]), k1 = eight_values(kc[t][f][2], kc[t][f][3]);
 #pragma unroll
                 for (int n = 0; n < kParts; ++n) {
-                    z[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[n][2 * f], z[t], 0, 0, 0);
-                    z[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q[n][2 * f + 1], z[t], 0, 0, 0);
+                    z[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q[2 * f][n], z[t], 0, 0, 0);
+                    z[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[2 * f + 1][n], z[t], 0, 0, 0);
                 }
             }
             if (kRest) {
-                const half8 k0 = eight_codes(kr[t][0], kr[t][1]);
+                const bf16x8 k0 = eight_values(kr[t][0], kr[t][1]);
 #pragma unroll
-                for (int n = 0; n < kParts; ++n) z[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[n][2 * kFull], z[t], 0, 0, 0);
+                for (int n = 0; n < kParts; ++n) z[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q[2 * kFull][n], z[t], 0, 0, 0);
             }
         }
         // scores in units of log2; a page without a token that is seen may hold anything as its scale
@@ -345,7 +320,7 @@ __global__ __launch_bounds__(kWG, W > 128 ? 1 : 2) void k_attend_few(Pool p, Que
                 l += e;
                 x[j] = e * scale;
             }
-            split_weights<kWeights>(x, w[h]);
+            split_factors<kWeights>(x, w[h]);
         }
 #pragma unroll
         for (int d = 0; d < kDims; ++d) {
@@ -399,9 +374,8 @@ __global__ __launch_bounds__(kWG, W > 128 ? 1 : 2) void k_attend_few(Pool p, Que
 // ----------------------------------------------------------------------------------------------------- many rows: prompts
 //
 // A workgroup takes 32 rows a wavefront (tokens and the query heads of a key head side by side) and goes through the tokens 64 at
-// a time. All its threads turn the tile's codes into the numbers of the products, once, on their way to LDS: keys to halves
-// (q is scaled to halves exactly), values to bf16; rows in LDS are 16 bytes longer than their data, so that the 16 lanes that read
-// one place of 16 rows meet 64 different banks. While a tile is multiplied, the next one is written to the other half of the LDS and the
+// a time. All its threads turn the tile's codes into the bf16 numbers of the products, once, on their way to LDS;
+// rows in LDS are 16 bytes longer than their data, so that the 16 lanes that read one place of 16 rows meet 64 different banks. While a tile is multiplied, the next one is written to the other half of the LDS and the
 // codes of the one after it, and the page numbers of a third, are on their way.
 //
 // v_mfma_f32_32x32x16, scores transposed as above: a lane holds 32 of a tile's scores of one row, tokens 8 i + 4 h + (0..3)
@@ -415,7 +389,7 @@ __global__ __launch_bounds__(kWG, W > 128 ? 1 : 2) void k_attend_few(Pool p, Que
 template <int W, typename T>
 __global__ __launch_bounds__(kWG, sizeof(T) == 2 && W <= 128 ? 2 : 1) void k_attend_many(Pool p, Query a, uint32_t row_tiles) {
     constexpr int kThreads = kWG, kRows = kManyRows;
-    constexpr int kParts = sizeof(T) == 2 ? 1 : 2, kWeights = sizeof(T) == 2 ? 2 : 3;
+    constexpr int kParts = sizeof(T) == 2 ? 1 : 3, kWeights = sizeof(T) == 2 ? 2 : 3;
     constexpr int kChunks = (W * 4 + kThreads - 1) / kThreads;      // pieces of 16 codes a thread turns, of keys and of values
     constexpr int kKeyRow = 2 * W + 16, kValueRow = 2 * kTile + 16;   // bytes
     constexpr int kKeyTile = kTile * kKeyRow, kValueTile = W * kValueRow;
@@ -449,7 +423,7 @@ __global__ __launch_bounds__(kWG, sizeof(T) == 2 && W <= 128 ? 2 : 1) void k_att
         const int64_t wave_row = row0 + 32 * wave;
         const int32_t wave_first = s.pos + static_cast<int32_t>(wave_row / a.group);
         const int32_t wave_last = wave_row < rows ? s.pos + static_cast<int32_t>(min(wave_row + 31, rows - 1) / a.group) : -1;
-        half8 q[kParts][W / 16];
+        bf16x8 q[W / 16][kParts];
         float q_factor;
         {
             const T *row = static_cast<const T *>(a.q) + my_token * a.q_token_stride + my_head * a.q_head_stride;
@@ -468,10 +442,10 @@ __global__ __launch_bounds__(kWG, sizeof(T) == 2 && W <= 128 ? 2 : 1) void k_att
                 float x[8];
                 load_eight(row, 16 * f + 8 * h, p.head_dim, a.aligned, x);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = ldexpf(x[i] * sign, 14 - e);
-                split_halves<kParts>(x, &q[0][f], &q[kParts - 1][f]);
+                for (int i = 0; i < 8; ++i) x[i] = ldexpf(x[i] * sign, -e);
+                split_factors<kParts>(x, q[f]);
             }
-            q_factor = ldexpf(fabsf(a.scale) * kLog2e, e - 14);
+            q_factor = ldexpf(fabsf(a.scale) * kLog2e, e);
         }
         constexpr int kDims = W / 32;
         f32x16 o[kDims];
@@ -516,9 +490,9 @@ __global__ __launch_bounds__(kWG, sizeof(T) == 2 && W <= 128 ? 2 : 1) void k_att
             for (int n = 0; n < kChunks; ++n) {
                 const int32_t ch = n * kThreads + static_cast<int32_t>(tid);
                 if (kThreads * kChunks != W * 4 && ch >= W * 4) continue;
-                half8 *k = reinterpret_cast<half8 *>(key_lds[half] + (ch / (W / 16)) * kKeyRow + 32 * (ch % (W / 16)));
-                k[0] = eight_codes(kc[n][0], kc[n][1]);
-                k[1] = eight_codes(kc[n][2], kc[n][3]);
+                bf16x8 *k = reinterpret_cast<bf16x8 *>(key_lds[half] + (ch / (W / 16)) * kKeyRow + 32 * (ch % (W / 16)));
+                k[0] = eight_values(kc[n][0], kc[n][1]);
+                k[1] = eight_values(kc[n][2], kc[n][3]);
                 bf16x8 *v = reinterpret_cast<bf16x8 *>(value_lds[half] + (ch >> 2) * kValueRow + 32 * (ch & 3));
                 v[0] = eight_values(vc[n][0], vc[n][2]);
                 v[1] = eight_values(vc[n][1], vc[n][3]);
@@ -567,16 +541,16 @@ __global__ __launch_bounds__(kWG, sizeof(T) == 2 && W <= 128 ? 2 : 1) void k_att
                 z[0] = z[1] = f32x16{};
                 const uint8_t *at = key_lds[half] + c * kKeyRow + 16 * h;
                 // two tokens' groups in turn, so that a product does not wait for the one before it
-                const auto piece = [&](int j) { return *reinterpret_cast<const half8 *>(at + 32 * (j & 1) * kKeyRow + 32 * (j >> 1)); };
-                half8 k[kAhead];
+                const auto piece = [&](int j) { return *reinterpret_cast<const bf16x8 *>(at + 32 * (j & 1) * kKeyRow + 32 * (j >> 1)); };
+                bf16x8 k[kAhead];
 #pragma unroll
                 for (int j = 0; j < kAhead; ++j) k[j] = piece(j);
 #pragma unroll
                 for (int j = 0; j < W / 8; ++j) {
-                    const half8 now = k[j % kAhead];
+                    const bf16x8 now = k[j % kAhead];
                     if (j + kAhead < W / 8) k[j % kAhead] = piece(j + kAhead);
 #pragma unroll
-                    for (int n = 0; n < kParts; ++n) z[j & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now, q[n][j >> 1], z[j & 1], 0, 0, 0);
+                    for (int n = 0; n < kParts; ++n) z[j & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(now, q[j >> 1][n], z[j & 1], 0, 0, 0);
                 }
             }
             if (i + 1 < end) to_lds(half ^ 1);
@@ -626,7 +600,7 @@ __global__ __launch_bounds__(kWG, sizeof(T) == 2 && W <= 128 ? 2 : 1) void k_att
                         l += e;
                         x[j] = e * vf[g];
                     }
-                    split_weights<kWeights>(x, w[g]);
+                    split_factors<kWeights>(x, w[g]);
                 }
                 add_values(w, half);
             }

@@ -211,6 +211,26 @@ def test_attend_with_extreme_queries_and_scales(kind, new):
 
 
 @pytest.mark.parametrize("kind,new", [("bf16", 1), ("f32", 1), ("bf16", 40), ("f32", 40)])
+@pytest.mark.parametrize("dim", [40, 96, 128, 192, 256])
+def test_attend_with_queries_whose_largest_elements_meet_zeros(kind, new, dim):
+    """Elements of q that are 2^20 to 2^100 times all others, in dimensions whose key codes are 128: the others make the scores."""
+    rng = np.random.default_rng(23)
+    lengths, heads, page = [150 + new], 2, 32
+    pool, table = make(rng, 1, lengths, heads, dim, page)
+    scales(rng, pool, table)
+    for slot in table[0]:
+        for h in range(heads):
+            pool.at("k", 0, slot, h)[0][:, [0, dim - 1]] = 128
+    start = starts([new])
+    q = rng.standard_normal((new, 8, dim)) * 2
+    q[..., 0] = 2.0 ** np.array([100, 80, 60, 40, 35, 30, 25, 20])
+    q[..., dim - 1] = -1.5 * q[..., 0]
+    q = rounded(q, kind)
+    out, lse = run_attend(cache_of(pool), table, lengths, q, start, kind)
+    check_attend(pool, table, lengths, q, start, kind, out, lse, dim ** -0.5)
+
+
+@pytest.mark.parametrize("kind,new", [("bf16", 1), ("f32", 1), ("bf16", 40), ("f32", 40)])
 def test_attend_with_values_near_the_largest_number(kind, new):
     """Values of 3e38 at one token, whose weight is 2^7 times that of the tokens before it: the result is as large, its sums no larger."""
     rng = np.random.default_rng(22)
