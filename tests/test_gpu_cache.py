@@ -317,6 +317,25 @@ def test_attend_splits_of_every_width(kind, dim, lengths, new, group):
     check_attend(pool, table, lengths, q, start, kind, out, lse, dim ** -0.5)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("dim", [40, 64, 96, 128, 192, 256])
+@pytest.mark.parametrize("lengths,new,parts", [([1700, 30, 900], [1, 1, 1], 3), ([9000], [2], 17), ([1300, 1000, 9], [40, 3, 9], 2), ([2900, 50], [70, 50], 5)])
+def test_attend_joins_parts_of_every_width(kind, dim, lengths, new, parts):
+    """Rows in up to `parts` parts, in fewer where a sequence is shorter, by both kernels of joins; the workspace says that the call is split."""
+    rng = np.random.default_rng(24)
+    heads, group, page = 2, 3, 64
+    pool, table = make(rng, len(lengths), lengths, heads, dim, page)
+    scales(rng, pool, table)
+    start = starts(new)
+    q = rounded(rng.standard_normal((start[-1], heads * group, dim)) * 2, kind)
+    cache, t = cache_of(pool), E.CacheTable(dev(table), ints(lengths))
+    x = dev(q).to(TYPES[kind])
+    need = E.entro_cache_attend_workspace_bytes(cache, t, E.CacheQuery(x, x, ints(start), max(new), max(lengths)))
+    assert need == start[-1] * heads * group * parts * (ref.width(dim) + 1) * 4
+    out, lse = run_attend(cache, table, lengths, q, start, kind)
+    check_attend(pool, table, lengths, q, start, kind, out, lse, dim ** -0.5)
+
+
 def test_attend_long_context_splits_and_repeats():
     """A context long enough to be split over the chip; the same call again gives the same bits."""
     rng = np.random.default_rng(10)
