@@ -473,11 +473,12 @@ typedef struct {
     uint32_t reserved;           /* 0 */
 } entro_cache_query;
 
-/* Host: bytes a dimension row takes in the pool (the layouts on Eq. 1's grid given above): head_dim rounded up to 64, 96,
- * 128, 192 or 256; 0 for a head_dim of 0 or above ENTRO_CACHE_MAX_DIM. */
+/* Host: bytes a dimension row takes in the pool (a layout of this library: no passage of the paper defines it; the codes are those
+ * of Eq. 1): head_dim rounded up to 64, 96, 128, 192 or 256; 0 for a head_dim of 0 or above ENTRO_CACHE_MAX_DIM. */
 uint32_t entro_cache_width(uint32_t head_dim);
 
-/* Host: bytes of the codes (Eq. 1's integers) of k, and as many of v, that this pool needs; 0 if its sizes are not valid. */
+/* Host: bytes of the codes of k, and as many of v, that this pool needs; 0 if its sizes are not valid (no passage of the paper
+ * defines it; the codes are those of Eq. 1). */
 uint64_t entro_cache_codes_bytes(const entro_cache *c);
 
 /* Eq. 1's grid map for the keys and values of new tokens, into the pages of their positions.  For every block, head, and
@@ -494,12 +495,14 @@ entro_status entro_cache_append(const entro_cache *c, const entro_cache_table *t
  * nearest even), zeros where a position has no page. */
 entro_status entro_cache_read(const entro_cache *c, const entro_cache_table *t, const entro_cache_rows *r, void *hip_stream);
 
-/* Bytes of device workspace entro_cache_attend ("Latency Reduction from Huffman Coding": the phase's work split over the
- * chip) needs for these sizes on the current device; may be 0.  Only max_new, max_len and sizes count, no pointer is followed. */
+/* Bytes of device workspace entro_cache_attend needs for these sizes on the current device; may be 0.  Only max_new, max_len and
+ * sizes count, no pointer is followed.  (Part of the phase that "Latency Reduction from Huffman Coding" is about; no passage of
+ * the paper defines it.) */
 uint64_t entro_cache_attend_workspace_bytes(const entro_cache *c, const entro_cache_table *t, const entro_cache_query *q);
 
-/* Attention of token generation and of prompts over the cache, whose 8-bit codes are read as they are ("Latency Reduction
- * from Huffman Coding": fewer bytes read per token).  For the query at position i of a sequence and a query head:
+/* Attention of token generation and of prompts over the cache, whose 8-bit codes are read as they are.  (No passage of the paper
+ * defines it; "Latency Reduction from Huffman Coding" has the reason, fewer bytes read per token.)  For the query at position i
+ * of a sequence and a query head:
  *   out = sum_j p_j v_j, p = softmax_j(scale * q . k_j), lse = log(sum_j exp(scale * q . k_j)), over the positions j <= i that have a
  *   page and, if window > 0, i - j < window or j < sinks.
  * A query that sees nothing gets out 0 and lse -inf.  Sums are held in fp32.  bf16: q is taken exactly, probabilities
@@ -509,10 +512,11 @@ uint64_t entro_cache_attend_workspace_bytes(const entro_cache *c, const entro_ca
 entro_status entro_cache_attend(const entro_cache *c, const entro_cache_table *t, const entro_cache_query *q, void *workspace,
                                 uint64_t workspace_bytes, void *hip_stream);
 
-/* Bytes of device workspace the two calls below need (blocks of tokens as the segments of Fig. 3: independent pieces of known place). */
+/* Bytes of device workspace the two calls below need.  (This and the rest of the page tables serve the phase that "Latency Reduction
+ * from Huffman Coding" is about; no passage of the paper defines it.) */
 uint64_t entro_cache_pages_workspace_bytes(const entro_cache *c, const entro_cache_table *t, const entro_cache_table *next);
 
-/* The table of the next step (each sequence's pages, like Fig. 3's segments, are found through a table alone, so that sequences can share them):
+/* The table of the next step (serving in the phase of "Latency Reduction from Huffman Coding"; no passage of the paper defines it):
  * row b of `next` goes on from row parent[b] of t (NULL: from row b; a value outside t: an empty row, the sequence has
  * ended).  It keeps the first min(length, length + grow[b]) tokens (grow NULL: all) and, if window > 0, drops pages that no
  * further query can see (entro_cache_query's window and sinks); its length becomes max(0, length + grow[b]), with pages for the
@@ -527,14 +531,16 @@ entro_status entro_cache_regroup(const entro_cache *c, const entro_cache_table *
                                  uint32_t window, uint32_t sinks, const entro_cache_table *next, int32_t *status, void *workspace,
                                  uint64_t workspace_bytes, void *hip_stream);
 
-/* Brings the pages that t names to the front of the pool (as Fig. 3's segments lie back to back): with n pages in use, the
- * i-th used page of number n or above moves to the i-th free page below n, in all layers.  `next` (buffers of its own, seqs
- * and stride of t) receives the table that names them there; pages n.. can be given back once it is in use.  No page in use is overwritten.
+/* Brings the pages that t names to the front of the pool (serving in the phase of "Latency Reduction from Huffman Coding"; no
+ * passage of the paper defines it): with n pages in use, the i-th used page of number n or above moves to the i-th free page
+ * below n, in all layers.  `next` (buffers of its own, seqs and stride of t) receives the table that names them there; pages n.. can
+ * be given back once it is in use.  No page in use is overwritten.
  * status: as above; its last word counts the pages moved. */
 entro_status entro_cache_compact(const entro_cache *c, const entro_cache_table *t, const entro_cache_table *next, int32_t *status,
                                  void *workspace, uint64_t workspace_bytes, void *hip_stream);
 
-/* Host: the meaning of a status word of the two calls above (tables of Fig. 3's kind): ENTRO_OK or ENTRO_ERR_CAPACITY. */
+/* Host: the meaning of a status word of the two calls above: ENTRO_OK or ENTRO_ERR_CAPACITY (error reporting of the phase of "Latency
+ * Reduction from Huffman Coding"; no passage of the paper defines it). */
 entro_status entro_cache_status(int32_t status_word);
 
 /* Text of the last HIP error seen by the calling thread ("" if none) (error reporting; no

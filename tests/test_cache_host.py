@@ -1,5 +1,7 @@
 """Host side of the token cache: sizes, refusals before anything reaches a GPU, and the binding's own checks (CPU only)."""
 import ctypes as C
+import os
+import re
 
 import numpy as np
 import pytest
@@ -266,3 +268,14 @@ def test_read_refuses_rows_that_share_their_places(calls_made):
                 E.entro_cache_read(cache, table, E.CacheRows(k, v, start, 1))
             E.entro_cache_append(cache, table, E.CacheRows(k, v, start, 1))         # rows that are only read may
     assert calls_made == ["entro_cache_append"] * 4
+
+
+def test_the_header_says_which_calls_the_paper_does_not_define():
+    """The paper defines the grid that keys and values are put on (Eq. 1), and nothing else of the cache."""
+    header = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "entro.h")).read()
+    comments = dict((name, re.sub(r"[\s*]+", " ", text)) for text, name in re.findall(r"/\*((?:(?!\*/).)*)\*/\s*\w+ (entro_cache_\w+)\(", header, re.S))
+    assert set(comments) == {n for n in B.EXPORTED if n.startswith("entro_cache_")}
+    for name, text in comments.items():
+        defined = name in ("entro_cache_append", "entro_cache_read")
+        assert ("Eq. 1" in text) if defined else ("no passage of the paper defines it" in text.lower()), name
+        assert "Fig. 3" not in text, name
