@@ -486,6 +486,8 @@ uint64_t entro_cache_codes_bytes(const entro_cache *c);
  *   a = the largest |x| among the block's new finite elements; s' = max(s, a / 127), s being the block's scale, or 0 if it
  *   holds no tokens before the new ones; code = clamp(rint(x / s'), -127, 127) + 128;
  *   where s' > s, the block's older codes c become rint((c - 128) * s / s') + 128.
+ * Each such move rounds again: a value is off by at most half the sum of the scales that it was rounded at, its first and those that its
+ * block has risen to since (half the last scale if the block was written at once, page_tokens times that at the worst).
  * binary32 arithmetic, round-half-even, true division.  A NaN becomes 128 (the value 0), an infinity the end of the grid; s' = 0 makes
  * all codes 128.  Writing the same rows again changes nothing.  A page must belong to one sequence at the positions
  * written (entro_cache_regroup sees to that), and calls for one pool are to be ordered. */

@@ -425,6 +425,32 @@ def test_append_token_by_token_with_a_scale_that_rises(kind, heads, page, dim):
         pool.k, pool.v = cache.k.cpu().numpy(), cache.v.cpu().numpy()
 
 
+@pytest.mark.parametrize("page,dim,rise", [(64, 128, 1.002), (64, 128, 1.1), (256, 40, 1.01), (16, 64, 2.0)])
+def test_errors_of_a_block_whose_scale_rises_token_by_token(page, dim, rise):
+    """Every value is off by at most half the sum of the scales that it was rounded at; a quotient's own rounding is a relative 2^-23, of at
+    most 127, at each."""
+    rng = np.random.default_rng(25)
+    heads = 2
+    pool, table = make(rng, 1, [page], heads, dim, page)
+    cache, table_dev = cache_of(pool), dev(table)
+    rows, before = {"k": [], "v": []}, {"k": [], "v": []}
+    for n in range(1, page + 1):
+        for name in "kv":
+            x = rng.uniform(-1, 1, (1, heads, dim)) * rise ** n
+            x[..., n % dim] = rise ** n
+            rows[name].append(x.astype(np.float32))
+        E.entro_cache_append(cache, E.CacheTable(table_dev, ints([n])), E.CacheRows(dev(rows["k"][-1]), dev(rows["v"][-1]), ints([0, 1]), 1))
+        for name in "kv":
+            before[name].append(getattr(cache, name + "_scale")[0, table[0, 0]].cpu().numpy().astype(np.float64))
+    back = [torch.zeros(page, heads, dim, device=DEV) for _ in "kv"]
+    E.entro_cache_read(cache, E.CacheTable(table_dev, ints([page])), E.CacheRows(*back, ints([0, page]), page))
+    for got, name in zip(back, "kv"):
+        scale = np.array(before[name])                                    # [token][head]
+        assert np.all(np.diff(scale, axis=0) > 0)
+        bound = np.cumsum(scale[::-1], 0)[::-1] * (0.5 + 2.0 ** -15)
+        assert np.all(np.abs(got.cpu().numpy() - np.concatenate(rows[name])) <= bound[..., None])
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
 def test_append_takes_values_that_are_no_numbers(kind):
     """NaN, infinities, a block of zeros, values too small for a scale of their own, the largest finite ones."""
