@@ -527,6 +527,10 @@ uint64_t entro_cache_pages_workspace_bytes(const entro_cache *c, const entro_cac
  * others get copies (of all layers).  New pages are the lowest free ones, rows in ascending order, a row's copy
  * before what it grows by; free is what no row of `next` holds, so pages that only t holds may be overwritten.  `next`
  * has buffers of its own.
+ * What a window has dropped does not come back: after a later grow below 0, queries that would see dropped tokens do so no more, and
+ * where the row then goes on inside a dropped page, it has none for the rest of that page's positions (rows there are not kept, and seen by
+ * no query); the next position's page is a new one.  A program that takes tokens back under a window drops pages by a window that is
+ * longer by as many tokens as it may take back.
  * parent, grow: device, [next->seqs].  status: device, 16-byte aligned, int32[4]: status word, pages in use, free pages, copies.
  * Where pages or slots do not suffice the status word says so (entro_cache_status), nothing is copied and `next` is not to be used. */
 entro_status entro_cache_regroup(const entro_cache *c, const entro_cache_table *t, const int32_t *parent, const int32_t *grow,

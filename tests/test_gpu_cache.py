@@ -594,6 +594,38 @@ def test_regroup_of_random_tables():
     assert done >= 10
 
 
+@pytest.mark.parametrize("spare_window", [0, 48])
+def test_tokens_taken_back_under_a_window(spare_window):
+    """100 tokens, 45 taken back and 10 written again, with a window of 20: by that window pages are dropped that the row then goes on in, and
+    what it writes there is seen by no query; by a window longer by 48 everything that the definition sees is there."""
+    rng = np.random.default_rng(26)
+    page, heads, dim, window = 16, 2, 64, 20
+    pool, table = make(rng, 1, [100], heads, dim, page, spare=6, slots=8)
+    scales(rng, pool, table)
+    cache, tables = cache_of(pool), [E.CacheTable(dev(table), ints([100])), E.CacheTable.empty(1, 8)]
+    status = torch.zeros(4, dtype=torch.int32, device=DEV)
+    room = torch.empty(E.entro_cache_pages_workspace_bytes(cache, *tables), dtype=torch.uint8, device=DEV)
+    for grow in (0, -45, 10):
+        E.entro_cache_regroup(cache, *tables, status, room, grow=ints([grow]), window=window + spare_window)
+        tables.reverse()
+        torch.cuda.synchronize()
+        assert status[0].item() == 0
+    now = tables[0].slots.cpu().numpy()
+    assert tables[0].lengths.item() == 65
+    # positions 55..63 go on in the block of 48..63, 64 begins a block
+    assert now[0, 4] >= 0 and (now[0, 3] >= 0) == (spare_window > 0) and (now[0, 2] >= 0) == (spare_window > 0)
+    k, v = (rng.standard_normal((10, heads, dim)).astype(np.float32) for _ in "kv")
+    E.entro_cache_append(cache, tables[0], E.CacheRows(dev(k), dev(v), ints([0, 10]), 10))
+    torch.cuda.synchronize()
+    twin, whole = pool.copy(), np.where(now >= 0, now, table if spare_window else -1)
+    ref.append(twin, whole, [65], k, v, [0, 10])
+    twin.k, twin.v = cache.k.cpu().numpy(), cache.v.cpu().numpy()
+    q = rng.standard_normal((10, 4, dim)).astype(np.float32)
+    out, lse = run_attend(cache, now, [65], q, np.array([0, 10]), "f32", window=window)
+    check_attend(twin, whole, [65], q, np.array([0, 10]), "f32", out, lse, dim ** -0.5, window)
+    assert bool(torch.isneginf(lse[0, 0])) == (spare_window == 0)
+
+
 @pytest.mark.parametrize("case", range(5))
 def test_compact_against_the_definition(case):
     rng = np.random.default_rng(4000 + case)
