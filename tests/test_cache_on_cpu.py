@@ -40,10 +40,10 @@ def host(tmp_path_factory):
     L = compiled(tmp_path_factory.mktemp("host_cache"), "host_cache.cpp", "\n".join([
         source("entro_cache.h"), source("entro_cache.hip").replace(include, ""), "namespace {", part("struct Query {", "typedef"),
         part("constexpr uint32_t kMostSplits", "constexpr float"), part("entro_status check_query_sizes")]))
-    for name in ("append", "read", "attend"):
+    for name in ("append", "read", "attend", "regroup", "compact"):
         call, twin = getattr(L, "entro_cache_" + name), getattr(B.lib(), "entro_cache_" + name)
         call.argtypes = twin.argtypes
-    L.entro_cache_attend_workspace_bytes.restype = C.c_uint64
+    L.entro_cache_attend_workspace_bytes.restype = L.entro_cache_pages_workspace_bytes.restype = C.c_uint64
     return L
 
 
@@ -144,3 +144,52 @@ def test_attend_refuses_more_sequences_and_heads_than_a_launch_takes(host):
     table.seqs = (1 << 18) - 8
     assert host.entro_cache_attend(C.byref(cache), C.byref(table), C.byref(query), None, 0, None) == B.ENTRO_OK and len(launched(host)) == 1
     host.host_only_note(0)
+
+
+def page_call(host, mem, pool, table, lengths, seqs, stride, call):
+    """(next table, lengths, status) of regroup or compact; pool's pages move in place."""
+    layers = pool.k.shape[0]
+    cache = B.CCache(pool.k.ctypes.data, pool.v.ctypes.data, pool.k_scale.ctypes.data, pool.v_scale.ctypes.data, layers, pool.pages, pool.page, pool.heads, pool.dim, 0)
+    slots, at = mem(table, np.int32), mem(lengths, np.int32)
+    to, then, status = mem(np.full((seqs, stride), 77), np.int32), mem(np.full(seqs, 77), np.int32), mem(np.full(4, 77), np.int32)
+    t, n = B.CCacheTable(slots.ctypes.data, at.ctypes.data, *slots.shape), B.CCacheTable(to.ctypes.data, then.ctypes.data, seqs, stride)
+    need = host.entro_cache_pages_workspace_bytes(C.byref(cache), C.byref(t), C.byref(n))
+    room = mem(np.full(need, 0xAB), np.uint8)
+    assert call(C.byref(cache), C.byref(t), C.byref(n), status.ctypes.data, room.ctypes.data, need) == B.ENTRO_OK
+    return to, then, status
+
+
+@pytest.mark.parametrize("first_wave,seqs,stride,page,most", [(0, 12, 20, 16, 150), (15, 12, 20, 16, 150), (2, 40, 9, 32, 60), (1, 20, 850, 16, 120)])
+def test_page_tables_whichever_wavefront_comes_first(host, first_wave, seqs, stride, page, most):
+    """Regroup and compact, by one workgroup and (the last sizes) by several launches, with forks, drops, growth, windows and pages that are none."""
+    host.host_first_wave(first_wave)
+    rng = np.random.default_rng(first_wave + seqs)
+    lengths = rng.integers(0, most, seqs)
+    need = [-(-n // page) for n in lengths]
+    pages = sum(need) + 2 * seqs + 10
+    pool, mem = ref.Pool(rng, 1, pages, 1, page, 1), Memory()
+    pool.k_scale[...], pool.v_scale[...] = rng.random(pool.k_scale.shape), rng.random(pool.v_scale.shape)
+    own_memory(mem, pool)
+    order, table, at = rng.permutation(pages), np.full((seqs, stride), -1, np.int32), 0
+    for b, n in enumerate(need):
+        table[b, :n] = order[at: at + n]
+        at += n
+    table[3, 0] = pages + 5
+    parent = mem(np.where(rng.random(seqs) < 0.2, np.arange(seqs), rng.integers(-1, seqs + 1, seqs)), np.int32)
+    grow = mem(rng.integers(-20, 12, seqs), np.int32)
+    window, sinks = 50, 20
+    twin = pool.copy()
+    want = ref.regroup(pages, page, table, lengths, seqs, stride, parent, grow, window, sinks)
+    assert want is not None and len(want[2]) > 0
+    to, then, status = page_call(host, mem, pool, table, lengths, seqs, stride, lambda c, t, n, st, ws, size: host.entro_cache_regroup(
+        c, t, parent.ctypes.data, grow.ctypes.data, window, sinks, n, st, ws, size, None))
+    assert np.array_equal(to, want[0]) and np.array_equal(then, want[1]) and list(status) == [0, want[3], pages - want[3], len(want[2])]
+    ref.copy_pages(twin, want[2])
+    for name in ("k", "v", "k_scale", "v_scale"):
+        assert np.array_equal(getattr(pool, name), getattr(twin, name)), name
+    want = ref.compact(pages, to, then)
+    to, then, status = page_call(host, mem, pool, to, then, seqs, stride, lambda c, t, n, st, ws, size: host.entro_cache_compact(c, t, n, st, ws, size, None))
+    assert np.array_equal(to, want[0]) and np.array_equal(then, want[1]) and list(status) == [0, want[3], pages - want[3], len(want[2])]
+    ref.copy_pages(twin, want[2])
+    for name in ("k", "v", "k_scale", "v_scale"):
+        assert np.array_equal(getattr(pool, name), getattr(twin, name)), name
