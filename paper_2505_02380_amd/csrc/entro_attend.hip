@@ -150,11 +150,11 @@ __device__ inline int exponent_of(float most) { return max(static_cast<int>((__f
 // the probabilities. Keys, values and probabilities so go from memory through registers to the matrix units, with no
 // exchange between lanes but for the maximum. Matrix unit slots that a tile of 16 rows leaves empty cost nothing.
 //
-// Bound by the bytes of the codes. The softmax and the turning of codes into numbers take about 500 vector instructions a
-// tile, a third of the time its 16 KB (128 dimensions) take to arrive; so what counts is that loads are always on their way: page numbers are
+// Bound by the bytes of the codes. The softmax and the turning of codes into numbers take about 750 vector instructions a
+// tile, half of the time its 16 KB (128 dimensions) take to arrive; so what counts is that loads are always on their way: page numbers are
 // asked for two tiles ahead, a tile's codes as soon as the last tile's have been used. Measured: 131072 tokens of 8 heads of 128
-// 55 us with the join (4.9 TB/s; loads alone 51 to 56), 32 sequences in a window of 4096 with 32 heads of 96 139 us (5.5 TB/s), 64 sequences of
-// up to 8192 tokens 127 us (4.4 TB/s: sequences of different lengths, see shape_of).
+// 55 us with the join (4.9 TB/s), 32 sequences in a window of 4096 with 32 heads of 96 142 us (5.4 TB/s), 64 sequences of
+// up to 8192 tokens 128 us (4.3 TB/s: sequences of different lengths, see shape_of); in fp32 the first of these 54 us, the last 127.
 template <int W, typename T>
 __global__ __launch_bounds__(kWG, W > 128 ? 1 : 2) void k_attend_few(Pool p, Query a) {
     constexpr int kParts = sizeof(T) == 2 ? 1 : 3;         // bf16 numbers that make an element of q in the first product
@@ -382,10 +382,12 @@ __global__ __launch_bounds__(kWG, W > 128 ? 1 : 2) void k_attend_few(Pool p, Que
 // of each 32, h being the lane's half. The values' tokens lie in LDS in the order 0-3, 8-11, 4-7, 12-15 of each 16, so that what a
 // lane reads of them for the second product are the tokens whose weights it has.
 //
-// Bound by issue: of a wavefront's time, matrix instructions take 40 % and vector instructions 50 %, and the two of different
-// wavefronts overlap little. 4096 rows of 32 heads of 128 over 8192 tokens: 650 us, 0.63 PFLOP/s of the definition's operations (0.95 of the
-// matrix units', as weights are two bf16 numbers); of that, about 280 us go with the second product, 180 with the first, 140 with the
-// softmax, 110 with codes on their way to LDS.
+// Bound by issue: of a compute unit's time, matrix instructions take 43 % and vector instructions 65 %, and together they
+// run in 19 %. 4096 rows of 32 heads of 128 over 8192 tokens: 635 to 650 us, 0.63 to 0.65 PFLOP/s of the definition's operations (0.95 of the
+// matrix units', as weights are two bf16 numbers). Left out one at a time, the second product takes 288 us with it, the first 202, the codes'
+// way to LDS 71. fp32 rows take twice the matrix instructions, and one workgroup a compute unit (382 registers at 96 dimensions): 98 row
+// groups of 4 key heads of 80 dimensions, each over about 1100 tokens, 182 us. Registers that do not fit are kept in memory: at 256 dimensions
+// 162 for fp32 and 30 for bf16, at 192 35 for fp32, at 96 and 128 2 and 5 for bf16.
 template <int W, typename T>
 __global__ __launch_bounds__(kWG, sizeof(T) == 2 && W <= 128 ? 2 : 1) void k_attend_many(Pool p, Query a, uint32_t row_tiles) {
     constexpr int kThreads = kWG, kRows = kManyRows;
@@ -779,8 +781,9 @@ Shape shape_of(const entro_cache *c, const entro_cache_table *t, const entro_cac
     if (q->window && len > uint64_t{q->window} + q->sinks + max_new + 2 * kTile) len = uint64_t{q->window} + q->sinks + max_new + 2 * kTile;
     const uint64_t tiles = (len + kTile - 1) / kTile, units = uint64_t{t->seqs} * c->kv_heads;
     uint64_t groups = units;
-    // up to 32 rows in groups of 16, one after the other (32 and 48 rows of 128 dimensions over 4096 tokens of 8 sequences: 45 and 66 us,
-    // by the kernel for many 56 and 61)
+    // up to 32 rows in groups of 16, one after the other. 32 rows over 4096 tokens of 64 sequences, by the kernel for few and by that for many:
+    // 89 and 115 us for 64 dimensions, 179 and 191 for 128; in fp32 98 and 269, 186 and 404. Of 8 sequences (128 dimensions): 20 rows 41 and 40, 32 rows 44 and
+    // 40, 48 rows 65 and 47, 64 rows 83 and 51; in fp32 32 rows 46 and 74.
     if (rows > 32) {
         s.many = true;
         const uint64_t row_tiles = (rows + kManyRows - 1) / kManyRows, most = kMostGroups / units;
@@ -791,15 +794,17 @@ Shape shape_of(const entro_cache *c, const entro_cache_table *t, const entro_cac
     uint64_t want, can;
     if (!s.many && units * 4 > cus * 2) {
         // the heads of many sequences fill the chip; pieces of at most 96 tiles keep one long sequence from being the last
-        // alone (8192 tokens of 64 sequences in one, two, four pieces: 128, 130, 127 us; 4096 of 32 with 32 heads: 139, 147, 154)
+        // alone. One piece, pieces of 96 tiles, of 48: 32768 tokens beside 63 sequences of 512 tokens 272, 70, 56 us, beside 63 of 4096 307, 134, 138;
+        // 64 sequences of up to 8192 tokens 130, 128, 132, all of 8192 171, 180, 185 (which one piece would suit)
         want = can = (tiles + 95) / 96;
     } else if (!s.many) {
         // two workgroups a compute unit are enough (131072 tokens, 8 heads: 64 pieces 55 us, 128 pieces 60 us); below 24 tiles the
-        // join costs more than it gives (9 tiles: 8.1 us in one piece, 11.3 in two)
+        // join costs as much as it gives (8 heads, in one piece and in two or three: 16 tiles 14.4 and 15.6 us, 20 tiles 16.0 and 16.9, 23 tiles 18.8 and
+        // 17.4, 24 tiles 19.4 and 15.9, 32 tiles 23.4 and 16.1)
         want = cus * 2 / units;
         can = tiles < 24 ? 1 : tiles / 8;
     } else {
-        // two workgroups a compute unit (64 tokens of 32 heads over 8192: 49 us, 1024 over 16384: 487 us in two pieces, 516 in one, 513 in four)
+        // two workgroups a compute unit (64 tokens of 32 heads over 8192: 46 us; 1024 over 16384 463 us)
         want = (cus * 2 + groups - 1) / groups;
         can = tiles / 8;
     }

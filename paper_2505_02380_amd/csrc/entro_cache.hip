@@ -202,8 +202,8 @@ __device__ inline void write_patch(const Pool &p, uint64_t unit, const Patch &a,
 
 // LANES lanes to a block and head: a wavefront where that has few patches, else the workgroup. Rows are read once where every lane
 // has one patch (up to 64 tokens of 128 dimensions), else twice.  Bound by the bytes of the rows and codes for prompts, by
-// the latency of dependent loads (row numbers, page and rows, scale) for single tokens.  24700 rows of 8 heads of 128: 44 us written,
-// 31 us read back as bf16 (3.5 and 4.9 TB/s); a row of each of 64 sequences 7.6 us.
+// the latency of dependent loads (row numbers, page and rows, scale) for single tokens.  26800 rows of 8 heads of 128 in bf16: 44 us written,
+// 32 us read back (3.8 and 5.2 TB/s); a row of each of 64 sequences 7.6 us written, 8.8 read, the 64 blocks that they lie in 10.7.
 template <typename T, int LANES>
 __global__ __launch_bounds__(kWG) void k_append(Pool p, Rows r, uint32_t blocks, uint32_t work) {
     __shared__ uint32_t most[2][kWG / 64];
