@@ -386,6 +386,67 @@ entro_status entro_encode_device(const uint8_t *q, uint64_t n, const entro_codeb
  * small), ENTRO_ERR_SIZE (the stream would reach 4 GiB). */
 entro_status entro_encode_device_status(uint32_t status_word);
 
+/* ------------------------------------------------ device side: positions
+ * What token generation does to queries and keys between its products and the
+ * cache: a norm of each head, and the rotation of its pairs of dimensions by
+ * angles that grow with the token's position.  Rows are fp32 or bf16; everything
+ * between reading and writing them is fp32, rounded once at the end.
+ *
+ * With n the head's elements after the norm (none, or over all head_dim of them):
+ *   ENTRO_NORM_RMS       n = x * gain / sqrt(mean(x^2) + eps)
+ *   ENTRO_NORM_CENTRED   n = (x - mean(x)) * gain / sqrt(mean((x - mean(x))^2) + eps)
+ * and pair i of the first `dims` dimensions being (i, i + dims / 2)
+ * (ENTRO_ROTARY_HALVES) or (2 i, 2 i + 1) (ENTRO_ROTARY_PAIRS), at position p
+ *   a = 2 pi * p * turns[i] / 2^64,
+ *   (u, w) becomes amplitude * (u cos a - w sin a, w cos a + u sin a);
+ * dimensions from dims on are n as they are.  p * turns[i] is taken modulo 2^64:
+ * angles are as exact at position 2^31 as at 1, and negative positions turn the
+ * other way.
+ */
+typedef enum { ENTRO_ROTARY_HALVES = 0, ENTRO_ROTARY_PAIRS = 1 } entro_rotary_layout;
+typedef enum { ENTRO_NORM_NONE = 0, ENTRO_NORM_RMS = 1, ENTRO_NORM_CENTRED = 2 } entro_norm;
+typedef enum { ENTRO_CONTEXT_AS_TRAINED = 0, ENTRO_CONTEXT_LINEAR = 1, ENTRO_CONTEXT_BY_PARTS = 2 } entro_context;
+
+/* How heads are normed and rotated.  Plain data, caller-owned. */
+typedef struct {
+    const uint64_t *turns;       /* device: [dims / 2], as entro_rotary_turns makes them */
+    const float *q_gain, *k_gain;   /* device: gains of the norm, or NULL for ones */
+    uint32_t q_gain_stride, k_gain_stride;   /* elements from one head's gains to the next one's; 0: [head_dim], the same for all heads */
+    uint32_t dims;               /* rotated dimensions: even, 0 .. head_dim */
+    uint32_t layout;             /* entro_rotary_layout */
+    uint32_t norm;               /* entro_norm */
+    float eps;                   /* of the norm, at least 1.2e-38 */
+    float amplitude;             /* of cosines and sines: 1, or what a lengthened context asks for */
+    uint32_t reserved;           /* 0 */
+} entro_rotary;
+
+/* Rows [tokens][heads][head_dim] with strides in elements (dimensions lie side by side).  They and the gains need no more than their
+ * elements' own alignment; rows that begin at multiples of 16 bytes are faster. */
+typedef struct {
+    const void *x;               /* device: read */
+    void *y;                     /* device: written; x itself (with the same strides), or memory apart from it */
+    uint64_t x_token_stride, x_head_stride, y_token_stride, y_head_stride;
+    uint32_t heads;
+    uint32_t reserved;           /* 0 */
+} entro_rotary_rows;
+
+/* Host: turns[i] = 2^64 * f_i / (2 pi) for the dims / 2 pairs of `dims` rotated dimensions, rounded, f_i radians a position: base^(-2 i / dims)
+ *   ENTRO_CONTEXT_AS_TRAINED   as it is (factor, trained, low and high are not looked at)
+ *   ENTRO_CONTEXT_LINEAR       divided by `factor` (positions interpolated, arXiv 2306.15595)
+ *   ENTRO_CONTEXT_BY_PARTS     f_i * (g + (1 - g) / factor), g = clamp((r - low) / (high - low), 0, 1), r = trained * f_i / (2 pi) the turns
+ *                              over the `trained` positions (arXiv 2309.00071, which has an amplitude of 0.1 ln(factor) + 1, low 1, high 32)
+ * ENTRO_ERR_SIZE for odd dims or more than ENTRO_CACHE_MAX_DIM, ENTRO_ERR_SCHEME for another kind, ENTRO_ERR_RANGE unless base >= 1, factor >= 1,
+ * trained >= 1 and 0 <= low < high, all finite.  (For the phase of "Latency Reduction from Huffman Coding"; no passage of the paper defines it.) */
+entro_status entro_rotary_turns(uint32_t dims, double base, uint32_t context, double factor, double trained, double low, double high,
+                                uint64_t *turns);
+
+/* Norms and rotations of q and k rows (either may be NULL) at positions[0 .. tokens - 1] (device).  type: ENTRO_F32 or ENTRO_BF16, of all rows.
+ * head_dim: 1 .. ENTRO_CACHE_MAX_DIM.  NaN and infinities stay within their head.  ENTRO_ERR_SIZE where tokens times heads reach
+ * 2^31, where y is x with other strides, and where dims is odd or above head_dim; ENTRO_ERR_RANGE for an eps or amplitude that is none.
+ * (For the phase of "Latency Reduction from Huffman Coding"; no passage of the paper defines it.) */
+entro_status entro_rotate(const entro_rotary *r, const entro_rotary_rows *q, const entro_rotary_rows *k, const int32_t *positions,
+                          uint32_t tokens, uint32_t head_dim, entro_dtype type, void *hip_stream);
+
 /* ------------------------------------------------ device side: the token cache
  * Token generation reads, after the weights, the keys and values of every token
  * so far ("Latency Reduction from Huffman Coding": the phase is bound by bytes
@@ -492,6 +553,14 @@ uint64_t entro_cache_codes_bytes(const entro_cache *c);
  * all codes 128.  Writing the same rows again changes nothing.  A page must belong to one sequence at the positions
  * written (entro_cache_regroup sees to that), and calls for one pool are to be ordered. */
 entro_status entro_cache_append(const entro_cache *c, const entro_cache_table *t, const entro_cache_rows *r, void *hip_stream);
+
+/* entro_cache_append of keys that entro_rotate has normed and rotated in fp32 (no rounding between), at the positions of their rows; values
+ * are written as they are.  q, or NULL: query rows of the same tokens and type, which are normed and rotated in the same launch (q->x to
+ * q->y, q->heads heads); rows that no sequence has are left alone.  Query rows are rotated wherever they stand, also before position 0 or where
+ * there is no page.  Rows need no more than their elements' own alignment.  Writing the same rows again changes nothing in the cache.
+ * (Eq. 1's grid map behind a rotation; no passage of the paper defines it.) */
+entro_status entro_cache_append_rotated(const entro_cache *c, const entro_cache_table *t, const entro_cache_rows *r, const entro_rotary *rotary,
+                                        const entro_rotary_rows *q, void *hip_stream);
 
 /* The inverse of Eq. 1's grid map for tokens of the cache: k and v rows receive (code - 128) * scale (bf16: rounded to
  * nearest even), zeros where a position has no page. */

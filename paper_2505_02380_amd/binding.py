@@ -13,6 +13,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ENTRO_UNSIGNED, ENTRO_ASYMMETRIC = 0, 1
 ENTRO_U8, ENTRO_U4_PACKED, ENTRO_F32, ENTRO_BF16 = 0, 1, 2, 3
 ENTRO_OP_DECODE, ENTRO_OP_DEQUANT, ENTRO_OP_GEMV = 0, 1, 2
+ENTRO_ROTARY_HALVES, ENTRO_ROTARY_PAIRS = 0, 1
+ENTRO_NORM_NONE, ENTRO_NORM_RMS, ENTRO_NORM_CENTRED = 0, 1, 2
+ENTRO_CONTEXT_AS_TRAINED, ENTRO_CONTEXT_LINEAR, ENTRO_CONTEXT_BY_PARTS = 0, 1, 2
 ENTRO_OK = 0
 (ENTRO_ERR_NULL, ENTRO_ERR_BITS, ENTRO_ERR_SCHEME, ENTRO_ERR_SIZE, ENTRO_ERR_NONFINITE, ENTRO_ERR_RANGE,
  ENTRO_ERR_SYMBOL, ENTRO_ERR_CODE_TOO_LONG, ENTRO_ERR_CAPACITY, ENTRO_ERR_CORRUPT, ENTRO_ERR_ALIGN,
@@ -70,6 +73,17 @@ class CCacheQuery(C.Structure):
                 ("start", C.c_void_p), ("tokens", C.c_uint32), ("max_new", C.c_uint32), ("max_len", C.c_uint32),
                 ("q_heads", C.c_uint32), ("type", C.c_uint32), ("layer", C.c_uint32), ("window", C.c_uint32), ("sinks", C.c_uint32),
                 ("scale", C.c_float), ("reserved", C.c_uint32)]
+
+
+class CRotary(C.Structure):
+    _fields_ = [("turns", C.c_void_p), ("q_gain", C.c_void_p), ("k_gain", C.c_void_p), ("q_gain_stride", C.c_uint32),
+                ("k_gain_stride", C.c_uint32), ("dims", C.c_uint32), ("layout", C.c_uint32), ("norm", C.c_uint32), ("eps", C.c_float),
+                ("amplitude", C.c_float), ("reserved", C.c_uint32)]
+
+
+class CRotaryRows(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("y", C.c_void_p), ("x_token_stride", C.c_uint64), ("x_head_stride", C.c_uint64),
+                ("y_token_stride", C.c_uint64), ("y_head_stride", C.c_uint64), ("heads", C.c_uint32), ("reserved", C.c_uint32)]
 
 
 class EntroError(RuntimeError):
@@ -150,6 +164,10 @@ def lib():
                                           C.c_uint64, C.c_void_p]),
         "entro_cache_compact": (C.c_int, [kp, kt, kt, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p]),
         "entro_cache_status": (C.c_int, [C.c_int32]),
+        "entro_rotary_turns": (C.c_int, [C.c_uint32, C.c_double, C.c_uint32, C.c_double, C.c_double, C.c_double, C.c_double, u64p]),
+        "entro_rotate": (C.c_int, [C.POINTER(CRotary), C.POINTER(CRotaryRows), C.POINTER(CRotaryRows), C.c_void_p, C.c_uint32, C.c_uint32, C.c_int,
+                                   C.c_void_p]),
+        "entro_cache_append_rotated": (C.c_int, [kp, kt, C.POINTER(CCacheRows), C.POINTER(CRotary), C.POINTER(CRotaryRows), C.c_void_p]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -169,7 +187,7 @@ EXPORTED = ["entro_quantize", "entro_build_codebook", "entro_codebook_from_count
             "entro_encoded_bytes", "entro_encode_device", "entro_encode_device_status",
             "entro_cache_width", "entro_cache_codes_bytes", "entro_cache_append", "entro_cache_read",
             "entro_cache_attend_workspace_bytes", "entro_cache_attend", "entro_cache_pages_workspace_bytes", "entro_cache_regroup",
-            "entro_cache_compact", "entro_cache_status"]
+            "entro_cache_compact", "entro_cache_status", "entro_rotary_turns", "entro_rotate", "entro_cache_append_rotated"]
 
 
 def _ptr(a: np.ndarray, t):
@@ -700,3 +718,84 @@ def entro_cache_compact(cache: Cache, table: CacheTable, following: CacheTable, 
 
 def entro_cache_status(word: int) -> int:
     return int(lib().entro_cache_status(int(word)))
+
+
+# ------------------------------------------------------------------------ positions
+def entro_rotary_turns(dims: int, base: float = 10000.0, context: int = ENTRO_CONTEXT_AS_TRAINED, factor: float = 1.0, trained: float = 1.0,
+                       low: float = 1.0, high: float = 32.0) -> np.ndarray:
+    """uint64[dims / 2]: what a position turns each pair by, in 2^-64 of a turn."""
+    turns = np.zeros(dims // 2, np.uint64)
+    _check(lib().entro_rotary_turns(dims, base, context, factor, trained, low, high, _ptr(turns, C.c_uint64)), "entro_rotary_turns")
+    return turns
+
+
+class Rotary:
+    """How heads are normed and rotated. turns: int64 device tensor [dims / 2] (entro_rotary_turns' numbers), None for no dims; gains: float32
+    [head_dim], or [heads][head_dim] for one set a head, or None."""
+
+    def __init__(self, turns, dims: int, layout: int = ENTRO_ROTARY_HALVES, amplitude: float = 1.0, norm: int = ENTRO_NORM_NONE, eps: float = 1e-6,
+                 q_gain=None, k_gain=None):
+        import torch
+        _need(dims == 0 if turns is None else (turns.dtype in (torch.int64, torch.uint64) and turns.is_contiguous() and 2 * turns.numel() == dims),
+              "turns is a contiguous int64 tensor of dims / 2")
+        for g in (q_gain, k_gain):
+            _need(g is None or (g.dtype == torch.float32 and g.dim() in (1, 2) and g.is_contiguous()), "gains are float32 [head_dim] or [heads][head_dim]")
+        self.turns, self.q_gain, self.k_gain = turns, q_gain, k_gain
+        self.tensors = [x for x in (turns, q_gain, k_gain) if x is not None]
+        at, stride = (lambda x: None if x is None else x.data_ptr()), (lambda g: 0 if g is None or g.dim() == 1 else g.stride(0))
+        self.c = CRotary(at(turns), at(q_gain), at(k_gain), stride(q_gain), stride(k_gain), dims, layout, norm, eps, amplitude, 0)
+
+    def fits(self, gain, heads: int, head_dim: int):
+        _need(gain is None or tuple(gain.shape) in ((head_dim,), (heads, head_dim)), f"gains are [{head_dim}] or [{heads}][{head_dim}]")
+
+
+class RotaryRows:
+    """Rows [tokens][heads][head_dim] that are read (x) and written (y: x itself, or a tensor apart from it; None: x)."""
+
+    def __init__(self, x, y=None):
+        y = x if y is None else y
+        _need(x.shape == y.shape and x.dtype == y.dtype, "x and y have one shape and type")
+        self.x, self.y, self.device = x, y, _device_of(x, y)
+        self.c = CRotaryRows(x.data_ptr(), y.data_ptr(), *_row_strides(x, "x"), *_row_strides(y, "y"), x.shape[1], 0)
+        _need(_own_places(y), "y's elements have places of their own")
+
+
+def _run_on(device, call):
+    """call() with `device` as the current one, which is where the library launches."""
+    import torch
+    if device.index in (None, torch.cuda.current_device()):
+        return call()
+    with torch.cuda.device(device):
+        return call()
+
+
+def entro_rotate(rotary: Rotary, q: Optional[RotaryRows], k: Optional[RotaryRows], positions, stream=None):
+    """Norms and rotations of q and k (either may be None) at positions, int32 [tokens]."""
+    sides = [s for s in (q, k) if s is not None]
+    _need(len(sides) > 0, "q or k is given")
+    x = sides[0].x
+    for s, gain in ((q, rotary.q_gain), (k, rotary.k_gain)):
+        if s is not None:
+            _need(s.x.dtype == x.dtype and s.x.shape[0] == x.shape[0] and s.x.shape[2] == x.shape[2], "q and k have one type, as many tokens and dimensions")
+            rotary.fits(gain, s.x.shape[1], x.shape[2])
+    at = _ints(positions, x.shape[0], "positions")
+    device = _device_of(positions, *(t for s in sides for t in (s.x, s.y)), *rotary.tensors)
+    _need(device is not None and device.type == "cuda", "all tensors of a call lie on one GPU")
+    refs = [None if s is None else C.byref(s.c) for s in (q, k)]
+    _run_on(device, lambda: _check(lib().entro_rotate(C.byref(rotary.c), *refs, at, x.shape[0], x.shape[2], _rows_type(x, "x"), _stream_ptr(stream)),
+                                   "entro_rotate"))
+
+
+def entro_cache_append_rotated(cache: Cache, table: CacheTable, rows: CacheRows, rotary: Rotary, queries: Optional[RotaryRows] = None, stream=None):
+    """entro_cache_append of keys that are normed and rotated on their way, and `queries` normed and rotated beside them."""
+    _same_heads(cache, table, rows.k, rows.start)
+    _need(rows.k.shape[1] == cache.kv_heads, f"rows have {cache.kv_heads} heads")
+    rotary.fits(rotary.k_gain, cache.kv_heads, cache.head_dim)
+    if queries is not None:
+        x = queries.x
+        _need(x.dtype == rows.k.dtype and x.shape[0] == rows.k.shape[0] and x.shape[2] == cache.head_dim, "queries have the type, tokens and dimensions of the rows")
+        rotary.fits(rotary.q_gain, x.shape[1], cache.head_dim)
+    _on_gpu(cache, table, rows, queries, *rotary.tensors)
+    q = None if queries is None else C.byref(queries.c)
+    _run_on(cache.device, lambda: _check(lib().entro_cache_append_rotated(C.byref(cache.c), C.byref(table.c), C.byref(rows.c), C.byref(rotary.c), q,
+                                                                          _stream_ptr(stream)), "entro_cache_append_rotated"))

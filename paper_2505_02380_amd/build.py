@@ -16,7 +16,7 @@ DEVICE_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang"
                 "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument"]
 
 
-DEVICE_SOURCES = ["entro_device", "entro_compress", "entro_cache", "entro_attend"]
+DEVICE_SOURCES = ["entro_device", "entro_compress", "entro_cache", "entro_attend", "entro_rotate"]
 
 
 def sources():
