@@ -583,6 +583,37 @@ uint64_t entro_cache_attend_workspace_bytes(const entro_cache *c, const entro_ca
 entro_status entro_cache_attend(const entro_cache *c, const entro_cache_table *t, const entro_cache_query *q, void *workspace,
                                 uint64_t workspace_bytes, void *hip_stream);
 
+/* Groups of sequences that begin with the same pages: a prompt answered several times, beams, users behind one document.  Sequences
+ * first[g] .. first[g+1] - 1 of the table form group g; sequences before first[0] and from first[groups] on are in none.  `first` ascends. */
+typedef struct {
+    const int32_t *first;        /* device: [groups + 1] */
+    int32_t *shared;             /* device: [groups] tokens that the sequences of a group have in the same pages; written by entro_cache_shared,
+                                  * read by entro_cache_attend_shared */
+    uint32_t groups;
+    uint32_t max_seqs, max_shared;   /* most sequences and most shared tokens of a group: hints, as max_new and max_len */
+    uint32_t reserved;           /* 0 */
+} entro_cache_groups;
+
+/* shared[g] = page_tokens times the number of leading slots in which all rows of t in group g name the same page (one of the
+ * pool's) and hold page_tokens tokens; 0 for a group without sequences.  Pages that regroup shares are found whoever forked from whom; a program
+ * that forks only within its groups may also keep older values, as what its sequences share only grows.  (For the phase of "Latency
+ * Reduction from Huffman Coding"; no passage of the paper defines it.) */
+entro_status entro_cache_shared(const entro_cache *c, const entro_cache_table *t, const entro_cache_groups *g, void *hip_stream);
+
+/* Bytes of device workspace entro_cache_attend_shared needs for these sizes on the current device.  Only hints and sizes count, no pointer is
+ * followed.  (For the phase of "Latency Reduction from Huffman Coding"; no passage of the paper defines it.) */
+uint64_t entro_cache_attend_shared_workspace_bytes(const entro_cache *c, const entro_cache_table *t, const entro_cache_query *q,
+                                                   const entro_cache_groups *g);
+
+/* entro_cache_attend for groups of sequences: what it computes and how exactly is said there; here the tokens that a group's sequences
+ * share are read and multiplied once for all its rows, each sequence's further tokens for its own, and both are joined by their lse.
+ * shared[g] must not exceed what entro_cache_shared gives: its tokens are taken from the pages of the group's first sequence.  A query may stand
+ * among the shared tokens (then fewer are taken as shared), windows may begin there, groups may be of one sequence or none.
+ * The order of sums depends on sizes and lengths, never on the run.  ENTRO_ERR_SIZE also where groups or sequences times kv_heads reach
+ * 2^23, or sequences times q_heads 2^24.  (For the phase of "Latency Reduction from Huffman Coding"; no passage of the paper defines it.) */
+entro_status entro_cache_attend_shared(const entro_cache *c, const entro_cache_table *t, const entro_cache_query *q, const entro_cache_groups *g,
+                                       void *workspace, uint64_t workspace_bytes, void *hip_stream);
+
 /* Bytes of device workspace the two calls below need.  (This and the rest of the page tables serve the phase that "Latency Reduction
  * from Huffman Coding" is about; no passage of the paper defines it.) */
 uint64_t entro_cache_pages_workspace_bytes(const entro_cache *c, const entro_cache_table *t, const entro_cache_table *next);

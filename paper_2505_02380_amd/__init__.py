@@ -22,6 +22,7 @@ from .binding import (  # noqa: F401
     entro_cache_width, entro_cache_append, entro_cache_read, entro_cache_attend_workspace_bytes, entro_cache_attend,
     entro_cache_pages_workspace_bytes, entro_cache_regroup, entro_cache_compact, entro_cache_status,
     Rotary, RotaryRows, entro_rotary_turns, entro_rotate, entro_cache_append_rotated,
+    CacheGroups, entro_cache_shared, entro_cache_attend_shared_workspace_bytes, entro_cache_attend_shared,
     ENTRO_ROTARY_HALVES, ENTRO_ROTARY_PAIRS, ENTRO_NORM_NONE, ENTRO_NORM_RMS, ENTRO_NORM_CENTRED,
     ENTRO_CONTEXT_AS_TRAINED, ENTRO_CONTEXT_LINEAR, ENTRO_CONTEXT_BY_PARTS,
     ENTRO_UNSIGNED, ENTRO_ASYMMETRIC, ENTRO_U8, ENTRO_U4_PACKED, ENTRO_F32, ENTRO_BF16,

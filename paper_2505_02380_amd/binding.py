@@ -75,6 +75,11 @@ class CCacheQuery(C.Structure):
                 ("scale", C.c_float), ("reserved", C.c_uint32)]
 
 
+class CCacheGroups(C.Structure):
+    _fields_ = [("first", C.c_void_p), ("shared", C.c_void_p), ("groups", C.c_uint32), ("max_seqs", C.c_uint32), ("max_shared", C.c_uint32),
+                ("reserved", C.c_uint32)]
+
+
 class CRotary(C.Structure):
     _fields_ = [("turns", C.c_void_p), ("q_gain", C.c_void_p), ("k_gain", C.c_void_p), ("q_gain_stride", C.c_uint32),
                 ("k_gain_stride", C.c_uint32), ("dims", C.c_uint32), ("layout", C.c_uint32), ("norm", C.c_uint32), ("eps", C.c_float),
@@ -164,6 +169,9 @@ def lib():
                                           C.c_uint64, C.c_void_p]),
         "entro_cache_compact": (C.c_int, [kp, kt, kt, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p]),
         "entro_cache_status": (C.c_int, [C.c_int32]),
+        "entro_cache_shared": (C.c_int, [kp, kt, C.POINTER(CCacheGroups), C.c_void_p]),
+        "entro_cache_attend_shared_workspace_bytes": (C.c_uint64, [kp, kt, C.POINTER(CCacheQuery), C.POINTER(CCacheGroups)]),
+        "entro_cache_attend_shared": (C.c_int, [kp, kt, C.POINTER(CCacheQuery), C.POINTER(CCacheGroups), C.c_void_p, C.c_uint64, C.c_void_p]),
         "entro_rotary_turns": (C.c_int, [C.c_uint32, C.c_double, C.c_uint32, C.c_double, C.c_double, C.c_double, C.c_double, u64p]),
         "entro_rotate": (C.c_int, [C.POINTER(CRotary), C.POINTER(CRotaryRows), C.POINTER(CRotaryRows), C.c_void_p, C.c_uint32, C.c_uint32, C.c_int,
                                    C.c_void_p]),
@@ -187,7 +195,8 @@ EXPORTED = ["entro_quantize", "entro_build_codebook", "entro_codebook_from_count
             "entro_encoded_bytes", "entro_encode_device", "entro_encode_device_status",
             "entro_cache_width", "entro_cache_codes_bytes", "entro_cache_append", "entro_cache_read",
             "entro_cache_attend_workspace_bytes", "entro_cache_attend", "entro_cache_pages_workspace_bytes", "entro_cache_regroup",
-            "entro_cache_compact", "entro_cache_status", "entro_rotary_turns", "entro_rotate", "entro_cache_append_rotated"]
+            "entro_cache_compact", "entro_cache_status", "entro_rotary_turns", "entro_rotate", "entro_cache_append_rotated",
+            "entro_cache_shared", "entro_cache_attend_shared_workspace_bytes", "entro_cache_attend_shared"]
 
 
 def _ptr(a: np.ndarray, t):
@@ -799,3 +808,33 @@ def entro_cache_append_rotated(cache: Cache, table: CacheTable, rows: CacheRows,
     q = None if queries is None else C.byref(queries.c)
     _run_on(cache.device, lambda: _check(lib().entro_cache_append_rotated(C.byref(cache.c), C.byref(table.c), C.byref(rows.c), C.byref(rotary.c), q,
                                                                           _stream_ptr(stream)), "entro_cache_append_rotated"))
+
+
+# ---------------------------------------------------------------------------------------------------- groups behind a prefix
+class CacheGroups:
+    """Groups of sequences that begin with the same pages. first: int32 [groups + 1], ascending; shared: int32 [groups], tokens in shared pages
+    (entro_cache_shared writes it)."""
+
+    def __init__(self, first, shared, max_seqs: int, max_shared: int):
+        n = first.numel() - 1
+        _need(n > 0, "first is [groups + 1]")
+        self.first, self.shared, self.device = first, shared, _device_of(first, shared)
+        self.c = CCacheGroups(_ints(first, None, "first"), _ints(shared, n, "shared"), n, max_seqs, max_shared, 0)
+
+
+def entro_cache_shared(cache: Cache, table: CacheTable, groups: CacheGroups, stream=None):
+    """Writes groups.shared from the table."""
+    _on_gpu(cache, table, groups)
+    _run_on(cache.device, lambda: _check(lib().entro_cache_shared(C.byref(cache.c), C.byref(table.c), C.byref(groups.c), _stream_ptr(stream)),
+                                         "entro_cache_shared"))
+
+
+def entro_cache_attend_shared_workspace_bytes(cache: Cache, table: CacheTable, query: CacheQuery, groups: CacheGroups) -> int:
+    return int(lib().entro_cache_attend_shared_workspace_bytes(C.byref(cache.c), C.byref(table.c), C.byref(query.c), C.byref(groups.c)))
+
+
+def entro_cache_attend_shared(cache: Cache, table: CacheTable, query: CacheQuery, groups: CacheGroups, workspace, stream=None):
+    _same_heads(cache, table, query.q, query.start)
+    _on_gpu(cache, table, query, groups, workspace)
+    _run_on(cache.device, lambda: _check(lib().entro_cache_attend_shared(C.byref(cache.c), C.byref(table.c), C.byref(query.c), C.byref(groups.c),
+                                                                         *_workspace(workspace), _stream_ptr(stream)), "entro_cache_attend_shared"))

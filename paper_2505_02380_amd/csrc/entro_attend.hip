@@ -88,6 +88,8 @@ __device__ inline float column_sum(float v) {
 struct Tiles {
     int32_t sinks, from, count;
     __device__ int32_t at(int32_t i) const { return i < sinks ? i : from + i - sinks; }
+    // how many of them lie before `tile`
+    __device__ int32_t before(int32_t tile) const { return min(sinks, tile) + min(max(tile - from, 0), count - sinks); }
 };
 
 __device__ inline Tiles tiles_of(const Pool &p, const Query &a, int32_t first, int32_t last) {
@@ -104,9 +106,43 @@ __device__ inline Tiles tiles_of(const Pool &p, const Query &a, int32_t first, i
     return t;
 }
 
-// How the tiles of a group of rows are shared out to at most `splits` workgroups.
-__device__ inline int32_t tiles_per_split(const Query &a, int32_t count) {
-    return max((count + static_cast<int32_t>(a.splits) - 1) / static_cast<int32_t>(a.splits), static_cast<int32_t>(a.least));
+// How the tiles of a group of rows are shared out to at most `splits` workgroups, of at least `least` each.
+__device__ inline int32_t tiles_per_split(uint32_t splits, uint32_t least, int32_t count) {
+    return max((count + static_cast<int32_t>(splits) - 1) / static_cast<int32_t>(splits), static_cast<int32_t>(least));
+}
+
+__device__ inline int32_t tiles_per_split(const Query &a, int32_t count) { return tiles_per_split(a.splits, a.least, count); }
+
+// Which of the tokens that its rows see a workgroup takes: all of a sequence's, those that a group of sequences shares, or those
+// behind them.
+enum { kWhole, kShared, kOwn };
+
+// The work of a workgroup.  kWhole: s, table, head, split and the query's splits.
+struct Part {
+    Span s;                        // its rows; kShared: those of all sequences of a group, pos and length - 1 the least and the largest position
+    uint32_t table;                // the table's row that names the pages
+    uint32_t head, split;
+    uint32_t splits, least;        // as a Query's, of this kind of tokens
+    uint32_t parts, slot;          // parts of a row in the workspace, and the place of this kind's first one
+    int32_t tiles;                 // that the group shares
+    uint32_t first, last;          // sequences of the group
+};
+
+template <int MODE>
+__device__ inline uint64_t part_at(const Query &a, const Part &w, uint64_t row_and_head) {
+    return MODE == kWhole ? row_and_head * a.splits + w.split : row_and_head * w.parts + w.slot + w.split;
+}
+
+// The position of one of a group's rows.
+__device__ inline int32_t position_of(const Pool &p, const Query &a, const Part &w, uint32_t token) {
+    uint32_t lo = w.first, hi = w.last;
+    while (hi - lo > 1) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (a.start[mid] <= static_cast<int32_t>(token)) lo = mid;
+        else hi = mid;
+    }
+    const Span s = span_of(a.start, p.lengths, lo, a.tokens);
+    return s.pos + static_cast<int32_t>(token) - s.row;
 }
 
 template <typename T> __device__ inline float load_as_f32(const T *p);
@@ -155,32 +191,43 @@ __device__ inline int exponent_of(float most) { return max(static_cast<int>((__f
 // asked for two tiles ahead, a tile's codes as soon as the last tile's have been used. Measured: 131072 tokens of 8 heads of 128
 // 55 us with the join (4.9 TB/s), 32 sequences in a window of 4096 with 32 heads of 96 142 us (5.4 TB/s), 64 sequences of
 // up to 8192 tokens 128 us (4.3 TB/s: sequences of different lengths, see shape_of); in fp32 the first of these 54 us, the last 127.
-template <int W, typename T>
-__global__ __launch_bounds__(kWG, W > 128 ? 1 : 2) void k_attend_few(Pool p, Query a) {
+template <int W>
+struct FewLds {
+    float merge_o[4][16][W + 4], merge_m[4][16], merge_l[4][16];
+};
+
+template <int W, typename T, int MODE>
+__device__ __forceinline__ void attend_few(const Pool &p, const Query &a, const Part &w, FewLds<W> &lds) {
     constexpr int kParts = sizeof(T) == 2 ? 1 : 3;         // bf16 numbers that make an element of q in the first product
     constexpr int kWeights = sizeof(T) == 2 ? 2 : 3;       // bf16 numbers that make a weight of the second
     constexpr int kFull = W / 64, kRest = W % 64 ? 1 : 0;   // loads of 64 dimensions of 16 tokens, and of 32
     constexpr int kDims = W / 16;
-    __shared__ float merge_o[4][16][W + 4];
-    __shared__ float merge_m[4][16], merge_l[4][16];
+    auto &merge_o = lds.merge_o;
+    auto &merge_m = lds.merge_m, &merge_l = lds.merge_l;
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15u;
-    // Workgroups go to the XCDs in turn. Those of one XCD take the key heads of the same sequence and split, whose codes lie side by side, and
-    // the splits of a sequence go to different XCDs, so that long sequences do not meet on one.
-    const uint32_t r = p.seqs < 8 ? blockIdx.x : blockIdx.x / 8, head = r % p.kv_heads, split = r / p.kv_heads % a.splits, block = r / p.kv_heads / a.splits;
-    const uint32_t b = p.seqs < 8 ? block : 8 * block + ((blockIdx.x - split) & 7u);
-    if (b >= p.seqs) return;
-    const Span s = span_of(a.start, p.lengths, b, a.tokens);
+    const uint32_t b = w.table, head = w.head, split = w.split;
+    const Span s = w.s;
     const uint64_t page_bytes = uint64_t{W} << p.page_shift, page_stride = page_bytes * p.kv_heads;
     const uint8_t *k_head = p.k + head * page_bytes, *v_head = p.v + head * page_bytes;
     const float *ks_head = p.k_scale + head, *vs_head = p.v_scale + head;
     const uint32_t in_page = (1u << p.page_shift) - 1;
     const int64_t rows = int64_t{s.count} * a.group;
     for (int64_t row0 = 0; row0 < rows; row0 += 16) {
-        const int32_t first = s.pos + static_cast<int32_t>(row0 / a.group);
-        const int32_t last = s.pos + static_cast<int32_t>(min(row0 + 15, rows - 1) / a.group);
+        const int32_t first = MODE == kShared ? s.pos : s.pos + static_cast<int32_t>(row0 / a.group);
+        const int32_t last = MODE == kShared ? s.length - 1 : s.pos + static_cast<int32_t>(min(row0 + 15, rows - 1) / a.group);
         const Tiles tiles = tiles_of(p, a, first, last);
-        const int32_t per = tiles_per_split(a, tiles.count), begin = static_cast<int32_t>(split) * per, end = min(begin + per, tiles.count);
-        if (begin >= end && split > 0) continue;
+        const int32_t cut = MODE == kWhole ? 0 : tiles.before(w.tiles), from = MODE == kOwn ? cut : 0, until = MODE == kShared ? cut : tiles.count;
+        const int32_t per = MODE == kWhole ? tiles_per_split(a, tiles.count) : tiles_per_split(w.splits, w.least, until - from);
+        const int32_t begin = from + static_cast<int32_t>(split) * per, end = min(begin + per, until);
+        if (MODE == kWhole && begin >= end && split > 0) continue;
+        if (MODE != kWhole && begin >= end) {
+            if (tid < 16 && row0 + tid < rows) {
+                const uint32_t token = static_cast<uint32_t>(s.row) + static_cast<uint32_t>((row0 + tid) / a.group);
+                const uint32_t q_head = head * a.group + static_cast<uint32_t>((row0 + tid) % a.group);
+                a.part_lse[part_at<MODE>(a, w, uint64_t{token} * a.q_heads + q_head)] = -INFINITY;
+            }
+            continue;
+        }
     // A tile's codes and scales as this lane has them: keys of the tokens 16 (c / 4) .., values of the tokens 16 g ..  As soon as a
     // tile's keys have been multiplied the next tile's are asked for, and so for the values; page numbers come a tile earlier
     // still, so that nothing waits for them.  (A second set of registers for the codes does not fit.)
@@ -221,8 +268,8 @@ __global__ __launch_bounds__(kWG, W > 128 ? 1 : 2) void k_attend_few(Pool p, Que
     const bool mine = my_row < rows;
     const uint32_t my_token = static_cast<uint32_t>(s.row) + static_cast<uint32_t>((mine ? my_row : row0) / a.group);
     const uint32_t my_head = head * a.group + static_cast<uint32_t>((mine ? my_row : row0) % a.group);
-    const int32_t my_pos = s.pos + static_cast<int32_t>(my_token) - s.row;
-    
+    const int32_t my_pos = MODE != kShared ? s.pos + static_cast<int32_t>(my_token) - s.row : a.window ? position_of(p, a, w, my_token) : s.pos;
+
     bf16x8 q[W / 32][kParts];
     float q_factor;
     {
@@ -310,7 +357,7 @@ __global__ __launch_bounds__(kWG, W > 128 ? 1 : 2) void k_attend_few(Pool p, Que
             for (int d = 0; d < kDims; ++d) o[d] *= by;
         }
         const float base = m == -INFINITY ? 0.0f : m + kRise;
-        bf16x8 w[2][kWeights];
+        bf16x8 weights[2][kWeights];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             float x[8];
@@ -320,15 +367,15 @@ __global__ __launch_bounds__(kWG, W > 128 ? 1 : 2) void k_attend_few(Pool p, Que
                 l += e;
                 x[j] = e * scale;
             }
-            split_factors<kWeights>(x, w[h]);
+            split_factors<kWeights>(x, weights[h]);
         }
 #pragma unroll
         for (int d = 0; d < kDims; ++d) {
             const bf16x8 v0 = eight_values(vc[d][0], vc[d][1]), v1 = eight_values(vc[d][2], vc[d][3]);
 #pragma unroll
             for (int n = 0; n < kWeights; ++n) {
-                o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, w[0][n], o[d], 0, 0, 0);
-                o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, w[1][n], o[d], 0, 0, 0);
+                o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, weights[0][n], o[d], 0, 0, 0);
+                o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, weights[1][n], o[d], 0, 0, 0);
             }
         }
         ask_values(i + 4);
@@ -358,17 +405,33 @@ __global__ __launch_bounds__(kWG, W > 128 ? 1 : 2) void k_attend_few(Pool p, Que
                 float x = 0.0f;
                 for (int i = 0; i < 4; ++i) x += merge_o[i][r][d] * share[i];
                 x = sum == sum ? x * inv : sum;
-                if (a.splits == 1)
+                if (MODE == kWhole && a.splits == 1)
                     store_as(static_cast<T *>(a.out) + token * a.out_token_stride + q_head * a.out_head_stride + d, x);
                 else
-                    a.part_o[(at * a.splits + split) * W + d] = x;
+                    a.part_o[part_at<MODE>(a, w, at) * W + d] = x;
             }
             if (d0 == 0) {
-                if (a.splits > 1) a.part_lse[at * a.splits + split] = lse;
+                if (MODE != kWhole || a.splits > 1) a.part_lse[part_at<MODE>(a, w, at)] = lse;
                 else if (a.lse) a.lse[at] = lse * kLn2;
             }
         }
     }
+}
+
+template <int W, typename T>
+__global__ __launch_bounds__(kWG, W > 128 ? 1 : 2) void k_attend_few(Pool p, Query a) {
+    __shared__ FewLds<W> lds;
+    // Workgroups go to the XCDs in turn. Those of one XCD take the key heads of the same sequence and split, whose codes lie side by side, and
+    // the splits of a sequence go to different XCDs, so that long sequences do not meet on one.
+    const uint32_t r = p.seqs < 8 ? blockIdx.x : blockIdx.x / 8, head = r % p.kv_heads, split = r / p.kv_heads % a.splits, block = r / p.kv_heads / a.splits;
+    const uint32_t b = p.seqs < 8 ? block : 8 * block + ((blockIdx.x - split) & 7u);
+    if (b >= p.seqs) return;
+    Part w = {};
+    w.s = span_of(a.start, p.lengths, b, a.tokens);
+    w.table = b;
+    w.head = head;
+    w.split = split;
+    attend_few<W, T, kWhole>(p, a, w, lds);
 }
 
 // ----------------------------------------------------------------------------------------------------- many rows: prompts
@@ -388,21 +451,27 @@ __global__ __launch_bounds__(kWG, W > 128 ? 1 : 2) void k_attend_few(Pool p, Que
 // way to LDS 71. fp32 rows take twice the matrix instructions, and one workgroup a compute unit (382 registers at 96 dimensions): 98 row
 // groups of 4 key heads of 80 dimensions, each over about 1100 tokens, 182 us. Registers that do not fit are kept in memory: at 256 dimensions
 // 162 for fp32 and 30 for bf16, at 192 35 for fp32, at 96 and 128 2 and 5 for bf16.
-template <int W, typename T>
-__global__ __launch_bounds__(kWG, sizeof(T) == 2 && W <= 128 ? 2 : 1) void k_attend_many(Pool p, Query a, uint32_t row_tiles) {
+template <int W>
+struct ManyLds {
+    static constexpr int kKeyRow = 2 * W + 16, kValueRow = 2 * kTile + 16;   // bytes
+    __attribute__((aligned(16))) uint8_t key[2][kTile * kKeyRow], value[2][W * kValueRow];
+    f32x4 ks[2], vs[2];
+    int32_t ok[2][4];
+};
+
+template <int W, typename T, int MODE>
+__device__ __forceinline__ void attend_many(const Pool &p, const Query &a, const Part &w, uint32_t tile_from_end, uint32_t row_tiles, ManyLds<W> &lds) {
     constexpr int kThreads = kWG, kRows = kManyRows;
     constexpr int kParts = sizeof(T) == 2 ? 1 : 3, kWeights = sizeof(T) == 2 ? 2 : 3;
     constexpr int kChunks = (W * 4 + kThreads - 1) / kThreads;      // pieces of 16 codes a thread turns, of keys and of values
-    constexpr int kKeyRow = 2 * W + 16, kValueRow = 2 * kTile + 16;   // bytes
-    constexpr int kKeyTile = kTile * kKeyRow, kValueTile = W * kValueRow;
-    __shared__ __attribute__((aligned(16))) uint8_t key_lds[2][kKeyTile], value_lds[2][kValueTile];
-    __shared__ f32x4 tile_ks[2], tile_vs[2];
-    __shared__ int32_t tile_ok[2][4];
+    constexpr int kKeyRow = ManyLds<W>::kKeyRow, kValueRow = ManyLds<W>::kValueRow;
+    auto &key_lds = lds.key;
+    auto &value_lds = lds.value;
+    auto &tile_ks = lds.ks, &tile_vs = lds.vs;
+    auto &tile_ok = lds.ok;
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, c = lane & 31u;
-    // workgroups of one key head follow each other at multiples of the number of heads: with 8 heads, on one XCD and its L2
-    const uint32_t units = p.seqs * p.kv_heads, unit = blockIdx.x % units, head = unit % p.kv_heads, b = unit / p.kv_heads;
-    const uint32_t split = blockIdx.x / units % a.splits, tile_from_end = blockIdx.x / units / a.splits;
-    const Span s = span_of(a.start, p.lengths, b, a.tokens);
+    const uint32_t b = w.table, head = w.head, split = w.split;
+    const Span s = w.s;
     const uint64_t page_bytes = uint64_t{W} << p.page_shift, page_stride = page_bytes * p.kv_heads;
     const uint8_t *k_head = p.k + head * page_bytes, *v_head = p.v + head * page_bytes;
     const uint32_t in_page = (1u << p.page_shift) - 1;
@@ -411,20 +480,26 @@ __global__ __launch_bounds__(kWG, sizeof(T) == 2 && W <= 128 ? 2 : 1) void k_att
     // the last rows see the most tokens: they come first
     for (int64_t group = groups - 1 - tile_from_end; group >= 0; group -= row_tiles) {
         const int64_t row0 = group * kRows;
-        const int32_t first = s.pos + static_cast<int32_t>(row0 / a.group);
-        const int32_t last = s.pos + static_cast<int32_t>(min(row0 + kRows - 1, rows - 1) / a.group);
+        const int32_t first = MODE == kShared ? s.pos : s.pos + static_cast<int32_t>(row0 / a.group);
+        const int32_t last = MODE == kShared ? s.length - 1 : s.pos + static_cast<int32_t>(min(row0 + kRows - 1, rows - 1) / a.group);
         const Tiles tiles = tiles_of(p, a, first, last);
-        const int32_t per = tiles_per_split(a, tiles.count), begin = static_cast<int32_t>(split) * per, end = min(begin + per, tiles.count);
-        if (begin >= end && split > 0) continue;
+        const int32_t cut = MODE == kWhole ? 0 : tiles.before(w.tiles), from = MODE == kOwn ? cut : 0, until = MODE == kShared ? cut : tiles.count;
+        const int32_t per = MODE == kWhole ? tiles_per_split(a, tiles.count) : tiles_per_split(w.splits, w.least, until - from);
+        const int32_t begin = from + static_cast<int32_t>(split) * per, end = min(begin + per, until);
+        if (MODE == kWhole && begin >= end && split > 0) continue;
         const int64_t my_row = row0 + 32 * wave + c;
         const bool mine = my_row < rows;
         const uint32_t my_token = static_cast<uint32_t>(s.row) + static_cast<uint32_t>((mine ? my_row : row0) / a.group);
         const uint32_t my_head = head * a.group + static_cast<uint32_t>((mine ? my_row : row0) % a.group);
-        const int32_t my_pos = mine ? s.pos + static_cast<int32_t>(my_token) - s.row : -1;
+        if (MODE != kWhole && begin >= end) {
+            if (mine && h == 0) a.part_lse[part_at<MODE>(a, w, uint64_t{my_token} * a.q_heads + my_head)] = -INFINITY;
+            continue;
+        }
+        const int32_t my_pos = !mine ? -1 : MODE != kShared ? s.pos + static_cast<int32_t>(my_token) - s.row : a.window ? position_of(p, a, w, my_token) : s.pos;
         // positions of the wavefront's rows
         const int64_t wave_row = row0 + 32 * wave;
-        const int32_t wave_first = s.pos + static_cast<int32_t>(wave_row / a.group);
-        const int32_t wave_last = wave_row < rows ? s.pos + static_cast<int32_t>(min(wave_row + 31, rows - 1) / a.group) : -1;
+        const int32_t wave_first = MODE == kShared ? first : s.pos + static_cast<int32_t>(wave_row / a.group);
+        const int32_t wave_last = wave_row >= rows ? -1 : MODE == kShared ? last : s.pos + static_cast<int32_t>(min(wave_row + 31, rows - 1) / a.group);
         bf16x8 q[W / 16][kParts];
         float q_factor;
         {
@@ -520,7 +595,7 @@ __global__ __launch_bounds__(kWG, sizeof(T) == 2 && W <= 128 ? 2 : 1) void k_att
         // What the matrix units take from LDS is asked for kAhead pieces before it is used.
         constexpr int kAhead = 4;
         // the second product: weights of four times 16 tokens
-        const auto add_values = [&](const bf16x8 (*w)[kWeights], int half) {
+        const auto add_values = [&](const bf16x8 (*weights)[kWeights], int half) {
             const uint8_t *at = value_lds[half] + c * kValueRow + 16 * h;
             const auto piece = [&](int i) { return *reinterpret_cast<const bf16x8 *>(at + 32 * (i % kDims) * kValueRow + 32 * (i / kDims)); };
             bf16x8 v[kAhead];
@@ -531,7 +606,7 @@ __global__ __launch_bounds__(kWG, sizeof(T) == 2 && W <= 128 ? 2 : 1) void k_att
                 const bf16x8 now = v[i % kAhead];
                 if (i + kAhead < 4 * kDims) v[i % kAhead] = piece(i + kAhead);
 #pragma unroll
-                for (int n = 0; n < kWeights; ++n) o[i % kDims] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(now, w[i / kDims][n], o[i % kDims], 0, 0, 0);
+                for (int n = 0; n < kWeights; ++n) o[i % kDims] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(now, weights[i / kDims][n], o[i % kDims], 0, 0, 0);
             }
         };
         for (int32_t i = begin; i < end; ++i) {
@@ -592,7 +667,7 @@ __global__ __launch_bounds__(kWG, sizeof(T) == 2 && W <= 128 ? 2 : 1) void k_att
                     for (int d = 0; d < kDims; ++d) o[d] *= by;
                 }
                 const float base = m == -INFINITY ? 0.0f : m + kRise;
-                bf16x8 w[4][kWeights];
+                bf16x8 weights[4][kWeights];
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {       // 16 tokens
                     float x[8];
@@ -602,9 +677,9 @@ __global__ __launch_bounds__(kWG, sizeof(T) == 2 && W <= 128 ? 2 : 1) void k_att
                         l += e;
                         x[j] = e * vf[g];
                     }
-                    split_factors<kWeights>(x, w[g]);
+                    split_factors<kWeights>(x, weights[g]);
                 }
-                add_values(w, half);
+                add_values(weights, half);
             }
             __syncthreads();
         }
@@ -614,22 +689,35 @@ __global__ __launch_bounds__(kWG, sizeof(T) == 2 && W <= 128 ? 2 : 1) void k_att
             const float lse = l > 0.0f ? base + __builtin_amdgcn_logf(l * kUnit) : l == l ? -INFINITY : l;
             const uint64_t at = uint64_t{my_token} * a.q_heads + my_head;
             T *out = static_cast<T *>(a.out) + my_token * a.out_token_stride + my_head * a.out_head_stride;
-            float *part = a.part_o + (at * a.splits + split) * W;
+            float *part = a.part_o + part_at<MODE>(a, w, at) * W;
 #pragma unroll
             for (int d = 0; d < kDims; ++d)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
                     const uint32_t dim = 32 * d + 8 * (j / 4) + 4 * h + (j & 3);
                     const float x = l == l ? o[d][j] * inv : l;
-                    if (a.splits > 1) part[dim] = x;
+                    if (MODE != kWhole || a.splits > 1) part[dim] = x;
                     else if (dim < p.head_dim) store_as(out + dim, x);
                 }
             if (h == 0) {
-                if (a.splits > 1) a.part_lse[at * a.splits + split] = lse;
+                if (MODE != kWhole || a.splits > 1) a.part_lse[part_at<MODE>(a, w, at)] = lse;
                 else if (a.lse) a.lse[at] = lse * kLn2;
             }
         }
     }
+}
+
+template <int W, typename T>
+__global__ __launch_bounds__(kWG, sizeof(T) == 2 && W <= 128 ? 2 : 1) void k_attend_many(Pool p, Query a, uint32_t row_tiles) {
+    __shared__ ManyLds<W> lds;
+    // workgroups of one key head follow each other at multiples of the number of heads: with 8 heads, on one XCD and its L2
+    const uint32_t units = p.seqs * p.kv_heads, unit = blockIdx.x % units;
+    Part w = {};
+    w.head = unit % p.kv_heads;
+    w.table = unit / p.kv_heads;
+    w.split = blockIdx.x / units % a.splits;
+    w.s = span_of(a.start, p.lengths, w.table, a.tokens);
+    attend_many<W, T, kWhole>(p, a, w, blockIdx.x / units / a.splits, row_tiles, lds);
 }
 
 // Joins the parts of rows whose tiles were split. A workgroup per row and head: its lanes stand for four dimensions each, and as often as
@@ -690,8 +778,9 @@ __global__ __launch_bounds__(kWG) void k_attend_join(Pool p, Query a) {
     }
 }
 
-// The same for many rows in a few parts: a wavefront per row and head, no more than a lane a part.
-template <int W, typename T>
+// The same for many rows in a few parts: a wavefront per row and head, no more than a lane a part.  Behind k_attend_shared, ALL: every part
+// has its lse, minus infinity where it saw nothing and left its sums unwritten.
+template <int W, typename T, bool ALL = false>
 __global__ __launch_bounds__(kWG) void k_attend_join_rows(Pool p, Query a) {
     constexpr uint32_t kLanes = W / 4, kSets = 64 / kLanes;
     const uint32_t lane = threadIdx.x & 63u, set = lane / kLanes, d = lane % kLanes;
@@ -702,11 +791,14 @@ __global__ __launch_bounds__(kWG) void k_attend_join_rows(Pool p, Query a) {
     for (int32_t nth = static_cast<int32_t>(blockIdx.y); nth < s.count; nth += static_cast<int32_t>(gridDim.y)) {
         const uint32_t token = static_cast<uint32_t>(s.row + nth);
         const uint64_t at = uint64_t{token} * a.q_heads + h;
-        const int64_t row0 = (int64_t{nth} * a.group + h % a.group) / kManyRows * kManyRows;
-        const Tiles tiles = tiles_of(p, a, s.pos + static_cast<int32_t>(row0 / a.group),
-                                     s.pos + static_cast<int32_t>(min(row0 + kManyRows - 1, rows - 1) / a.group));
-        const int32_t per = tiles_per_split(a, tiles.count);
-        const uint32_t parts = static_cast<uint32_t>(max((tiles.count + per - 1) / per, 1));
+        uint32_t parts = a.splits;
+        if (!ALL) {
+            const int64_t row0 = (int64_t{nth} * a.group + h % a.group) / kManyRows * kManyRows;
+            const Tiles tiles = tiles_of(p, a, s.pos + static_cast<int32_t>(row0 / a.group),
+                                         s.pos + static_cast<int32_t>(min(row0 + kManyRows - 1, rows - 1) / a.group));
+            const int32_t per = tiles_per_split(a, tiles.count);
+            parts = static_cast<uint32_t>(max((tiles.count + per - 1) / per, 1));
+        }
         const float mine = lane < parts ? a.part_lse[at * a.splits + lane] : -INFINITY;
         float most = mine;
         for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
@@ -718,7 +810,7 @@ __global__ __launch_bounds__(kWG) void k_attend_join_rows(Pool p, Query a) {
         for (uint32_t i0 = 0; i0 < parts; i0 += kSets) {
             const uint32_t i = i0 + set;
             const float by = __shfl(share, static_cast<int>(min(i, 63u)));
-            if (set < kSets && i < parts) x += part[i * kLanes + d] * by;
+            if (set < kSets && i < parts && (!ALL || by != 0.0f)) x += part[i * kLanes + d] * by;
         }
 #pragma unroll
         for (uint32_t i = 1; i < kSets; ++i)
@@ -736,6 +828,301 @@ __global__ __launch_bounds__(kWG) void k_attend_join_rows(Pool p, Query a) {
         if (lane == 0 && a.lse) a.lse[at] = sum > 0.0f ? (base + __builtin_amdgcn_logf(sum)) * kLn2 : (sum == sum ? -INFINITY : sum);
     }
 }
+
+// ---------------------------------------------------------------------------------------- groups of sequences behind a prefix
+//
+// The tokens that a group's sequences share are multiplied with all its rows together (tiles of 16 rows, or 128 of many), so that their codes
+// are read, turned and multiplied once and not once a sequence; every sequence's further tokens go by the same launch's other
+// workgroups, and k_attend_join_rows brings the parts of a row together.  What is shared is rounded down to whole tiles, and to
+// what all of the group's rows see where there is no window; the rest of it is taken as each sequence's own.
+struct Groups {
+    const int32_t *first, *shared;
+    uint32_t groups;
+    uint32_t blocks;                         // workgroups for shared tokens: they come first
+    uint32_t row_tiles, splits, least;       // of those
+    uint32_t own_tiles, own_splits, own_least;   // own_tiles: 0 where few rows have a kernel of their own
+};
+
+// The group of sequence b, or a number that is none.  (All lanes, 64 of the ascending starts at a time.)
+__device__ inline uint32_t group_of(const Groups &g, uint32_t b) {
+    const uint32_t lane = threadIdx.x & 63u;
+    const int32_t at = static_cast<int32_t>(b);
+    uint32_t lo = 0, n = g.groups + 1;
+    while (n > 64) {
+        const uint32_t step = (n + 63) / 64, i = lo + min(lane * step, n - 1);
+        const uint32_t below = static_cast<uint32_t>(__builtin_popcountll(__ballot(lane * step < n && g.first[i] <= at)));
+        if (below == 0) return g.groups;
+        lo += (below - 1) * step;
+        n = min(step, n - (below - 1) * step);
+    }
+    const uint32_t below = static_cast<uint32_t>(__builtin_popcountll(__ballot(lane < n && g.first[lo + min(lane, n - 1)] <= at)));
+    return below == 0 ? g.groups : lo + below - 1;
+}
+
+// Sequences, rows and shared tiles of group `nth`.  `lds`: two numbers a wavefront.
+__device__ inline void take_group(const Pool &p, const Query &a, const Groups &g, uint32_t nth, int32_t *lds, Part *w) {
+    const uint32_t tid = threadIdx.x;
+    const int32_t seqs = static_cast<int32_t>(p.seqs), rows = static_cast<int32_t>(a.tokens);
+    const int32_t first = min(max(g.first[nth], 0), seqs), last = min(max(g.first[nth + 1], first), seqs);
+    int32_t least = 0x7fffffff, most = -1;
+    for (int32_t b = first + static_cast<int32_t>(tid); b < last; b += kWG) {
+        const Span s = span_of(a.start, p.lengths, static_cast<uint32_t>(b), a.tokens);
+        if (s.count) least = min(least, s.pos), most = max(most, s.length - 1);
+    }
+    for (int o = 32; o; o >>= 1) least = min(least, __shfl_xor(least, o)), most = max(most, __shfl_xor(most, o));
+    if ((tid & 63u) == 0) lds[2 * (tid >> 6)] = least, lds[2 * (tid >> 6) + 1] = most;
+    __syncthreads();
+    for (int i = 0; i < kWG / 64; ++i) least = min(least, lds[2 * i]), most = max(most, lds[2 * i + 1]);
+    __syncthreads();
+    const int64_t slots = int64_t{p.stride} << p.page_shift;
+    const int64_t tokens = most < 0 ? 0 : min(min(int64_t{g.shared[nth]}, slots), int64_t{least} + 1);
+    w->tiles = tokens < kTile ? 0 : static_cast<int32_t>(tokens / kTile);
+    w->first = static_cast<uint32_t>(first);
+    w->last = static_cast<uint32_t>(last);
+    w->s.row = min(max(a.start[first], 0), rows);
+    w->s.count = first < last ? min(max(a.start[last], w->s.row), rows) - w->s.row : 0;
+    w->s.pos = least;
+    w->s.length = most + 1;
+}
+
+template <int W, bool MANY> struct SharedLds {
+    union {
+        FewLds<W> few;
+        ManyLds<W> many;
+        int32_t group[2 * kWG / 64];
+    };
+};
+template <int W> struct SharedLds<W, false> {
+    union {
+        FewLds<W> few;
+        int32_t group[2 * kWG / 64];
+    };
+};
+
+template <int W, typename T, bool MANY>
+__global__ __launch_bounds__(kWG, MANY ? (sizeof(T) == 2 && W <= 128 ? 2 : 1) : (W > 128 ? 1 : 2)) void k_attend_shared(Pool p, Query a, Groups g) {
+    __shared__ SharedLds<W, MANY> lds;
+    Part w = {};
+    w.parts = g.splits + g.own_splits;
+    if (blockIdx.x < g.blocks) {
+        // the row tiles and splits of a key head follow each other at multiples of the number of units: with 8 heads, on one XCD and its L2
+        const uint32_t units = g.groups * p.kv_heads, unit = blockIdx.x % units;
+        w.head = unit % p.kv_heads;
+        w.split = blockIdx.x / units % g.splits;
+        w.splits = g.splits;
+        w.least = g.least;
+        take_group(p, a, g, unit / p.kv_heads, lds.group, &w);
+        if (w.s.count == 0) return;
+        w.table = w.first;
+        if constexpr (MANY) attend_many<W, T, kShared>(p, a, w, blockIdx.x / units / g.splits, g.row_tiles, lds.many);
+        else attend_few<W, T, kShared>(p, a, w, lds.few);
+        return;
+    }
+    const uint32_t r = blockIdx.x - g.blocks, head = r % p.kv_heads, split = r / p.kv_heads % g.own_splits, rest = r / p.kv_heads / g.own_splits;
+    const uint32_t b = rest % p.seqs;
+    const Span s = span_of(a.start, p.lengths, b, a.tokens);
+    if (s.count == 0) return;
+    const uint32_t nth = group_of(g, b);
+    if (nth < g.groups) {
+        take_group(p, a, g, nth, lds.group, &w);
+    } else if (split == 0) {                       // in no group: it has no shared parts
+        const uint64_t count = uint64_t{static_cast<uint32_t>(s.count)} * a.group * g.splits;
+        for (uint64_t i = uint64_t{rest / p.seqs} * kWG + threadIdx.x; i < count; i += uint64_t{max(g.own_tiles, 1u)} * kWG) {
+            const uint64_t row = i / g.splits, token = static_cast<uint32_t>(s.row) + row / a.group;
+            a.part_lse[(token * a.q_heads + head * a.group + row % a.group) * w.parts + i % g.splits] = -INFINITY;
+        }
+    }
+    w.s = s;
+    w.table = b;
+    w.head = head;
+    w.split = split;
+    w.splits = g.own_splits;
+    w.least = g.own_least;
+    w.slot = g.splits;
+    if constexpr (MANY) {
+        if (g.own_tiles) {
+            attend_many<W, T, kOwn>(p, a, w, rest / p.seqs, g.own_tiles, lds.many);
+            return;
+        }
+    }
+    attend_few<W, T, kOwn>(p, a, w, lds.few);
+}
+
+// Tokens in leading pages that a group's rows share: a workgroup a group, slots in steps of kWG until some row parts.
+__global__ __launch_bounds__(kWG) void k_shared(Pool p, const int32_t *first, int32_t *shared, uint32_t groups) {
+    __shared__ int32_t lds[kWG / 64];
+    const uint32_t tid = threadIdx.x;
+    const int32_t seqs = static_cast<int32_t>(p.seqs);
+    for (uint32_t g = blockIdx.x; g < groups; g += gridDim.x) {
+        const int32_t begin = min(max(first[g], 0), seqs), end = min(max(first[g + 1], begin), seqs);
+        int32_t full = begin < end ? static_cast<int32_t>(p.stride) : 0;
+        for (int32_t b = begin + static_cast<int32_t>(tid); b < end; b += kWG) full = min(full, max(p.lengths[b], 0) >> p.page_shift);
+        for (int o = 32; o; o >>= 1) full = min(full, __shfl_xor(full, o));
+        __syncthreads();
+        if ((tid & 63u) == 0) lds[tid >> 6] = full;
+        __syncthreads();
+        for (int i = 0; i < kWG / 64; ++i) full = min(full, lds[i]);
+        int32_t same = full;                       // the first slot in which they part
+        for (int32_t s0 = 0; s0 < full && same == full; s0 += kWG) {
+            const int32_t s = s0 + static_cast<int32_t>(tid);
+            bool parts = false;
+            if (s < full) {
+                const int32_t *column = p.slots + s;
+                const int32_t id = column[uint64_t{static_cast<uint32_t>(begin)} * p.stride];
+                parts = static_cast<uint32_t>(id) >= p.pages;
+                for (int32_t b = begin + 1; b < end; ++b) parts |= column[uint64_t{static_cast<uint32_t>(b)} * p.stride] != id;
+            }
+            int32_t at = parts ? s : full;
+            for (int o = 32; o; o >>= 1) at = min(at, __shfl_xor(at, o));
+            __syncthreads();
+            if ((tid & 63u) == 0) lds[tid >> 6] = at;
+            __syncthreads();
+            for (int i = 0; i < kWG / 64; ++i) same = min(same, lds[i]);
+        }
+        if (tid == 0) shared[g] = same << p.page_shift;
+    }
+}
+
+// defined below
+using QueryCheck = entro_status(const entro_cache *, const entro_cache_query *);
+QueryCheck check_query, check_query_sizes;
+int compute_units();
+
+entro_status check_groups_sizes(const entro_cache_groups *g) {
+    if (!g) return ENTRO_ERR_NULL;
+    return g->groups == 0 || g->groups > 0x7ffffffeu ? ENTRO_ERR_SIZE : ENTRO_OK;
+}
+
+entro_status check_groups(const entro_cache_groups *g) {
+    if (const entro_status s = check_groups_sizes(g)) return s;
+    if (!g->first || !g->shared) return ENTRO_ERR_NULL;
+    return aligned16(g->first) && aligned16(g->shared) ? ENTRO_OK : ENTRO_ERR_ALIGN;
+}
+
+constexpr uint64_t kHalfGroups = kMostGroups / 2;     // workgroups for shared and for own tokens
+constexpr uint32_t kMostShared = 48, kMostOwn = 16;   // parts of either: the join has a lane for each
+
+struct SharedShape {
+    bool many;
+    Groups g;
+    uint64_t bytes;
+    uint32_t join_rows;
+};
+
+uint64_t tiles_in(uint64_t tokens, const entro_cache_query *q, uint64_t rows) {
+    const uint64_t seen = uint64_t{q->window} + q->sinks + rows + 2 * kTile;
+    return ((q->window && tokens > seen ? seen : tokens) + kTile - 1) / kTile;
+}
+
+uint32_t between(uint64_t x, uint64_t lo, uint64_t hi) { return static_cast<uint32_t>(x > hi ? hi : x < lo ? lo : x); }
+
+// How far the tokens of either kind are split.  Hints may say anything: the kernels' own loops cover the rest.
+SharedShape shared_shape_of(const entro_cache *c, const entro_cache_table *t, const entro_cache_query *q, const entro_cache_groups *groups) {
+    SharedShape s = {};
+    const uint32_t max_new = between(q->max_new, 1, q->tokens < 1 ? 1 : q->tokens), group = q->q_heads / c->kv_heads;
+    const uint64_t seqs = between(groups->max_seqs, 1, t->seqs), own_rows = uint64_t{max_new} * group;
+    const uint64_t all = seqs * max_new, rows = (all < q->tokens ? all : q->tokens) * group;
+    const uint64_t shared = groups->max_shared < q->max_len ? groups->max_shared : q->max_len;
+    const uint64_t tiles = tiles_in(shared, q, max_new), own_tiles = tiles_in(uint64_t{q->max_len} - shared + kTile, q, max_new);
+    const uint64_t cus = static_cast<uint64_t>(compute_units()), units = uint64_t{groups->groups} * c->kv_heads, own_units = uint64_t{t->seqs} * c->kv_heads;
+    s.many = rows > 32;
+    s.join_rows = max_new > 65535 ? 65535 : max_new;
+    s.g.groups = groups->groups;
+    s.g.row_tiles = s.many ? between((rows + kManyRows - 1) / kManyRows, 1, kHalfGroups / units) : 1;
+    const uint64_t fill = units * s.g.row_tiles;
+    const uint64_t want = (cus * 2 + fill - 1) / fill, can = s.many ? tiles / 4 : tiles / 8;
+    uint64_t fit = kHalfGroups / fill;
+    s.g.splits = between(want < can ? want : can, 1, fit < kMostShared ? fit : kMostShared);
+    s.g.least = between((tiles + s.g.splits - 1) / s.g.splits, 1, 0x7fffffff);
+    s.g.blocks = static_cast<uint32_t>(fill * s.g.splits);
+    const bool own_many = s.many && own_rows > 32;
+    s.g.own_tiles = own_many ? between((own_rows + kManyRows - 1) / kManyRows, 1, kHalfGroups / own_units) : 0;
+    const uint64_t own_fill = own_units * (own_many ? s.g.own_tiles : 1);
+    const uint64_t own_want = (cus * 2 + own_fill - 1) / own_fill, own_can = own_tiles < 24 ? 1 : own_tiles / 8;
+    fit = kHalfGroups / own_fill;
+    s.g.own_splits = between(own_want < own_can ? own_want : own_can, 1, fit < kMostOwn ? fit : kMostOwn);
+    s.g.own_least = between((own_tiles + s.g.own_splits - 1) / s.g.own_splits, 1, 0x7fffffff);
+    s.bytes = uint64_t{q->tokens} * q->q_heads * (s.g.splits + s.g.own_splits) * (entro_cache_width(c->head_dim) + 1) * 4;
+    return s;
+}
+
+template <int W, typename T>
+void launch_shared(const Pool &p, const Query &a, const SharedShape &s, hipStream_t st) {
+    const uint32_t own = p.seqs * p.kv_heads * s.g.own_splits * (s.g.own_tiles ? s.g.own_tiles : 1);
+    const dim3 grid(s.g.blocks + own);
+    if (s.many)
+        hipLaunchKernelGGL((k_attend_shared<W, T, true>), grid, dim3(kWG), 0, st, p, a, s.g);
+    else
+        hipLaunchKernelGGL((k_attend_shared<W, T, false>), grid, dim3(kWG), 0, st, p, a, s.g);
+    hipLaunchKernelGGL((k_attend_join_rows<W, T, true>), dim3((p.seqs * a.q_heads + kWG / 64 - 1) / (kWG / 64), s.join_rows), dim3(kWG), 0, st, p, a);
+}
+
+template <typename T>
+void launch_shared_width(const Pool &p, const Query &a, const SharedShape &s, hipStream_t st) {
+    switch (p.width) {
+        case 64: return launch_shared<64, T>(p, a, s, st);
+        case 96: return launch_shared<96, T>(p, a, s, st);
+        case 128: return launch_shared<128, T>(p, a, s, st);
+        case 192: return launch_shared<192, T>(p, a, s, st);
+        case 256: return launch_shared<256, T>(p, a, s, st);
+    }
+}
+
+bool launchable(const entro_cache *c, const entro_cache_table *t, const entro_cache_query *q, const entro_cache_groups *g) {
+    return uint64_t{g->groups} * c->kv_heads <= kHalfGroups && uint64_t{t->seqs} * c->kv_heads <= kHalfGroups && uint64_t{t->seqs} * q->q_heads <= kMostGroups &&
+           uint64_t{q->tokens} * q->q_heads <= 0x7fffffffull;
+}
+
+}  // namespace
+
+extern "C" {
+
+entro_status entro_cache_shared(const entro_cache *c, const entro_cache_table *t, const entro_cache_groups *g, void *hip_stream) {
+    if (const entro_status s = check_cache(c)) return s;
+    if (const entro_status s = check_table(t)) return s;
+    if (const entro_status s = check_groups(g)) return s;
+    hipLaunchKernelGGL(k_shared, dim3(g->groups < 65536 ? g->groups : 65536), dim3(kWG), 0, static_cast<hipStream_t>(hip_stream), pool_of(c, t, 0), g->first,
+                       g->shared, g->groups);
+    return hip_ok(hipGetLastError(), "entro_cache_shared") ? ENTRO_OK : ENTRO_ERR_DEVICE;
+}
+
+uint64_t entro_cache_attend_shared_workspace_bytes(const entro_cache *c, const entro_cache_table *t, const entro_cache_query *q,
+                                                   const entro_cache_groups *g) {
+    if (check_sizes(c) != ENTRO_OK || check_table_sizes(t) != ENTRO_OK || check_query_sizes(c, q) != ENTRO_OK || check_groups_sizes(g) != ENTRO_OK) return 0;
+    return launchable(c, t, q, g) ? shared_shape_of(c, t, q, g).bytes : 0;
+}
+
+entro_status entro_cache_attend_shared(const entro_cache *c, const entro_cache_table *t, const entro_cache_query *q, const entro_cache_groups *g,
+                                       void *workspace, uint64_t workspace_bytes, void *hip_stream) {
+    if (const entro_status s = check_cache(c)) return s;
+    if (const entro_status s = check_table(t)) return s;
+    if (const entro_status s = check_query(c, q)) return s;
+    if (const entro_status s = check_groups(g)) return s;
+    if (q->tokens == 0) return ENTRO_OK;
+    if (!launchable(c, t, q, g)) return ENTRO_ERR_SIZE;
+    SharedShape shape = shared_shape_of(c, t, q, g);
+    if (!workspace) return ENTRO_ERR_NULL;
+    if (!aligned16(workspace)) return ENTRO_ERR_ALIGN;
+    if (workspace_bytes < shape.bytes) return ENTRO_ERR_CAPACITY;
+    shape.g.first = g->first;
+    shape.g.shared = g->shared;
+    const Pool p = pool_of(c, t, q->layer);
+    const bool aligned = ((q->q_token_stride | q->q_head_stride) & 7u) == 0;
+    const uint32_t parts = shape.g.splits + shape.g.own_splits;
+    float *part_o = static_cast<float *>(workspace), *part_lse = part_o + uint64_t{q->tokens} * q->q_heads * parts * p.width;
+    const Query a = {q->q, q->out, q->lse, q->q_token_stride, q->q_head_stride, q->out_token_stride, q->out_head_stride, q->start,
+                     q->tokens, q->q_heads, q->q_heads / c->kv_heads, q->window, q->sinks, q->scale, aligned, parts, 1, part_o, part_lse};
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (q->type == ENTRO_F32)
+        launch_shared_width<float>(p, a, shape, st);
+    else
+        launch_shared_width<uint16_t>(p, a, shape, st);
+    return hip_ok(hipGetLastError(), "entro_cache_attend_shared") ? ENTRO_OK : ENTRO_ERR_DEVICE;
+}
+
+}  // extern "C"
+
+namespace {
 
 entro_status check_query_sizes(const entro_cache *c, const entro_cache_query *q) {
     if (!q) return ENTRO_ERR_NULL;
