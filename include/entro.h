@@ -610,7 +610,7 @@ uint64_t entro_cache_attend_shared_workspace_bytes(const entro_cache *c, const e
  * shared[g] must not exceed what entro_cache_shared gives: its tokens are taken from the pages of the group's first sequence.  A query may stand
  * among the shared tokens (then fewer are taken as shared), windows may begin there, groups may be of one sequence or none.
  * The order of sums depends on sizes and lengths, never on the run.  ENTRO_ERR_SIZE also where groups or sequences times kv_heads reach
- * 2^23, or sequences times q_heads 2^24.  (For the phase of "Latency Reduction from Huffman Coding"; no passage of the paper defines it.) */
+ * 2^23.  (For the phase of "Latency Reduction from Huffman Coding"; no passage of the paper defines it.) */
 entro_status entro_cache_attend_shared(const entro_cache *c, const entro_cache_table *t, const entro_cache_query *q, const entro_cache_groups *g,
                                        void *workspace, uint64_t workspace_bytes, void *hip_stream);
 

@@ -750,12 +750,13 @@ class Rotary:
         for g in (q_gain, k_gain):
             _need(g is None or (g.dtype == torch.float32 and g.dim() in (1, 2) and g.is_contiguous()), "gains are float32 [head_dim] or [heads][head_dim]")
         self.turns, self.q_gain, self.k_gain = turns, q_gain, k_gain
-        self.tensors = [x for x in (turns, q_gain, k_gain) if x is not None]
+        given = [x for x in (turns, q_gain, k_gain) if x is not None]
+        self.device = _device_of(*given) if given else True              # True: there is nothing that lies anywhere
         at, stride = (lambda x: None if x is None else x.data_ptr()), (lambda g: 0 if g is None or g.dim() == 1 else g.stride(0))
         self.c = CRotary(at(turns), at(q_gain), at(k_gain), stride(q_gain), stride(k_gain), dims, layout, norm, eps, amplitude, 0)
 
     def fits(self, gain, heads: int, head_dim: int):
-        _need(gain is None or tuple(gain.shape) in ((head_dim,), (heads, head_dim)), f"gains are [{head_dim}] or [{heads}][{head_dim}]")
+        _need(gain is None or gain.shape == (head_dim,) or gain.shape == (heads, head_dim), "gains are [head_dim] or [heads][head_dim]")
 
 
 class RotaryRows:
@@ -764,7 +765,7 @@ class RotaryRows:
     def __init__(self, x, y=None):
         y = x if y is None else y
         _need(x.shape == y.shape and x.dtype == y.dtype, "x and y have one shape and type")
-        self.x, self.y, self.device = x, y, _device_of(x, y)
+        self.x, self.y, self.device, self.type = x, y, _device_of(x, y), _rows_type(x, "x")
         self.c = CRotaryRows(x.data_ptr(), y.data_ptr(), *_row_strides(x, "x"), *_row_strides(y, "y"), x.shape[1], 0)
         _need(_own_places(y), "y's elements have places of their own")
 
@@ -780,19 +781,19 @@ def _run_on(device, call):
 
 def entro_rotate(rotary: Rotary, q: Optional[RotaryRows], k: Optional[RotaryRows], positions, stream=None):
     """Norms and rotations of q and k (either may be None) at positions, int32 [tokens]."""
-    sides = [s for s in (q, k) if s is not None]
-    _need(len(sides) > 0, "q or k is given")
-    x = sides[0].x
-    for s, gain in ((q, rotary.q_gain), (k, rotary.k_gain)):
-        if s is not None:
-            _need(s.x.dtype == x.dtype and s.x.shape[0] == x.shape[0] and s.x.shape[2] == x.shape[2], "q and k have one type, as many tokens and dimensions")
-            rotary.fits(gain, s.x.shape[1], x.shape[2])
-    at = _ints(positions, x.shape[0], "positions")
-    device = _device_of(positions, *(t for s in sides for t in (s.x, s.y)), *rotary.tensors)
-    _need(device is not None and device.type == "cuda", "all tensors of a call lie on one GPU")
-    refs = [None if s is None else C.byref(s.c) for s in (q, k)]
-    _run_on(device, lambda: _check(lib().entro_rotate(C.byref(rotary.c), *refs, at, x.shape[0], x.shape[2], _rows_type(x, "x"), _stream_ptr(stream)),
-                                   "entro_rotate"))
+    side = q if k is None else k
+    _need(side is not None, "q or k is given")
+    tokens, heads, dim = side.x.shape
+    if q is not None:
+        _need(side is q or (q.x.shape[0] == tokens and q.x.shape[2] == dim and q.type == side.type), "q and k have one type, as many tokens and dimensions")
+        rotary.fits(rotary.q_gain, q.x.shape[1], dim)
+    if k is not None:
+        rotary.fits(rotary.k_gain, heads, dim)
+    at, device = _ints(positions, tokens, "positions"), positions.device
+    _need(device.type == "cuda" and all(s is None or s.device == device for s in (q, k)) and (rotary.device is True or rotary.device == device),
+          "all tensors of a call lie on one GPU")
+    _run_on(device, lambda: _check(lib().entro_rotate(C.byref(rotary.c), None if q is None else C.byref(q.c), None if k is None else C.byref(k.c), at, tokens, dim,
+                                                      side.type, _stream_ptr(stream)), "entro_rotate"))
 
 
 def entro_cache_append_rotated(cache: Cache, table: CacheTable, rows: CacheRows, rotary: Rotary, queries: Optional[RotaryRows] = None, stream=None):
@@ -804,7 +805,7 @@ def entro_cache_append_rotated(cache: Cache, table: CacheTable, rows: CacheRows,
         x = queries.x
         _need(x.dtype == rows.k.dtype and x.shape[0] == rows.k.shape[0] and x.shape[2] == cache.head_dim, "queries have the type, tokens and dimensions of the rows")
         rotary.fits(rotary.q_gain, x.shape[1], cache.head_dim)
-    _on_gpu(cache, table, rows, queries, *rotary.tensors)
+    _on_gpu(cache, table, rows, queries, None if rotary.device is True else rotary)
     q = None if queries is None else C.byref(queries.c)
     _run_on(cache.device, lambda: _check(lib().entro_cache_append_rotated(C.byref(cache.c), C.byref(table.c), C.byref(rows.c), C.byref(rotary.c), q,
                                                                           _stream_ptr(stream)), "entro_cache_append_rotated"))

@@ -201,6 +201,7 @@ __device__ __forceinline__ void attend_few(const Pool &p, const Query &a, const 
     constexpr int kParts = sizeof(T) == 2 ? 1 : 3;         // bf16 numbers that make an element of q in the first product
     constexpr int kWeights = sizeof(T) == 2 ? 2 : 3;       // bf16 numbers that make a weight of the second
     constexpr int kFull = W / 64, kRest = W % 64 ? 1 : 0;   // loads of 64 dimensions of 16 tokens, and of 32
+    constexpr int kStep = MODE == kOwn ? 1 : 4;             // the tiles go round the four wavefronts; kOwn: a wavefront has work of its own
     constexpr int kDims = W / 16;
     auto &merge_o = lds.merge_o;
     auto &merge_m = lds.merge_m, &merge_l = lds.merge_l;
@@ -221,9 +222,10 @@ __device__ __forceinline__ void attend_few(const Pool &p, const Query &a, const 
         const int32_t begin = from + static_cast<int32_t>(split) * per, end = min(begin + per, until);
         if (MODE == kWhole && begin >= end && split > 0) continue;
         if (MODE != kWhole && begin >= end) {
-            if (tid < 16 && row0 + tid < rows) {
-                const uint32_t token = static_cast<uint32_t>(s.row) + static_cast<uint32_t>((row0 + tid) / a.group);
-                const uint32_t q_head = head * a.group + static_cast<uint32_t>((row0 + tid) % a.group);
+            const uint32_t nth = MODE == kOwn ? lane : tid;
+            if (nth < 16 && row0 + nth < rows) {
+                const uint32_t token = static_cast<uint32_t>(s.row) + static_cast<uint32_t>((row0 + nth) / a.group);
+                const uint32_t q_head = head * a.group + static_cast<uint32_t>((row0 + nth) % a.group);
                 a.part_lse[part_at<MODE>(a, w, uint64_t{token} * a.q_heads + q_head)] = -INFINITY;
             }
             continue;
@@ -262,7 +264,7 @@ __device__ __forceinline__ void attend_few(const Pool &p, const Query &a, const 
         for (int d = 0; d < kDims; ++d) vc[d] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(vp + (uint64_t{16u * d} << p.page_shift)));
         vs = vs_head[uint64_t{static_cast<uint32_t>(max(v_page, 0))} * p.kv_heads];
     };
-    const int32_t i0 = begin + static_cast<int32_t>(wave);
+    const int32_t i0 = begin + (MODE == kOwn ? 0 : static_cast<int32_t>(wave));
     // the lane's row
     const int64_t my_row = row0 + c;
     const bool mine = my_row < rows;
@@ -281,7 +283,7 @@ __device__ __forceinline__ void attend_few(const Pool &p, const Query &a, const 
             load_eight(row, f < 2 * kFull ? (f / 2) * 64 + g * 16 + (f & 1) * 8 : kFull * 64 + g * 8, p.head_dim, a.aligned, x[f]);
         if (i0 < end) {
             take_pages(i0);
-            ask_pages(i0 + 4);
+            ask_pages(i0 + kStep);
             ask_keys(i0);
             ask_values(i0);
         }
@@ -304,7 +306,7 @@ __device__ __forceinline__ void attend_few(const Pool &p, const Query &a, const 
     for (int d = 0; d < kDims; ++d) o[d] = f32x4{0, 0, 0, 0};
     float m = -INFINITY, l = 0.0f;
 
-    for (int32_t i = i0; i < end; i += 4) {
+    for (int32_t i = i0; i < end; i += kStep) {
         const int32_t t0 = tile_at(i);
         page = v_page;
         f32x4 z[4];
@@ -328,9 +330,9 @@ __device__ __forceinline__ void attend_few(const Pool &p, const Query &a, const 
         }
         // scores in units of log2; a page without a token that is seen may hold anything as its scale
         const float factor = fmaxf(ks * q_factor, 1e-37f);
-        take_pages(i + 4);
-        ask_pages(i + 8);
-        ask_keys(i + 4);
+        take_pages(i + kStep);
+        ask_pages(i + 2 * kStep);
+        ask_keys(i + kStep);
         if (!(t0 + kTile - 1 <= first && (!a.window || static_cast<uint32_t>(last - t0) < a.window) && __all(page >= 0))) {
 #pragma unroll
             for (int t = 0; t < 4; ++t)
@@ -378,9 +380,19 @@ __device__ __forceinline__ void attend_few(const Pool &p, const Query &a, const 
                 o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, weights[1][n], o[d], 0, 0, 0);
             }
         }
-        ask_values(i + 4);
+        ask_values(i + kStep);
     }
         l = column_sum(l);
+        if constexpr (MODE == kOwn) {
+            if (mine) {
+                const float inv = l > 0.0f ? 1.0f / l : 0.0f, base = m == -INFINITY ? 0.0f : m;
+                const uint64_t at = part_at<MODE>(a, w, uint64_t{my_token} * a.q_heads + my_head);
+#pragma unroll
+                for (int d = 0; d < kDims; ++d) *reinterpret_cast<f32x4 *>(a.part_o + at * W + 16 * d + 4 * g) = l == l ? o[d] * inv : f32x4{l, l, l, l};
+                if (g == 0) a.part_lse[at] = l > 0.0f ? base + __builtin_amdgcn_logf(l * kUnit) : l == l ? -INFINITY : l;
+            }
+            continue;
+        }
         // the four wavefronts' parts
         __syncthreads();
 #pragma unroll
@@ -502,13 +514,42 @@ __device__ __forceinline__ void attend_many(const Pool &p, const Query &a, const
         const int32_t wave_last = wave_row >= rows ? -1 : MODE == kShared ? last : s.pos + static_cast<int32_t>(min(wave_row + 31, rows - 1) / a.group);
         bf16x8 q[W / 16][kParts];
         float q_factor;
-        {
+        constexpr bool kEarly = MODE != kWhole;    // q's elements are asked for before all else and kept as they are
+        u32x4 raw[W / 16][sizeof(T) / 2];
+        if constexpr (kEarly) {
             const T *row = static_cast<const T *>(a.q) + my_token * a.q_token_stride + my_head * a.q_head_stride;
+#pragma unroll
+            for (int f = 0; f < W / 16; ++f) {
+                const uint32_t d = 16 * f + 8 * h;
+                if (a.aligned && d + 8 <= p.head_dim) {
+#pragma unroll
+                    for (uint32_t i = 0; i < sizeof(T) / 2; ++i) raw[f][i] = reinterpret_cast<const u32x4 *>(row + d)[i];
+                } else {
+                    float x[8];
+                    load_eight(row, d, p.head_dim, false, x);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (sizeof(T) == 2) raw[f][0][i] = upper_halves(x[2 * i], x[2 * i + 1]);
+                        else raw[f][0][i] = __float_as_uint(x[i]), raw[f][sizeof(T) / 2 - 1][i] = __float_as_uint(x[4 + i]);
+                    }
+                }
+            }
+        }
+        const auto eight_of = [&](int f, float *x) {
+            if constexpr (kEarly) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    x[i] = __uint_as_float(sizeof(T) == 4 ? raw[f][(i / 4) % (sizeof(T) / 2)][i & 3] : i & 1 ? raw[f][0][i / 2] & 0xffff0000u : raw[f][0][i / 2] << 16);
+            } else {
+                load_eight(static_cast<const T *>(a.q) + my_token * a.q_token_stride + my_head * a.q_head_stride, 16 * f + 8 * h, p.head_dim, a.aligned, x);
+            }
+        };
+        const auto take_q = [&]() {
             float most = 0.0f;
 #pragma unroll
             for (int f = 0; f < W / 16; ++f) {
                 float x[8];
-                load_eight(row, 16 * f + 8 * h, p.head_dim, a.aligned, x);
+                eight_of(f, x);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(x[i]));
             }
@@ -517,13 +558,14 @@ __device__ __forceinline__ void attend_many(const Pool &p, const Query &a, const
 #pragma unroll
             for (int f = 0; f < W / 16; ++f) {
                 float x[8];
-                load_eight(row, 16 * f + 8 * h, p.head_dim, a.aligned, x);
+                eight_of(f, x);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[i] = ldexpf(x[i] * sign, -e);
                 split_factors<kParts>(x, q[f]);
             }
             q_factor = ldexpf(fabsf(a.scale) * kLog2e, e);
-        }
+        };
+        if (MODE == kWhole) take_q();
         constexpr int kDims = W / 32;
         f32x16 o[kDims];
 #pragma unroll
@@ -586,6 +628,7 @@ __device__ __forceinline__ void attend_many(const Pool &p, const Query &a, const
             ask_pages(begin);
             ask_codes(begin);
             ask_pages(begin + 1);
+            if (MODE != kWhole) take_q();          // while the first codes are on their way
             to_lds(0);
             ask_codes(begin + 1);
             ask_pages(begin + 2);
@@ -778,9 +821,8 @@ __global__ __launch_bounds__(kWG) void k_attend_join(Pool p, Query a) {
     }
 }
 
-// The same for many rows in a few parts: a wavefront per row and head, no more than a lane a part.  Behind k_attend_shared, ALL: every part
-// has its lse, minus infinity where it saw nothing and left its sums unwritten.
-template <int W, typename T, bool ALL = false>
+// The same for many rows in a few parts: a wavefront per row and head, no more than a lane a part.
+template <int W, typename T>
 __global__ __launch_bounds__(kWG) void k_attend_join_rows(Pool p, Query a) {
     constexpr uint32_t kLanes = W / 4, kSets = 64 / kLanes;
     const uint32_t lane = threadIdx.x & 63u, set = lane / kLanes, d = lane % kLanes;
@@ -791,14 +833,11 @@ __global__ __launch_bounds__(kWG) void k_attend_join_rows(Pool p, Query a) {
     for (int32_t nth = static_cast<int32_t>(blockIdx.y); nth < s.count; nth += static_cast<int32_t>(gridDim.y)) {
         const uint32_t token = static_cast<uint32_t>(s.row + nth);
         const uint64_t at = uint64_t{token} * a.q_heads + h;
-        uint32_t parts = a.splits;
-        if (!ALL) {
-            const int64_t row0 = (int64_t{nth} * a.group + h % a.group) / kManyRows * kManyRows;
-            const Tiles tiles = tiles_of(p, a, s.pos + static_cast<int32_t>(row0 / a.group),
-                                         s.pos + static_cast<int32_t>(min(row0 + kManyRows - 1, rows - 1) / a.group));
-            const int32_t per = tiles_per_split(a, tiles.count);
-            parts = static_cast<uint32_t>(max((tiles.count + per - 1) / per, 1));
-        }
+        const int64_t row0 = (int64_t{nth} * a.group + h % a.group) / kManyRows * kManyRows;
+        const Tiles tiles = tiles_of(p, a, s.pos + static_cast<int32_t>(row0 / a.group),
+                                     s.pos + static_cast<int32_t>(min(row0 + kManyRows - 1, rows - 1) / a.group));
+        const int32_t per = tiles_per_split(a, tiles.count);
+        const uint32_t parts = static_cast<uint32_t>(max((tiles.count + per - 1) / per, 1));
         const float mine = lane < parts ? a.part_lse[at * a.splits + lane] : -INFINITY;
         float most = mine;
         for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
@@ -810,7 +849,7 @@ __global__ __launch_bounds__(kWG) void k_attend_join_rows(Pool p, Query a) {
         for (uint32_t i0 = 0; i0 < parts; i0 += kSets) {
             const uint32_t i = i0 + set;
             const float by = __shfl(share, static_cast<int>(min(i, 63u)));
-            if (set < kSets && i < parts && (!ALL || by != 0.0f)) x += part[i * kLanes + d] * by;
+            if (set < kSets && i < parts) x += part[i * kLanes + d] * by;
         }
 #pragma unroll
         for (uint32_t i = 1; i < kSets; ++i)
@@ -833,7 +872,7 @@ __global__ __launch_bounds__(kWG) void k_attend_join_rows(Pool p, Query a) {
 //
 // The tokens that a group's sequences share are multiplied with all its rows together (tiles of 16 rows, or 128 of many), so that their codes
 // are read, turned and multiplied once and not once a sequence; every sequence's further tokens go by the same launch's other
-// workgroups, and k_attend_join_rows brings the parts of a row together.  What is shared is rounded down to whole tiles, and to
+// workgroups, and k_shared_join brings the parts of a row together.  What is shared is rounded down to whole tiles, and to
 // what all of the group's rows see where there is no window; the rest of it is taken as each sequence's own.
 struct Groups {
     const int32_t *first, *shared;
@@ -842,6 +881,9 @@ struct Groups {
     uint32_t row_tiles, splits, least;       // of those
     uint32_t own_tiles, own_splits, own_least;   // own_tiles: 0 where few rows have a kernel of their own
 };
+
+// A number that all lanes have alike, as a scalar.
+__device__ inline int32_t scalar(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // The group of sequence b, or a number that is none.  (All lanes, 64 of the ascending starts at a time.)
 __device__ inline uint32_t group_of(const Groups &g, uint32_t b) {
@@ -859,28 +901,39 @@ __device__ inline uint32_t group_of(const Groups &g, uint32_t b) {
     return below == 0 ? g.groups : lo + below - 1;
 }
 
-// Sequences, rows and shared tiles of group `nth`.  `lds`: two numbers a wavefront.
-__device__ inline void take_group(const Pool &p, const Query &a, const Groups &g, uint32_t nth, int32_t *lds, Part *w) {
-    const uint32_t tid = threadIdx.x;
-    const int32_t seqs = static_cast<int32_t>(p.seqs), rows = static_cast<int32_t>(a.tokens);
-    const int32_t first = min(max(g.first[nth], 0), seqs), last = min(max(g.first[nth + 1], first), seqs);
+// Sequences, rows and shared tiles of group `nth`, by every wavefront for itself.
+__device__ inline void take_group(const Pool &p, const Query &a, const Groups &g, uint32_t nth, Part *w) {
+    const int32_t lane = static_cast<int32_t>(threadIdx.x & 63u), seqs = static_cast<int32_t>(p.seqs), rows = static_cast<int32_t>(a.tokens);
+    const Span mine = span_of(a.start, p.lengths, static_cast<uint32_t>(min(lane, seqs - 1)), a.tokens);      // asked for beside the group's bounds
+    const int32_t first = scalar(min(max(g.first[nth], 0), seqs)), last = scalar(min(max(g.first[nth + 1], first), seqs)), shared = g.shared[nth];
     int32_t least = 0x7fffffff, most = -1;
-    for (int32_t b = first + static_cast<int32_t>(tid); b < last; b += kWG) {
-        const Span s = span_of(a.start, p.lengths, static_cast<uint32_t>(b), a.tokens);
+    const auto add = [&](const Span &s) {
         if (s.count) least = min(least, s.pos), most = max(most, s.length - 1);
+    };
+    if (last <= 64) {
+        if (lane >= first && lane < last) add(mine);
+    } else {
+#pragma unroll 4
+        for (int32_t b = first; b < last; b += 64) add(span_of(a.start, p.lengths, static_cast<uint32_t>(min(b + lane, last - 1)), a.tokens));
     }
     for (int o = 32; o; o >>= 1) least = min(least, __shfl_xor(least, o)), most = max(most, __shfl_xor(most, o));
-    if ((tid & 63u) == 0) lds[2 * (tid >> 6)] = least, lds[2 * (tid >> 6) + 1] = most;
-    __syncthreads();
-    for (int i = 0; i < kWG / 64; ++i) least = min(least, lds[2 * i]), most = max(most, lds[2 * i + 1]);
-    __syncthreads();
+    least = scalar(least);
+    most = scalar(most);
     const int64_t slots = int64_t{p.stride} << p.page_shift;
-    const int64_t tokens = most < 0 ? 0 : min(min(int64_t{g.shared[nth]}, slots), int64_t{least} + 1);
+    const int64_t tokens = most < 0 ? 0 : min(min(int64_t{shared}, slots), int64_t{least} + 1);
     w->tiles = tokens < kTile ? 0 : static_cast<int32_t>(tokens / kTile);
     w->first = static_cast<uint32_t>(first);
     w->last = static_cast<uint32_t>(last);
-    w->s.row = min(max(a.start[first], 0), rows);
-    w->s.count = first < last ? min(max(a.start[last], w->s.row), rows) - w->s.row : 0;
+    int32_t row = 0, end = 0;
+    if (first < last && last <= 64) {
+        row = __builtin_amdgcn_readlane(mine.row, first);
+        end = __builtin_amdgcn_readlane(mine.row + mine.count, last - 1);
+    } else if (first < last) {
+        row = min(max(a.start[first], 0), rows);
+        end = min(max(a.start[last], row), rows);
+    }
+    w->s.row = row;
+    w->s.count = max(end - row, 0);
     w->s.pos = least;
     w->s.length = most + 1;
 }
@@ -889,14 +942,10 @@ template <int W, bool MANY> struct SharedLds {
     union {
         FewLds<W> few;
         ManyLds<W> many;
-        int32_t group[2 * kWG / 64];
     };
 };
 template <int W> struct SharedLds<W, false> {
-    union {
-        FewLds<W> few;
-        int32_t group[2 * kWG / 64];
-    };
+    FewLds<W> few;
 };
 
 template <int W, typename T, bool MANY>
@@ -911,36 +960,40 @@ __global__ __launch_bounds__(kWG, MANY ? (sizeof(T) == 2 && W <= 128 ? 2 : 1) : 
         w.split = blockIdx.x / units % g.splits;
         w.splits = g.splits;
         w.least = g.least;
-        take_group(p, a, g, unit / p.kv_heads, lds.group, &w);
+        take_group(p, a, g, unit / p.kv_heads, &w);
         if (w.s.count == 0) return;
         w.table = w.first;
         if constexpr (MANY) attend_many<W, T, kShared>(p, a, w, blockIdx.x / units / g.splits, g.row_tiles, lds.many);
         else attend_few<W, T, kShared>(p, a, w, lds.few);
         return;
     }
-    const uint32_t r = blockIdx.x - g.blocks, head = r % p.kv_heads, split = r / p.kv_heads % g.own_splits, rest = r / p.kv_heads / g.own_splits;
-    const uint32_t b = rest % p.seqs;
+    // few rows: a wavefront for itself takes a sequence, key head and split, so that heads whose codes lie side by side are in one workgroup
+    const bool by_waves = !MANY || g.own_tiles == 0;
+    const uint32_t r = by_waves ? (blockIdx.x - g.blocks) * (kWG / 64) + static_cast<uint32_t>(scalar(static_cast<int32_t>(threadIdx.x >> 6))) : blockIdx.x - g.blocks;
+    const uint32_t split = r / p.kv_heads % g.own_splits, rest = r / p.kv_heads / g.own_splits, b = by_waves ? rest : rest % p.seqs;
+    if (b >= p.seqs) return;
     const Span s = span_of(a.start, p.lengths, b, a.tokens);
     if (s.count == 0) return;
     const uint32_t nth = group_of(g, b);
+    w.head = r % p.kv_heads;
     if (nth < g.groups) {
-        take_group(p, a, g, nth, lds.group, &w);
+        take_group(p, a, g, nth, &w);
     } else if (split == 0) {                       // in no group: it has no shared parts
+        const uint32_t lanes = by_waves ? 64 : kWG, lane = threadIdx.x % lanes;
         const uint64_t count = uint64_t{static_cast<uint32_t>(s.count)} * a.group * g.splits;
-        for (uint64_t i = uint64_t{rest / p.seqs} * kWG + threadIdx.x; i < count; i += uint64_t{max(g.own_tiles, 1u)} * kWG) {
+        for (uint64_t i = lane; i < count; i += lanes) {
             const uint64_t row = i / g.splits, token = static_cast<uint32_t>(s.row) + row / a.group;
-            a.part_lse[(token * a.q_heads + head * a.group + row % a.group) * w.parts + i % g.splits] = -INFINITY;
+            a.part_lse[(token * a.q_heads + w.head * a.group + row % a.group) * w.parts + i % g.splits] = -INFINITY;
         }
     }
     w.s = s;
     w.table = b;
-    w.head = head;
     w.split = split;
     w.splits = g.own_splits;
     w.least = g.own_least;
     w.slot = g.splits;
     if constexpr (MANY) {
-        if (g.own_tiles) {
+        if (!by_waves) {
             attend_many<W, T, kOwn>(p, a, w, rest / p.seqs, g.own_tiles, lds.many);
             return;
         }
@@ -948,38 +1001,109 @@ __global__ __launch_bounds__(kWG, MANY ? (sizeof(T) == 2 && W <= 128 ? 2 : 1) : 
     attend_few<W, T, kOwn>(p, a, w, lds.few);
 }
 
-// Tokens in leading pages that a group's rows share: a workgroup a group, slots in steps of kWG until some row parts.
+// Joins the parts of every row and head, a wavefront each, no more than a lane a part.  A part that saw nothing has minus infinity as its lse and
+// left its sums unwritten: they are read, as nothing waits for what the lse says, and left out.
+template <int W, typename T>
+__global__ __launch_bounds__(kWG) void k_shared_join(Pool p, Query a) {
+    constexpr uint32_t kLanes = W / 4, kSets = 64 / kLanes, kAhead = 4;
+    const uint32_t lane = threadIdx.x & 63u, set = lane / kLanes, d = lane % kLanes, parts = a.splits;
+    const int32_t from = a.start[0], until = a.start[p.seqs];
+    const uint32_t all = a.tokens * a.q_heads, step = gridDim.x * (kWG / 64);
+    for (uint64_t i = blockIdx.x * (kWG / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); i < all; i += step) {
+        const uint32_t at = static_cast<uint32_t>(i), token = at / a.q_heads, h = at % a.q_heads;
+        const float mine = lane < parts ? a.part_lse[uint64_t{at} * parts + lane] : -INFINITY;
+        if (static_cast<int32_t>(token) < from || static_cast<int32_t>(token) >= until) continue;      // a row of no sequence
+        float most = mine;
+        for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+        const float base = most == -INFINITY ? 0.0f : most, share = __builtin_amdgcn_exp2f(mine - base);
+        float sum = share;
+        for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+        const f32x4 *part = reinterpret_cast<const f32x4 *>(a.part_o + uint64_t{at} * parts * W);
+        f32x4 x = {0, 0, 0, 0};
+        for (uint32_t i0 = 0; i0 < parts; i0 += kAhead * kSets) {
+            f32x4 y[kAhead];
+#pragma unroll
+            for (uint32_t n = 0; n < kAhead; ++n) y[n] = part[min(i0 + n * kSets + min(set, kSets - 1), parts - 1) * kLanes + d];
+#pragma unroll
+            for (uint32_t n = 0; n < kAhead; ++n) {
+                const uint32_t i = i0 + n * kSets + set;
+                const float by = __shfl(share, static_cast<int>(min(i, 63u)));
+                if (set < kSets && i < parts && by != 0.0f) x += y[n] * by;
+            }
+        }
+#pragma unroll
+        for (uint32_t i = 1; i < kSets; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float other = __shfl(x[j], static_cast<int>(d + i * kLanes));
+                if (set == 0) x[j] += other;
+            }
+        const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+        T *out = static_cast<T *>(a.out) + token * a.out_token_stride + h * a.out_head_stride;
+        if (set == 0)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (4 * d + j < p.head_dim) store_as(out + 4 * d + j, sum == sum ? x[j] * inv : sum);
+        if (lane == 0 && a.lse) a.lse[at] = sum > 0.0f ? (base + __builtin_amdgcn_logf(sum)) * kLn2 : (sum == sum ? -INFINITY : sum);
+    }
+}
+
+// Tokens in leading pages that a group's rows share.  How many slots all of its rows fill: a workgroup a group.
+__device__ inline int32_t full_slots(const Pool &p, int32_t begin, int32_t end, int32_t *lds) {
+    const uint32_t tid = threadIdx.x;
+    int32_t full = begin < end ? static_cast<int32_t>(p.stride) : 0;
+    for (int32_t b = begin + static_cast<int32_t>(tid); b < end; b += kWG) full = min(full, max(p.lengths[b], 0) >> p.page_shift);
+    for (int o = 32; o; o >>= 1) full = min(full, __shfl_xor(full, o));
+    __syncthreads();
+    if ((tid & 63u) == 0) lds[tid >> 6] = full;
+    __syncthreads();
+    for (int i = 0; i < kWG / 64; ++i) full = min(full, lds[i]);
+    return full;
+}
+
+// The first of 64 slots from s0 on in which the rows part, `full` if none before that: every wavefront takes a quarter of the rows.
+__device__ inline int32_t first_parting(const Pool &p, int32_t begin, int32_t end, int32_t s0, int32_t full, int32_t *lds) {
+    const uint32_t tid = threadIdx.x;
+    const int32_t s = s0 + static_cast<int32_t>(tid & 63u);
+    const int32_t *column = p.slots + min(s, static_cast<int32_t>(p.stride) - 1);
+    const int32_t id = column[uint64_t{static_cast<uint32_t>(begin)} * p.stride];
+    bool parts = static_cast<uint32_t>(id) >= p.pages;
+#pragma unroll 8
+    for (int32_t b = begin + 1 + static_cast<int32_t>(tid >> 6); b < end; b += kWG / 64) parts |= column[uint64_t{static_cast<uint32_t>(b)} * p.stride] != id;
+    int32_t at = parts ? min(s, full) : full;
+    for (int o = 32; o; o >>= 1) at = min(at, __shfl_xor(at, o));
+    __syncthreads();
+    if ((tid & 63u) == 0) lds[tid >> 6] = at;
+    __syncthreads();
+    for (int i = 0; i < kWG / 64; ++i) at = min(at, lds[i]);
+    return at;
+}
+
+// A workgroup a group, up to the first slot in which they part; PIECES: how far they could agree, which k_shared_pieces then lowers.
+template <bool PIECES>
 __global__ __launch_bounds__(kWG) void k_shared(Pool p, const int32_t *first, int32_t *shared, uint32_t groups) {
     __shared__ int32_t lds[kWG / 64];
-    const uint32_t tid = threadIdx.x;
     const int32_t seqs = static_cast<int32_t>(p.seqs);
     for (uint32_t g = blockIdx.x; g < groups; g += gridDim.x) {
         const int32_t begin = min(max(first[g], 0), seqs), end = min(max(first[g + 1], begin), seqs);
-        int32_t full = begin < end ? static_cast<int32_t>(p.stride) : 0;
-        for (int32_t b = begin + static_cast<int32_t>(tid); b < end; b += kWG) full = min(full, max(p.lengths[b], 0) >> p.page_shift);
-        for (int o = 32; o; o >>= 1) full = min(full, __shfl_xor(full, o));
-        __syncthreads();
-        if ((tid & 63u) == 0) lds[tid >> 6] = full;
-        __syncthreads();
-        for (int i = 0; i < kWG / 64; ++i) full = min(full, lds[i]);
-        int32_t same = full;                       // the first slot in which they part
-        for (int32_t s0 = 0; s0 < full && same == full; s0 += kWG) {
-            const int32_t s = s0 + static_cast<int32_t>(tid);
-            bool parts = false;
-            if (s < full) {
-                const int32_t *column = p.slots + s;
-                const int32_t id = column[uint64_t{static_cast<uint32_t>(begin)} * p.stride];
-                parts = static_cast<uint32_t>(id) >= p.pages;
-                for (int32_t b = begin + 1; b < end; ++b) parts |= column[uint64_t{static_cast<uint32_t>(b)} * p.stride] != id;
-            }
-            int32_t at = parts ? s : full;
-            for (int o = 32; o; o >>= 1) at = min(at, __shfl_xor(at, o));
-            __syncthreads();
-            if ((tid & 63u) == 0) lds[tid >> 6] = at;
-            __syncthreads();
-            for (int i = 0; i < kWG / 64; ++i) same = min(same, lds[i]);
-        }
-        if (tid == 0) shared[g] = same << p.page_shift;
+        const int32_t full = full_slots(p, begin, end, lds);
+        int32_t same = full;
+        if (!PIECES)
+            for (int32_t s0 = 0; s0 < full && same == full; s0 += 64) same = first_parting(p, begin, end, s0, full, lds);
+        if (threadIdx.x == 0) shared[g] = same << p.page_shift;
+    }
+}
+
+// 64 slots of a group a workgroup: all of a long table at once (the minimum is one of integers: its order counts for nothing).
+__global__ __launch_bounds__(kWG) void k_shared_pieces(Pool p, const int32_t *first, int32_t *shared, uint32_t groups, uint32_t pieces) {
+    __shared__ int32_t lds[kWG / 64];
+    const int32_t seqs = static_cast<int32_t>(p.seqs);
+    for (uint64_t w = blockIdx.x; w < uint64_t{groups} * pieces; w += gridDim.x) {
+        const uint32_t g = static_cast<uint32_t>(w / pieces);
+        const int32_t begin = min(max(first[g], 0), seqs), end = min(max(first[g + 1], begin), seqs), s0 = static_cast<int32_t>(w % pieces) * 64;
+        if (begin >= end) continue;
+        const int32_t at = first_parting(p, begin, end, s0, 0x7fffffff >> p.page_shift, lds);
+        if (threadIdx.x == 0 && at < s0 + 64) atomicMin(shared + g, at << p.page_shift);
     }
 }
 
@@ -999,6 +1123,7 @@ entro_status check_groups(const entro_cache_groups *g) {
     return aligned16(g->first) && aligned16(g->shared) ? ENTRO_OK : ENTRO_ERR_ALIGN;
 }
 
+constexpr uint32_t kShortTable = 512;                 // slots that one workgroup goes through
 constexpr uint64_t kHalfGroups = kMostGroups / 2;     // workgroups for shared and for own tokens
 constexpr uint32_t kMostShared = 48, kMostOwn = 16;   // parts of either: the join has a lane for each
 
@@ -1006,7 +1131,6 @@ struct SharedShape {
     bool many;
     Groups g;
     uint64_t bytes;
-    uint32_t join_rows;
 };
 
 uint64_t tiles_in(uint64_t tokens, const entro_cache_query *q, uint64_t rows) {
@@ -1026,35 +1150,42 @@ SharedShape shared_shape_of(const entro_cache *c, const entro_cache_table *t, co
     const uint64_t tiles = tiles_in(shared, q, max_new), own_tiles = tiles_in(uint64_t{q->max_len} - shared + kTile, q, max_new);
     const uint64_t cus = static_cast<uint64_t>(compute_units()), units = uint64_t{groups->groups} * c->kv_heads, own_units = uint64_t{t->seqs} * c->kv_heads;
     s.many = rows > 32;
-    s.join_rows = max_new > 65535 ? 65535 : max_new;
     s.g.groups = groups->groups;
     s.g.row_tiles = s.many ? between((rows + kManyRows - 1) / kManyRows, 1, kHalfGroups / units) : 1;
-    const uint64_t fill = units * s.g.row_tiles;
-    const uint64_t want = (cus * 2 + fill - 1) / fill, can = s.many ? tiles / 4 : tiles / 8;
-    uint64_t fit = kHalfGroups / fill;
+    // own tokens: at most 32 tiles a wavefront
+    const bool own_many = s.many && own_rows > 32;
+    s.g.own_tiles = own_many ? between((own_rows + kManyRows - 1) / kManyRows, 1, kHalfGroups / own_units) : 0;
+    const uint64_t own_fill = own_many ? own_units * s.g.own_tiles : (own_units + 3) / 4;
+    uint64_t fit = kHalfGroups / own_fill;
+    s.g.own_splits = between((own_tiles + 31) / 32, 1, fit < kMostOwn ? fit : kMostOwn);
+    s.g.own_least = between((own_tiles + s.g.own_splits - 1) / s.g.own_splits, 1, 0x7fffffff);
+    // shared tokens: one workgroup a compute unit, those for own tokens counted unless they are short, as two on one get in each other's way; where
+    // that leaves more than 16 tiles to a workgroup, two
+    const uint64_t slots = cus * (entro_cache_width(c->head_dim) > 128 || (s.many && q->type == ENTRO_F32) ? 1 : 2);
+    const uint64_t own_blocks = own_fill * s.g.own_splits, fill = units * s.g.row_tiles;
+    const auto leaves = [&](uint64_t room) { return own_blocks < room && own_tiles >= 8 ? room - own_blocks : room; };
+    uint64_t want = leaves(cus) / fill;
+    if (want * 16 < tiles) want = leaves(slots) / fill;
+    if (want < 2) want = (tiles + 23) / 24;                    // several rounds: none of them long
+    const uint64_t can = s.many ? tiles / 2 : tiles / 8;
+    fit = kHalfGroups / fill;
     s.g.splits = between(want < can ? want : can, 1, fit < kMostShared ? fit : kMostShared);
     s.g.least = between((tiles + s.g.splits - 1) / s.g.splits, 1, 0x7fffffff);
     s.g.blocks = static_cast<uint32_t>(fill * s.g.splits);
-    const bool own_many = s.many && own_rows > 32;
-    s.g.own_tiles = own_many ? between((own_rows + kManyRows - 1) / kManyRows, 1, kHalfGroups / own_units) : 0;
-    const uint64_t own_fill = own_units * (own_many ? s.g.own_tiles : 1);
-    const uint64_t own_want = (cus * 2 + own_fill - 1) / own_fill, own_can = own_tiles < 24 ? 1 : own_tiles / 8;
-    fit = kHalfGroups / own_fill;
-    s.g.own_splits = between(own_want < own_can ? own_want : own_can, 1, fit < kMostOwn ? fit : kMostOwn);
-    s.g.own_least = between((own_tiles + s.g.own_splits - 1) / s.g.own_splits, 1, 0x7fffffff);
     s.bytes = uint64_t{q->tokens} * q->q_heads * (s.g.splits + s.g.own_splits) * (entro_cache_width(c->head_dim) + 1) * 4;
     return s;
 }
 
 template <int W, typename T>
 void launch_shared(const Pool &p, const Query &a, const SharedShape &s, hipStream_t st) {
-    const uint32_t own = p.seqs * p.kv_heads * s.g.own_splits * (s.g.own_tiles ? s.g.own_tiles : 1);
+    const uint32_t units = p.seqs * p.kv_heads * s.g.own_splits, own = s.g.own_tiles ? units * s.g.own_tiles : (units + 3) / 4;
     const dim3 grid(s.g.blocks + own);
     if (s.many)
         hipLaunchKernelGGL((k_attend_shared<W, T, true>), grid, dim3(kWG), 0, st, p, a, s.g);
     else
         hipLaunchKernelGGL((k_attend_shared<W, T, false>), grid, dim3(kWG), 0, st, p, a, s.g);
-    hipLaunchKernelGGL((k_attend_join_rows<W, T, true>), dim3((p.seqs * a.q_heads + kWG / 64 - 1) / (kWG / 64), s.join_rows), dim3(kWG), 0, st, p, a);
+    hipLaunchKernelGGL((k_shared_join<W, T>), dim3(between((uint64_t{a.tokens} * a.q_heads + kWG / 64 - 1) / (kWG / 64), 1, kMostGroups)),
+                       dim3(kWG), 0, st, p, a);
 }
 
 template <typename T>
@@ -1069,8 +1200,7 @@ void launch_shared_width(const Pool &p, const Query &a, const SharedShape &s, hi
 }
 
 bool launchable(const entro_cache *c, const entro_cache_table *t, const entro_cache_query *q, const entro_cache_groups *g) {
-    return uint64_t{g->groups} * c->kv_heads <= kHalfGroups && uint64_t{t->seqs} * c->kv_heads <= kHalfGroups && uint64_t{t->seqs} * q->q_heads <= kMostGroups &&
-           uint64_t{q->tokens} * q->q_heads <= 0x7fffffffull;
+    return uint64_t{g->groups} * c->kv_heads <= kHalfGroups && uint64_t{t->seqs} * c->kv_heads <= kHalfGroups && uint64_t{q->tokens} * q->q_heads <= 0x7fffffffull;
 }
 
 }  // namespace
@@ -1081,8 +1211,17 @@ entro_status entro_cache_shared(const entro_cache *c, const entro_cache_table *t
     if (const entro_status s = check_cache(c)) return s;
     if (const entro_status s = check_table(t)) return s;
     if (const entro_status s = check_groups(g)) return s;
-    hipLaunchKernelGGL(k_shared, dim3(g->groups < 65536 ? g->groups : 65536), dim3(kWG), 0, static_cast<hipStream_t>(hip_stream), pool_of(c, t, 0), g->first,
-                       g->shared, g->groups);
+    const Pool p = pool_of(c, t, 0);
+    const dim3 grid(g->groups < 65536 ? g->groups : 65536);
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (t->stride <= kShortTable) {
+        hipLaunchKernelGGL(k_shared<false>, grid, dim3(kWG), 0, st, p, g->first, g->shared, g->groups);
+    } else {
+        const uint32_t pieces = (t->stride + 63) / 64;
+        const uint64_t all = uint64_t{g->groups} * pieces;
+        hipLaunchKernelGGL(k_shared<true>, grid, dim3(kWG), 0, st, p, g->first, g->shared, g->groups);
+        hipLaunchKernelGGL(k_shared_pieces, dim3(static_cast<uint32_t>(all < 65536 ? all : 65536)), dim3(kWG), 0, st, p, g->first, g->shared, g->groups, pieces);
+    }
     return hip_ok(hipGetLastError(), "entro_cache_shared") ? ENTRO_OK : ENTRO_ERR_DEVICE;
 }
 

@@ -8,6 +8,7 @@ namespace {
 using namespace entro_detail;
 
 constexpr int kWG = 256;
+constexpr uint32_t kHeads = 4;               // that a lane group takes one after the other, in large calls
 constexpr float kLeastEps = 1.2e-38f;
 
 struct Turning {
@@ -134,73 +135,93 @@ __device__ inline void turn_of(int32_t position, uint64_t turns, float amplitude
 
 template <typename T>
 __device__ inline void turns_of(const Turning &r, const Piece &c, int32_t position, float *cosine, float *sine) {
+    constexpr uint32_t P = kRun<T>;
     if (!c.turned) return;
+    uint64_t turns[P];
+    if (c.pair + P <= r.half) {
 #pragma unroll
-    for (uint32_t j = 0; j < kRun<T>; ++j) turn_of(position, r.turns[min(c.pair + j, r.half - 1)], r.amplitude, cosine + j, sine + j);
+        for (uint32_t j = 0; j < P; ++j) turns[j] = r.turns[c.pair + j];
+    } else {
+#pragma unroll
+        for (uint32_t j = 0; j < P; ++j) turns[j] = r.turns[min(c.pair + j, r.half - 1)];
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < P; ++j) turn_of(position, turns[j], r.amplitude, cosine + j, sine + j);
 }
 
-__device__ inline float head_sum(float v, uint32_t shift) {
-    for (int o = (1 << shift) >> 1; o; o >>= 1) v += __shfl_xor(v, o);
+// A number of a lane that holds another part of the same head: of the one 1, 2 or 16 away, or of one in the other half of 8 or 16 lanes, whose halves
+// have by then the same number in all their lanes.
+template <int STEP>
+__device__ inline float other_part(float v) {
+    constexpr int kSwap1 = 0xb1, kSwap2 = 0x4e, kHalfMirror = 0x141, kMirror = 0x140;      // patterns of lane moves
+    if constexpr (STEP >= 16) return __shfl_xor(v, STEP);
+    else return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), STEP == 1 ? kSwap1 : STEP == 2 ? kSwap2 : STEP == 4 ? kHalfMirror : kMirror, 0xf, 0xf, true));
+}
+
+// v brought together over the lanes of a head by f.
+template <typename F>
+__device__ inline float over_head(float v, uint32_t shift, F f) {
+    if (shift > 0) v = f(v, other_part<1>(v));
+    if (shift > 1) v = f(v, other_part<2>(v));
+    if (shift > 2) v = f(v, other_part<4>(v));
+    if (shift > 3) v = f(v, other_part<8>(v));
+    if (shift > 4) v = f(v, other_part<16>(v));
+    if (shift > 5) v = f(v, other_part<32>(v));
     return v;
 }
 
-__device__ inline float head_max(float v, uint32_t shift) {
-    for (int o = (1 << shift) >> 1; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-    return v;
-}
-
-// The norm of a head, whose lanes are all here.  Squares of large elements would leave the range: then all is done on elements less
-// their largest one's exponent (beside which eps is nothing).
+// The norm of a head, whose elements are x and, as they were read, raw.  All lanes are here.  Where the squares of some head of the wavefront leave the
+// range, all is done again on elements less the exponent of their head's largest one.
 template <typename T>
-__device__ inline void norm_head(const Turning &r, const Piece &c, const float *gain, bool gain_wide, float *x) {
+__device__ inline void norm_head(const Turning &r, const Piece &c, const float *gain, bool gain_wide, const Raw &raw, float *x) {
     constexpr uint32_t P = kRun<T>, N = 2 * P;
-    float g[N];
+    const auto here = [&](uint32_t j) { return j % P < c.count[j / P]; };
+    const auto add = [](float a, float b) { return a + b; };
+    const auto mean_square = [&]() {
+        if (r.norm == ENTRO_NORM_CENTRED) {
+            float sum = 0.0f;
+#pragma unroll
+            for (uint32_t j = 0; j < N; ++j) sum += x[j];
+            sum = over_head(sum, r.shift, add);
+#pragma unroll
+            for (uint32_t j = 0; j < N; ++j) x[j] = here(j) ? fmaf(-sum, r.inverse_dim, x[j]) : 0.0f;
+        }
+        float sum = 0.0f;
+#pragma unroll
+        for (uint32_t j = 0; j < N; ++j) sum = fmaf(x[j], x[j], sum);
+        return over_head(sum, r.shift, add) * r.inverse_dim;
+    };
+    float mean = mean_square(), eps = r.eps;
+    if (__any(!(mean < INFINITY))) {
+        head_values<T>(raw, x);
+        float most = 0.0f;
+#pragma unroll
+        for (uint32_t j = 0; j < N; ++j) most = fmaxf(most, fabsf(x[j]));
+        most = over_head(most, r.shift, [](float a, float b) { return fmaxf(a, b); });
+        const int e = most > 1e17f && most < INFINITY ? static_cast<int>(__float_as_uint(most) >> 23) - 127 : 0;
+#pragma unroll
+        for (uint32_t j = 0; j < N; ++j) x[j] = ldexpf(x[j], -e);
+        if (e) eps = fmaxf(ldexpf(eps, -2 * e), kLeastEps);
+        mean = mean_square();
+    }
+    const float by = rsqrtf(mean + eps);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         if (!gain) {
 #pragma unroll
-            for (uint32_t j = 0; j < P; ++j) g[i * P + j] = 1.0f;
+            for (uint32_t j = 0; j < P; ++j) x[i * P + j] *= by;
         } else if (gain_wide && c.count[i] == P && c.at[i] % 4 == 0) {
 #pragma unroll
             for (uint32_t j = 0; j < P; j += 4) {
                 const f32x4 w = *reinterpret_cast<const f32x4 *>(gain + c.at[i] + j);
 #pragma unroll
-                for (int n = 0; n < 4; ++n) g[i * P + j + n] = w[n];
+                for (uint32_t n = 0; n < 4; ++n) x[i * P + j + n] = x[i * P + j + n] * by * w[n];
             }
         } else {
 #pragma unroll
-            for (uint32_t j = 0; j < P; ++j) g[i * P + j] = j < c.count[i] ? gain[c.at[i] + j] : 0.0f;
+            for (uint32_t j = 0; j < P; ++j) x[i * P + j] = j < c.count[i] ? x[i * P + j] * by * gain[c.at[i] + j] : 0.0f;
         }
     }
-    const auto here = [&](uint32_t j) { return j % P < c.count[j / P]; };
-    const auto centre = [&]() {
-        float sum = 0.0f;
-#pragma unroll
-        for (uint32_t j = 0; j < N; ++j) sum += x[j];
-        sum = head_sum(sum, r.shift);
-#pragma unroll
-        for (uint32_t j = 0; j < N; ++j) x[j] = here(j) ? fmaf(-sum, r.inverse_dim, x[j]) : 0.0f;
-    };
-    const auto squares = [&]() {
-        float sum = 0.0f;
-#pragma unroll
-        for (uint32_t j = 0; j < N; ++j) sum = fmaf(x[j], x[j], sum);
-        return head_sum(sum, r.shift);
-    };
-    float most = 0.0f, eps = r.eps;
-#pragma unroll
-    for (uint32_t j = 0; j < N; ++j) most = fmaxf(most, fabsf(x[j]));
-    most = head_max(most, r.shift);
-    if (most > 1e17f && most < INFINITY) {
-        const int e = static_cast<int>(__float_as_uint(most) >> 23) - 127;
-#pragma unroll
-        for (uint32_t j = 0; j < N; ++j) x[j] = ldexpf(x[j], -e);
-        eps = fmaxf(ldexpf(eps, -2 * e), kLeastEps);
-    }
-    if (r.norm == ENTRO_NORM_CENTRED) centre();
-    const float by = rsqrtf(fmaf(squares(), r.inverse_dim, eps));
-#pragma unroll
-    for (uint32_t j = 0; j < N; ++j) x[j] = x[j] * by * g[j];
 }
 
 template <typename T, bool kPairs>
@@ -239,7 +260,7 @@ __device__ inline void rotate_heads(const Turning &r, const Side &q, const Side 
         const uint32_t head = h < q.heads ? h : h - q.heads;
         float x[2 * P];
         head_values<T>(raw[i], x);
-        if (r.norm) norm_head<T>(r, c, s.gain ? s.gain + uint64_t{head} * s.gain_stride : nullptr, s.gain_wide, x);
+        if (r.norm) norm_head<T>(r, c, s.gain ? s.gain + uint64_t{head} * s.gain_stride : nullptr, s.gain_wide, raw[i], x);
         turn_head<T, kPairs>(c, cosine, sine, x);
         if (mine && nth + i * per_token == h) write_head(static_cast<T *>(s.y) + row * s.y_token_stride + head * s.y_head_stride, c, s.wide, x);
     }
@@ -268,6 +289,12 @@ __device__ inline void rotate_queries(const Pool &p, const Rows &rows, const Tur
     }
 }
 
+// Query rows of sequences on their own, behind many new rows: beside the cache's workgroups they would have the registers of those.
+template <typename T, bool kPairs>
+__global__ __launch_bounds__(kWG) void k_rotate_queries(Pool p, Rows rows, Turning r, Side q, uint32_t each, uint32_t per_token) {
+    rotate_queries<T, kPairs, kHeads>(p, rows, r, q, blockIdx.x / each, blockIdx.x % each, each, per_token);
+}
+
 // The grid of k_append_rotated: workgroups for blocks of the cache, then some for the query rows of each sequence.
 struct Shares {
     uint32_t blocks, work, cache_groups;         // as entro_cache_append's; workgroups of the first kind
@@ -277,19 +304,19 @@ struct Shares {
 // LANES lanes to a block and head, as entro_cache_append has it, and its values' patches.  Keys go by lane groups of a head, which keep up
 // to 32 elements a lane between finding the block's largest element and writing its codes; blocks of more are read, normed and
 // turned twice.
-template <typename T, bool kPairs, int LANES, int HEADS>
+template <typename T, bool kPairs, int LANES>
 __global__ __launch_bounds__(kWG) void k_append_rotated(Pool p, Rows rows, Turning r, Side q, Side keys, Shares g) {
     __shared__ uint32_t most[2][kWG / 64];
     constexpr uint32_t kUnits = kWG / LANES, P = kRun<T>, kKeep = 16 / P;
     if (blockIdx.x >= g.cache_groups) {
         const uint32_t w = blockIdx.x - g.cache_groups;
-        rotate_queries<T, kPairs, HEADS>(p, rows, r, q, w / g.query_groups, w % g.query_groups, g.query_groups, g.per_token);
+        rotate_queries<T, kPairs, 1>(p, rows, r, q, w / g.query_groups, w % g.query_groups, g.query_groups, g.per_token);
         return;
     }
     const uint32_t lane = threadIdx.x % LANES, patches = ((p.head_dim + 7) / 8) << (p.page_shift - 2);
     const uint32_t lanes = 1u << r.shift, groups = LANES >> r.shift, mine = lane >> r.shift;
     const Piece c = piece_of<T, kPairs>(r, lane & (lanes - 1));
-    for (uint32_t w = blockIdx.x * kUnits + threadIdx.x / LANES; w < g.work; w += g.cache_groups * kUnits) {
+    for (uint32_t w = blockIdx.x * kUnits + __builtin_amdgcn_readfirstlane(threadIdx.x / LANES); w < g.work; w += g.cache_groups * kUnits) {
         each_block(p, rows, g.blocks, w, [&](const Block &b, uint32_t head) {
             const T *x = static_cast<const T *>(rows.x[0]) + static_cast<uint64_t>(b.row) * rows.token_stride[0] + head * rows.head_stride[0];
             const T *x_v = static_cast<const T *>(rows.x[1]) + static_cast<uint64_t>(b.row) * rows.token_stride[1] + head * rows.head_stride[1];
@@ -301,7 +328,7 @@ __global__ __launch_bounds__(kWG) void k_append_rotated(Pool p, Rows rows, Turni
                 float cosine[P], sine[P];
                 turns_of<T>(r, c, b.at + static_cast<int32_t>(t), cosine, sine);
                 head_values<T>(raw, y);
-                if (r.norm) norm_head<T>(r, c, gain, keys.gain_wide, y);
+                if (r.norm) norm_head<T>(r, c, gain, keys.gain_wide, raw, y);
                 turn_head<T, kPairs>(c, cosine, sine, y);
             };
             const auto largest_of = [&](const float *y, bool finite) {
@@ -443,8 +470,6 @@ Side side_of(const entro_rotary_rows *s, const float *gain, uint32_t gain_stride
             multiple(gain, 16) && gain_stride % 4 == 0};
 }
 
-constexpr uint32_t kHeads = 4;       // that a lane group takes one after the other, in large calls
-
 template <typename T, bool kPairs>
 void launch_rotate(const Turning &r, const Side &q, const Side &k, const int32_t *positions, uint32_t tokens, hipStream_t st) {
     const uint32_t heads = q.heads + k.heads, few = (heads + kHeads - 1) / kHeads;
@@ -462,20 +487,20 @@ template <typename T, bool kPairs, int LANES>
 void launch_append(const Pool &p, const Rows &rows, const Turning &r, const Side &q, const Side &keys, Shares g, uint64_t most_new, hipStream_t st) {
     const uint32_t groups = (g.work + kWG / LANES - 1) / (kWG / LANES);
     g.cache_groups = groups < 65536 ? groups : 65536;
-    bool many = false;
     if (q.heads) {
         const uint32_t few = (q.heads + kHeads - 1) / kHeads;
-        many = ((uint64_t{rows.tokens} * few) << r.shift) >= 64 * 2048;
-        g.per_token = many ? few : q.heads;
-        const uint64_t each = kWG >> r.shift, wanted = (most_new * g.per_token + each - 1) / each, fit = (1u << 23) / p.seqs;
-        g.query_groups = static_cast<uint32_t>(wanted < fit ? wanted : fit);
-        if (g.query_groups == 0) g.query_groups = 1;
+        const bool many = ((uint64_t{rows.tokens} * few) << r.shift) >= 64 * 2048;
+        const uint32_t per_token = many ? few : q.heads;
+        const uint64_t each = kWG >> r.shift, wanted = (most_new * per_token + each - 1) / each, fit = (1u << 23) / p.seqs;
+        const uint32_t query_groups = wanted < 1 ? 1 : static_cast<uint32_t>(wanted < fit ? wanted : fit);
+        if (many) {
+            hipLaunchKernelGGL((k_rotate_queries<T, kPairs>), dim3(query_groups * p.seqs), dim3(kWG), 0, st, p, rows, r, q, query_groups, per_token);
+        } else {
+            g.query_groups = query_groups;
+            g.per_token = per_token;
+        }
     }
-    const dim3 grid(g.cache_groups + g.query_groups * p.seqs);
-    if (many)
-        hipLaunchKernelGGL((k_append_rotated<T, kPairs, LANES, kHeads>), grid, dim3(kWG), 0, st, p, rows, r, q, keys, g);
-    else
-        hipLaunchKernelGGL((k_append_rotated<T, kPairs, LANES, 1>), grid, dim3(kWG), 0, st, p, rows, r, q, keys, g);
+    hipLaunchKernelGGL((k_append_rotated<T, kPairs, LANES>), dim3(g.cache_groups + g.query_groups * p.seqs), dim3(kWG), 0, st, p, rows, r, q, keys, g);
 }
 
 }  // namespace

@@ -166,7 +166,18 @@ def test_calls_refuse_any_one_tensor_in_host_memory(calls_made, monkeypatch, cal
 @pytest.fixture(scope="module")
 def host(tmp_path_factory):
     include = '#include "entro_cache.h"'
-    prelude = """namespace {
+    prelude = """#define __builtin_amdgcn_readfirstlane(x) (x)
+namespace {
+// lane moves: neighbours, pairs of neighbours, mirrored eights and sixteens
+int moved(int v, int how) {
+    const uint32_t l = threadIdx.x & 63u;
+    return shuffle(v, how == 0xb1 ? l ^ 1 : how == 0x4e ? l ^ 2 : how == 0x141 ? l ^ 7 : l ^ 15);
+}
+#define __builtin_amdgcn_mov_dpp(v, how, rows, banks, bound) moved(v, how)
+int __any(int x) {
+    for (uint32_t o = 1; o < 64; o <<= 1) x |= shuffle(x, (threadIdx.x & 63u) ^ o);
+    return x;
+}
 float __shfl_xor(float v, int o) { return __builtin_bit_cast(float, __shfl_xor(__builtin_bit_cast(int, v), o)); }
 uint32_t __umulhi(uint32_t a, uint32_t b) { return static_cast<uint32_t>(uint64_t{a} * b >> 32); }
 float rsqrtf(float x) { return 1.0f / sqrtf(x); }
@@ -243,7 +254,7 @@ def test_hints_of_any_size_make_launches_that_a_gpu_takes(host, seqs, stride, kv
         assert host.entro_cache_append_rotated(C.byref(cache), C.byref(table), C.byref(rows), C.byref(rotary), C.byref(q), None) == B.ENTRO_OK
     assert host.entro_rotate(C.byref(rotary), C.byref(q), None, at, (1 << 31) // q_heads - 1, 64, E.ENTRO_BF16, None) == B.ENTRO_OK
     n = host.host_launches(out, 300)
-    assert n == 3 * 7
+    assert 3 * 7 <= n <= 3 * 13
     for i in range(0, n, 3):
         assert 0 < out[i] < 1 << 32 and 0 < out[i + 1] and 0 < out[i + 2] < 1 << 16
     host.host_only_note(0)

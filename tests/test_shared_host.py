@@ -113,9 +113,10 @@ def host(tmp_path_factory):
     def part(begin, end=None):
         at = attend.index(begin)
         return attend[at: attend.index(end, at) if end else None]
-    stubs = """namespace {
+    stubs = """#define __builtin_amdgcn_readfirstlane(x) (x)
+namespace {
 template <int W, typename T, bool MANY, typename... A> void k_attend_shared(const A &...) {}
-template <int W, typename T, bool ALL, typename... A> void k_attend_join_rows(const A &...) {}
+template <int W, typename T, typename... A> void k_shared_join(const A &...) {}
 }
 """
     L = compiled(tmp_path_factory.mktemp("host_shared"), "host_cache.cpp", "\n".join([
@@ -128,15 +129,18 @@ template <int W, typename T, bool ALL, typename... A> void k_attend_join_rows(co
 
 
 @pytest.mark.parametrize("first_wave", [0, 2])
-@pytest.mark.parametrize("first", [[0, 3, 3, 5], [0, 5], [-2, 2, 9], [4, 2, 1]])
-def test_what_is_shared_as_host_code(host, first_wave, first):
+@pytest.mark.parametrize("first,long", [([0, 3, 3, 5], False), ([0, 5], True), ([-2, 2, 9], True), ([-2, 2, 9], False), ([4, 2, 1], True)])
+def test_what_is_shared_as_host_code(host, first_wave, first, long):
     host.host_first_wave(first_wave)
     rng, mem = np.random.default_rng(len(first)), Memory()
     page, pages, stride = 16, 900, 300
     table = np.tile(rng.permutation(pages)[:stride], (5, 1))
+    lengths = np.array([4800, 4790, 4800, 4500, 5000])
     table[3:, 270:] = 0
     table[2, 290], table[1, 258] = 5, 7
-    lengths = np.array([4800, 4790, 4800, 4500, 5000])
+    if long:
+        table = np.concatenate([np.full((5, 1), 3), table[:, :299], table], 1)
+        stride, lengths = 600, np.array([9600, 9590, 9600, 9300, 9700])
     slots, at = mem(table, np.int32), mem(lengths, np.int32)
     begin, out = mem(first, np.int32), mem(np.full(len(first) + 1, 77), np.int32)
     cache, t, g = B.CCache(PTR, PTR, PTR, PTR, 1, pages, page, 1, 64, 0), B.CCacheTable(slots.ctypes.data, at.ctypes.data, 5, stride), B.CCacheGroups(
