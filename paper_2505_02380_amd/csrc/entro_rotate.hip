@@ -2,13 +2,18 @@
 #include "entro_cache.h"
 
 #include <cmath>
+#include <type_traits>
 
 namespace {
 
 using namespace entro_detail;
 
 constexpr int kWG = 256;
-constexpr uint32_t kHeads = 4;               // that a lane group takes one after the other, in large calls
+// Heads that a lane group takes one after the other in large calls, with the angles of its position found once: 8192 rows of 40 heads of 128 in bf16,
+// four heads 41 us, eight 38; 4999 rows of 24 heads of 80 in fp32, four 26 us, eight 37 (152 registers).
+template <typename T> constexpr uint32_t kHeads = sizeof(T) == 2 ? 8 : 4;
+constexpr uint64_t kManyLanes = 64 * 2048;   // a call is large from here on: two wavefronts for every SIMD
+constexpr uint64_t kApartLanes = 64 * 8192;  // and its queries are rotated by a launch of their own
 constexpr float kLeastEps = 1.2e-38f;
 
 struct Turning {
@@ -25,13 +30,16 @@ struct Side {
     uint64_t x_token_stride, x_head_stride, y_token_stride, y_head_stride;
     const float *gain;
     uint32_t gain_stride, heads;
-    bool wide, gain_wide;                // rows, gains begin at multiples of 16 bytes
+    bool wide, gain_wide;                // rows, gains begin at multiples of four elements
 };
 
-// A lane has two runs of 16 bytes of a head: of the turned dimensions the first and the second halves of its pairs (halves), or
-// its pairs one after the other (pairs); of the others 32 bytes as they lie.  So rows are read and written in 16-byte
-// pieces, and both elements of a pair are in one lane.
-template <typename T> constexpr uint32_t kRun = 16 / sizeof(T);
+// A lane has two runs of four elements of a head: of the turned dimensions the first and the second halves of its pairs (halves), or
+// its pairs one after the other (pairs); of the others eight elements as they lie.  So rows are read and written in whole pieces,
+// and both elements of a pair are in one lane.  (Runs of eight bf16 elements, half as many lanes with up to 248 registers: a row
+// of each of 64 sequences into the cache 14.6 us instead of 10.9, 26 800 rows 92 instead of 85.)
+constexpr uint32_t kRun = 4;
+
+template <typename T> using Word = std::conditional_t<sizeof(T) == 2, u32x2, u32x4>;       // a run
 
 struct Piece {
     uint32_t at[2], count[2];            // first element of a run, and how many there are
@@ -39,9 +47,9 @@ struct Piece {
     bool turned;
 };
 
-template <typename T, bool kPairs>
+template <bool kPairs>
 __device__ inline Piece piece_of(const Turning &r, uint32_t unit) {
-    constexpr uint32_t P = kRun<T>;
+    constexpr uint32_t P = kRun;
     const uint32_t turned = (r.half + P - 1) / P;
     Piece c;
     c.turned = unit < turned;
@@ -62,26 +70,26 @@ __device__ inline Piece piece_of(const Turning &r, uint32_t unit) {
 }
 
 // The two runs of a head as they lie in memory.
+template <typename T>
 struct Raw {
-    u32x4 w[2];
+    Word<T> w[2];
 };
 
 template <typename T>
-__device__ inline Raw ask_head(const T *row, const Piece &c, bool wide) {
-    constexpr uint32_t P = kRun<T>;
-    Raw r;
+__device__ inline Raw<T> ask_head(const T *row, const Piece &c, bool wide) {
+    Raw<T> r;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        r.w[i] = u32x4{0, 0, 0, 0};
-        if (wide && c.count[i] == P && c.at[i] % P == 0) {
-            r.w[i] = *reinterpret_cast<const u32x4 *>(row + c.at[i]);
+        r.w[i] = Word<T>{};
+        if (wide && c.count[i] == kRun && c.at[i] % kRun == 0) {
+            r.w[i] = *reinterpret_cast<const Word<T> *>(row + c.at[i]);
         } else {
 #pragma unroll
-            for (uint32_t j = 0; j < P; ++j)
+            for (uint32_t j = 0; j < kRun; ++j)
                 if (j < c.count[i]) {
                     const T e = row[c.at[i] + j];
-                    if (sizeof(T) == 2) r.w[i][j / 2] |= static_cast<uint32_t>(e) << (16 * (j & 1));
-                    else r.w[i][j % 4] = __builtin_bit_cast(uint32_t, static_cast<float>(e));
+                    if constexpr (sizeof(T) == 2) r.w[i][j / 2] |= static_cast<uint32_t>(e) << (16 * (j & 1));
+                    else r.w[i][j] = __float_as_uint(e);
                 }
         }
     }
@@ -89,31 +97,34 @@ __device__ inline Raw ask_head(const T *row, const Piece &c, bool wide) {
 }
 
 template <typename T>
-__device__ inline void head_values(const Raw &r, float *x) {
-    constexpr uint32_t P = kRun<T>;
+__device__ inline void head_values(const Raw<T> &r, float *x) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (uint32_t j = 0; j < P; ++j)
-            x[i * P + j] = __uint_as_float(sizeof(T) == 4 ? r.w[i][j % 4] : j & 1 ? r.w[i][j / 2] & 0xffff0000u : r.w[i][j / 2] << 16);
+        for (uint32_t j = 0; j < kRun; ++j) {
+            if constexpr (sizeof(T) == 4) x[i * kRun + j] = __uint_as_float(r.w[i][j]);
+            else x[i * kRun + j] = __uint_as_float(j & 1 ? r.w[i][j / 2] & 0xffff0000u : r.w[i][j / 2] << 16);
+        }
+}
+
+// Two numbers rounded to nearest even, in one instruction; NaNs stay NaNs.
+__device__ inline uint32_t two_bf16(float a, float b) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(a), static_cast<__bf16>(b)});
 }
 
 template <typename T>
 __device__ inline void write_head(T *row, const Piece &c, bool wide, const float *x) {
-    constexpr uint32_t P = kRun<T>;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        T y[P];
-#pragma unroll
-        for (uint32_t j = 0; j < P; ++j) y[j] = store_from_f32<T>(x[i * P + j]);
-        if (wide && c.count[i] == P && c.at[i] % P == 0) {
-            u32x4 w;
-            __builtin_memcpy(&w, y, 16);
-            *reinterpret_cast<u32x4 *>(row + c.at[i]) = w;
+        if (wide && c.count[i] == kRun && c.at[i] % kRun == 0) {
+            const float *y = x + i * kRun;
+            if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4 *>(row + c.at[i]) = f32x4{y[0], y[1], y[2], y[3]};
+            else *reinterpret_cast<u32x2 *>(row + c.at[i]) = u32x2{two_bf16(y[0], y[1]), two_bf16(y[2], y[3])};
         } else {
 #pragma unroll
-            for (uint32_t j = 0; j < P; ++j)
-                if (j < c.count[i]) row[c.at[i] + j] = y[j];
+            for (uint32_t j = 0; j < kRun; ++j)
+                if (j < c.count[i]) row[c.at[i] + j] = store_from_f32<T>(x[i * kRun + j]);
         }
     }
 }
@@ -133,9 +144,8 @@ __device__ inline void turn_of(int32_t position, uint64_t turns, float amplitude
     *sine = amplitude * (quarter & 2 ? -s : s);
 }
 
-template <typename T>
 __device__ inline void turns_of(const Turning &r, const Piece &c, int32_t position, float *cosine, float *sine) {
-    constexpr uint32_t P = kRun<T>;
+    constexpr uint32_t P = kRun;
     if (!c.turned) return;
     uint64_t turns[P];
     if (c.pair + P <= r.half) {
@@ -173,8 +183,8 @@ __device__ inline float over_head(float v, uint32_t shift, F f) {
 // The norm of a head, whose elements are x and, as they were read, raw.  All lanes are here.  Where the squares of some head of the wavefront leave the
 // range, all is done again on elements less the exponent of their head's largest one.
 template <typename T>
-__device__ inline void norm_head(const Turning &r, const Piece &c, const float *gain, bool gain_wide, const Raw &raw, float *x) {
-    constexpr uint32_t P = kRun<T>, N = 2 * P;
+__device__ inline void norm_head(const Turning &r, const Piece &c, const float *gain, bool gain_wide, const Raw<T> &raw, float *x) {
+    constexpr uint32_t P = kRun, N = 2 * P;
     const auto here = [&](uint32_t j) { return j % P < c.count[j / P]; };
     const auto add = [](float a, float b) { return a + b; };
     const auto mean_square = [&]() {
@@ -210,13 +220,10 @@ __device__ inline void norm_head(const Turning &r, const Piece &c, const float *
         if (!gain) {
 #pragma unroll
             for (uint32_t j = 0; j < P; ++j) x[i * P + j] *= by;
-        } else if (gain_wide && c.count[i] == P && c.at[i] % 4 == 0) {
+        } else if (gain_wide && c.count[i] == P && c.at[i] % P == 0) {
+            const f32x4 w = *reinterpret_cast<const f32x4 *>(gain + c.at[i]);
 #pragma unroll
-            for (uint32_t j = 0; j < P; j += 4) {
-                const f32x4 w = *reinterpret_cast<const f32x4 *>(gain + c.at[i] + j);
-#pragma unroll
-                for (uint32_t n = 0; n < 4; ++n) x[i * P + j + n] = x[i * P + j + n] * by * w[n];
-            }
+            for (uint32_t j = 0; j < P; ++j) x[i * P + j] = x[i * P + j] * by * w[j];
         } else {
 #pragma unroll
             for (uint32_t j = 0; j < P; ++j) x[i * P + j] = j < c.count[i] ? x[i * P + j] * by * gain[c.at[i] + j] : 0.0f;
@@ -224,9 +231,9 @@ __device__ inline void norm_head(const Turning &r, const Piece &c, const float *
     }
 }
 
-template <typename T, bool kPairs>
+template <bool kPairs>
 __device__ inline void turn_head(const Piece &c, const float *cosine, const float *sine, float *x) {
-    constexpr uint32_t P = kRun<T>;
+    constexpr uint32_t P = kRun;
     if (!c.turned) return;
 #pragma unroll
     for (uint32_t j = 0; j < P; ++j) {
@@ -237,14 +244,16 @@ __device__ inline void turn_head(const Piece &c, const float *cosine, const floa
     }
 }
 
-// Heads nth, nth + per_token, .. of a row of q and k side by side, at one position. (All lanes of a wavefront come here together, `mine` or
+// Heads nth, nth + per_token, .. of a row of q and k side by side, at one position. Bound by bytes in large calls (8192 rows of 40 heads of 128 in
+// bf16 38 us, 4.4 TB/s; the angles and norms take about 400 vector instructions for eight heads), by latency in small ones (one row 3.4 us: position and
+// elements, sums, stores). (All lanes of a wavefront come here together, `mine` or
 // not: what lanes exchange is exchanged by all.)
 template <typename T, bool kPairs, int HEADS>
 __device__ inline void rotate_heads(const Turning &r, const Side &q, const Side &k, uint32_t row, int32_t position, uint32_t nth, uint32_t per_token, bool mine) {
-    constexpr uint32_t P = kRun<T>;
-    const Piece c = piece_of<T, kPairs>(r, threadIdx.x & ((1u << r.shift) - 1));
+    constexpr uint32_t P = kRun;
+    const Piece c = piece_of<kPairs>(r, threadIdx.x & ((1u << r.shift) - 1));
     const auto side = [&](uint32_t h) -> const Side & { return h < q.heads ? q : k; };
-    Raw raw[HEADS];
+    Raw<T> raw[HEADS];
 #pragma unroll
     for (int i = 0; i < HEADS; ++i) {
         const uint32_t h = min(nth + i * per_token, q.heads + k.heads - 1);
@@ -252,7 +261,7 @@ __device__ inline void rotate_heads(const Turning &r, const Side &q, const Side 
         raw[i] = ask_head(static_cast<const T *>(s.x) + row * s.x_token_stride + (h < q.heads ? h : h - q.heads) * s.x_head_stride, c, s.wide);
     }
     float cosine[P], sine[P];
-    turns_of<T>(r, c, position, cosine, sine);
+    turns_of(r, c, position, cosine, sine);
 #pragma unroll
     for (int i = 0; i < HEADS; ++i) {
         const uint32_t h = min(nth + i * per_token, q.heads + k.heads - 1);
@@ -261,7 +270,7 @@ __device__ inline void rotate_heads(const Turning &r, const Side &q, const Side 
         float x[2 * P];
         head_values<T>(raw[i], x);
         if (r.norm) norm_head<T>(r, c, s.gain ? s.gain + uint64_t{head} * s.gain_stride : nullptr, s.gain_wide, raw[i], x);
-        turn_head<T, kPairs>(c, cosine, sine, x);
+        turn_head<kPairs>(c, cosine, sine, x);
         if (mine && nth + i * per_token == h) write_head(static_cast<T *>(s.y) + row * s.y_token_stride + head * s.y_head_stride, c, s.wide, x);
     }
 }
@@ -289,10 +298,12 @@ __device__ inline void rotate_queries(const Pool &p, const Rows &rows, const Tur
     }
 }
 
-// Query rows of sequences on their own, behind many new rows: beside the cache's workgroups they would have the registers of those.
+// Query rows of sequences on their own, with many new rows: beside the cache's workgroups they would have the registers of those (26 800 rows of 32 query
+// and 8 key heads of 128: 302 us in one launch, 178 in two; 1600 rows of 24 and 4 heads of 96 in fp32: 24 in one, 33 in two).  Bound by bytes: 93 us
+// for those of the first, 4.7 TB/s.
 template <typename T, bool kPairs>
 __global__ __launch_bounds__(kWG) void k_rotate_queries(Pool p, Rows rows, Turning r, Side q, uint32_t each, uint32_t per_token) {
-    rotate_queries<T, kPairs, kHeads>(p, rows, r, q, blockIdx.x / each, blockIdx.x % each, each, per_token);
+    rotate_queries<T, kPairs, kHeads<T>>(p, rows, r, q, blockIdx.x / each, blockIdx.x % each, each, per_token);
 }
 
 // The grid of k_append_rotated: workgroups for blocks of the cache, then some for the query rows of each sequence.
@@ -303,11 +314,13 @@ struct Shares {
 
 // LANES lanes to a block and head, as entro_cache_append has it, and its values' patches.  Keys go by lane groups of a head, which keep up
 // to 32 elements a lane between finding the block's largest element and writing its codes; blocks of more are read, normed and
-// turned twice.
+// turned twice.  A row of each of 64 sequences (8 key heads of 128, and 32 query heads beside them): 10.9 us, bound by latency (bounds, rows and table,
+// sums, scale).  26 800 rows: 85 us, 1.9 TB/s, where entro_cache_append takes 44: three wavefronts a SIMD are what 168 registers leave, and every
+// key head finds its angles for itself (14 us of vector instructions by their count).
 template <typename T, bool kPairs, int LANES>
-__global__ __launch_bounds__(kWG) void k_append_rotated(Pool p, Rows rows, Turning r, Side q, Side keys, Shares g) {
+__global__ __launch_bounds__(kWG, 3) void k_append_rotated(Pool p, Rows rows, Turning r, Side q, Side keys, Shares g) {
     __shared__ uint32_t most[2][kWG / 64];
-    constexpr uint32_t kUnits = kWG / LANES, P = kRun<T>, kKeep = 16 / P;
+    constexpr uint32_t kUnits = kWG / LANES, P = kRun, kKeep = 16 / P;
     if (blockIdx.x >= g.cache_groups) {
         const uint32_t w = blockIdx.x - g.cache_groups;
         rotate_queries<T, kPairs, 1>(p, rows, r, q, w / g.query_groups, w % g.query_groups, g.query_groups, g.per_token);
@@ -315,7 +328,7 @@ __global__ __launch_bounds__(kWG) void k_append_rotated(Pool p, Rows rows, Turni
     }
     const uint32_t lane = threadIdx.x % LANES, patches = ((p.head_dim + 7) / 8) << (p.page_shift - 2);
     const uint32_t lanes = 1u << r.shift, groups = LANES >> r.shift, mine = lane >> r.shift;
-    const Piece c = piece_of<T, kPairs>(r, lane & (lanes - 1));
+    const Piece c = piece_of<kPairs>(r, lane & (lanes - 1));
     for (uint32_t w = blockIdx.x * kUnits + __builtin_amdgcn_readfirstlane(threadIdx.x / LANES); w < g.work; w += g.cache_groups * kUnits) {
         each_block(p, rows, g.blocks, w, [&](const Block &b, uint32_t head) {
             const T *x = static_cast<const T *>(rows.x[0]) + static_cast<uint64_t>(b.row) * rows.token_stride[0] + head * rows.head_stride[0];
@@ -324,12 +337,12 @@ __global__ __launch_bounds__(kWG) void k_append_rotated(Pool p, Rows rows, Turni
             float kept[kKeep][2 * P], v[4][8];
             uint32_t m[2] = {0, 0};
             const auto key = [&](uint32_t t, float *y) {
-                const Raw raw = ask_head(x + t * rows.token_stride[0], c, keys.wide);
+                const Raw<T> raw = ask_head(x + t * rows.token_stride[0], c, keys.wide);
                 float cosine[P], sine[P];
-                turns_of<T>(r, c, b.at + static_cast<int32_t>(t), cosine, sine);
+                turns_of(r, c, b.at + static_cast<int32_t>(t), cosine, sine);
                 head_values<T>(raw, y);
                 if (r.norm) norm_head<T>(r, c, gain, keys.gain_wide, raw, y);
-                turn_head<T, kPairs>(c, cosine, sine, y);
+                turn_head<kPairs>(c, cosine, sine, y);
             };
             const auto largest_of = [&](const float *y, bool finite) {
                 uint32_t all = 0;
@@ -393,9 +406,7 @@ __global__ __launch_bounds__(kWG) void k_append_rotated(Pool p, Rows rows, Turni
 #pragma unroll
                     for (uint32_t j = 0; j < P; ++j) code[j] = grid[0].divide ? code_by_division(y[i * P + j], grid[0].scale) : code_by_inverse(y[i * P + j], grid[0]);
                     if (c.count[i] == P && c.at[i] % P == 0) {
-#pragma unroll
-                        for (uint32_t j = 0; j < P; j += 4)
-                            *reinterpret_cast<uint32_t *>(at + c.at[i] + j) = four_codes(code[j], code[j + 1], code[j + 2], code[j + 3]);
+                        *reinterpret_cast<uint32_t *>(at + c.at[i]) = four_codes(code[0], code[1], code[2], code[3]);
                     } else {
 #pragma unroll
                         for (uint32_t j = 0; j < P; ++j)
@@ -454,9 +465,8 @@ entro_status check_side(const entro_rotary_rows *s, uint32_t tokens, uint32_t ty
     return ENTRO_OK;
 }
 
-Turning turning_of(const entro_rotary *r, uint32_t head_dim, uint32_t type) {
-    const uint32_t run = type == ENTRO_F32 ? 4 : 8, half = r->dims / 2;
-    const uint32_t units = (half + run - 1) / run + (head_dim - r->dims + 2 * run - 1) / (2 * run);
+Turning turning_of(const entro_rotary *r, uint32_t head_dim) {
+    const uint32_t half = r->dims / 2, units = (half + kRun - 1) / kRun + (head_dim - r->dims + 2 * kRun - 1) / (2 * kRun);
     uint32_t shift = 0;
     while ((1u << shift) < units) ++shift;                   // at most 33 units
     return {r->turns, half, head_dim, r->norm, shift, r->eps, r->amplitude, 1.0f / static_cast<float>(head_dim)};
@@ -464,21 +474,21 @@ Turning turning_of(const entro_rotary *r, uint32_t head_dim, uint32_t type) {
 
 Side side_of(const entro_rotary_rows *s, const float *gain, uint32_t gain_stride, uint32_t type) {
     if (!s) return Side{};
-    const uint64_t run = 16 / size_of(type);
-    const bool wide = multiple(s->x, 16) && multiple(s->y, 16) && (s->x_token_stride | s->x_head_stride | s->y_token_stride | s->y_head_stride) % run == 0;
+    const uint64_t run = kRun * size_of(type);
+    const bool wide = multiple(s->x, run) && multiple(s->y, run) && (s->x_token_stride | s->x_head_stride | s->y_token_stride | s->y_head_stride) % kRun == 0;
     return {s->x, s->y, s->x_token_stride, s->x_head_stride, s->y_token_stride, s->y_head_stride, gain, gain_stride, s->heads, wide,
             multiple(gain, 16) && gain_stride % 4 == 0};
 }
 
 template <typename T, bool kPairs>
 void launch_rotate(const Turning &r, const Side &q, const Side &k, const int32_t *positions, uint32_t tokens, hipStream_t st) {
-    const uint32_t heads = q.heads + k.heads, few = (heads + kHeads - 1) / kHeads;
-    const bool many = ((uint64_t{tokens} * few) << r.shift) >= 64 * 2048;
+    const uint32_t heads = q.heads + k.heads, few = (heads + kHeads<T> - 1) / kHeads<T>;
+    const bool many = ((uint64_t{tokens} * few) << r.shift) >= kManyLanes;
     const uint32_t per_token = many ? few : heads, items = tokens * per_token;
     const uint64_t groups = (uint64_t{items} + (kWG >> r.shift) - 1) / (kWG >> r.shift);
     const dim3 grid(static_cast<uint32_t>(groups < (1u << 23) ? groups : 1u << 23));
     if (many)
-        hipLaunchKernelGGL((k_rotate<T, kPairs, kHeads>), grid, dim3(kWG), 0, st, r, q, k, positions, items, per_token);
+        hipLaunchKernelGGL((k_rotate<T, kPairs, kHeads<T>>), grid, dim3(kWG), 0, st, r, q, k, positions, items, per_token);
     else
         hipLaunchKernelGGL((k_rotate<T, kPairs, 1>), grid, dim3(kWG), 0, st, r, q, k, positions, items, per_token);
 }
@@ -488,8 +498,8 @@ void launch_append(const Pool &p, const Rows &rows, const Turning &r, const Side
     const uint32_t groups = (g.work + kWG / LANES - 1) / (kWG / LANES);
     g.cache_groups = groups < 65536 ? groups : 65536;
     if (q.heads) {
-        const uint32_t few = (q.heads + kHeads - 1) / kHeads;
-        const bool many = ((uint64_t{rows.tokens} * few) << r.shift) >= 64 * 2048;
+        const uint32_t few = (q.heads + kHeads<T> - 1) / kHeads<T>;
+        const bool many = ((uint64_t{rows.tokens} * few) << r.shift) >= kApartLanes;
         const uint32_t per_token = many ? few : q.heads;
         const uint64_t each = kWG >> r.shift, wanted = (most_new * per_token + each - 1) / each, fit = (1u << 23) / p.seqs;
         const uint32_t query_groups = wanted < 1 ? 1 : static_cast<uint32_t>(wanted < fit ? wanted : fit);
@@ -541,7 +551,7 @@ entro_status entro_rotate(const entro_rotary *r, const entro_rotary_rows *q, con
     if (uint64_t{tokens} * ((q ? q->heads : 0) + (k ? k->heads : 0)) > 0x7fffffffull) return ENTRO_ERR_SIZE;
     if (!multiple(positions, 4)) return ENTRO_ERR_ALIGN;
     if (tokens == 0) return ENTRO_OK;
-    const Turning t = turning_of(r, head_dim, type);
+    const Turning t = turning_of(r, head_dim);
     const Side a = side_of(q, r->q_gain, r->q_gain_stride, type), b = side_of(k, r->k_gain, r->k_gain_stride, type);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (type == ENTRO_F32)
@@ -575,7 +585,7 @@ entro_status entro_cache_append_rotated(const entro_cache *c, const entro_cache_
     const Pool p = pool_of(c, t, r->layer);
     const bool aligned = multiple(r->v, 16) && ((r->v_token_stride | r->v_head_stride) & 7u) == 0;
     const Rows rows = {{r->k, r->v}, {r->k_token_stride, r->v_token_stride}, {r->k_head_stride, r->v_head_stride}, r->start, r->tokens, aligned};
-    const Turning turning = turning_of(rotary, c->head_dim, r->type);
+    const Turning turning = turning_of(rotary, c->head_dim);
     const entro_rotary_rows key_rows = {r->k, r->k, r->k_token_stride, r->k_head_stride, r->k_token_stride, r->k_head_stride, c->kv_heads, 0};
     const Side a = side_of(q, rotary->q_gain, rotary->q_gain_stride, r->type), keys = side_of(&key_rows, rotary->k_gain, rotary->k_gain_stride, r->type);
     const bool few = ((c->head_dim + 7) / 8) * (c->page_tokens / 4) <= 64;
