@@ -2,9 +2,10 @@
 
 Every step multiplies each beam's x with the compressed q, k and v matrices (one prepared launch for all beams), takes the next page
 table (forks, one more token), writes k and v into the cache, attends, and multiplies the result with the compressed output matrix. Products
-and attention hand each other bf16 rows in place.
+and attention hand each other bf16 rows in place. With --rotary keys and queries are normed and rotated by their positions in the pass that
+writes the cache; with --shared what the beams have in common is attended over once for all of them.
 
-    python examples/token_step.py [--layer mistral|smol] [--prompt 1000] [--beams 4] [--steps 32] [--window 0] [--sinks 0]
+    python examples/token_step.py [--layer mistral|smol] [--prompt 1000] [--beams 4] [--steps 32] [--window 0] [--sinks 0] [--rotary] [--shared]
 """
 import argparse
 import os
@@ -13,6 +14,7 @@ import time
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
+import numpy as np
 import torch
 
 import paper_2505_02380_amd as E
@@ -47,7 +49,7 @@ class Generation:
     """Beams over one layer: the cache, its two tables (of this step and of the next), and the step."""
 
     def __init__(self, layer: Layer, heads: int, kv_heads: int, dim: int, beams: int, most_tokens: int, page: int = 64, window: int = 0,
-                 sinks: int = 0):
+                 sinks: int = 0, rotary: bool = False, shared: bool = False):
         dev = layer.x.device
         slots = -(-most_tokens // page) + 1
         self.layer, self.window, self.sinks = layer, window, sinks
@@ -59,7 +61,16 @@ class Generation:
         rows = lambda x, n: x.view(beams, n, dim)  # noqa: E731
         self.rows = E.CacheRows(rows(layer.k, kv_heads), rows(layer.v, kv_heads), start, 1)
         self.query = E.CacheQuery(rows(layer.q, heads), rows(layer.attended, heads), start, 1, most_tokens, window=window, sinks=sinks)
-        need = E.entro_cache_attend_workspace_bytes(self.cache, self.tables[0], self.query)
+        self.rotary = self.groups = None
+        if rotary:
+            self.rotary = E.Rotary(torch.from_numpy(E.entro_rotary_turns(dim).view(np.int64)).to(dev), dim, norm=E.ENTRO_NORM_RMS,
+                                   q_gain=torch.ones(dim, device=dev), k_gain=torch.ones(dim, device=dev))
+            self.query_rows = E.RotaryRows(rows(layer.q, heads))                    # rotated where they lie
+        if shared:
+            self.groups = E.CacheGroups(torch.tensor([0, beams], dtype=torch.int32, device=dev), torch.zeros(1, dtype=torch.int32, device=dev), beams, most_tokens)
+            need = E.entro_cache_attend_shared_workspace_bytes(self.cache, self.tables[0], self.query, self.groups)
+        else:
+            need = E.entro_cache_attend_workspace_bytes(self.cache, self.tables[0], self.query)
         self.attend_room = torch.empty(max(16, need), dtype=torch.uint8, device=dev)
         self.one = torch.ones(beams, dtype=torch.int32, device=dev)
 
@@ -80,14 +91,24 @@ class Generation:
         self.next_table(grow=grow)
         start = torch.full((beams + 1,), n, dtype=torch.int32, device=k.device)
         start[0] = 0
-        E.entro_cache_append(self.cache, self.table, E.CacheRows(k, v, start, n))
+        self.append(E.CacheRows(k, v, start, n))
+
+    def append(self, rows, queries=None):
+        if self.rotary is None:
+            E.entro_cache_append(self.cache, self.table, rows)
+        else:
+            E.entro_cache_append_rotated(self.cache, self.table, rows, self.rotary, queries)
 
     def step(self, parent=None):
         """One token for every beam: y from x. parent: the beams that these go on from (None: themselves)."""
         E.entro_plan_run(self.layer.plans[0][0])
         self.next_table(parent=parent, grow=self.one)
-        E.entro_cache_append(self.cache, self.table, self.rows)
-        E.entro_cache_attend(self.cache, self.table, self.query, self.attend_room)
+        self.append(self.rows, None if self.rotary is None else self.query_rows)
+        if self.groups is None:
+            E.entro_cache_attend(self.cache, self.table, self.query, self.attend_room)
+        else:
+            E.entro_cache_shared(self.cache, self.table, self.groups)
+            E.entro_cache_attend_shared(self.cache, self.table, self.query, self.groups, self.attend_room)
         E.entro_plan_run(self.layer.plans[1][0])
         return self.layer.y
 
@@ -97,12 +118,14 @@ def main(argv=None):
     ap.add_argument("--layer", choices=sorted(LAYERS), default="mistral")
     for name, value in (("prompt", 1000), ("beams", 4), ("steps", 32), ("window", 0), ("sinks", 0)):
         ap.add_argument("--" + name, type=int, default=value)
+    for name in ("rotary", "shared"):
+        ap.add_argument("--" + name, action="store_true")
     a = ap.parse_args(argv)
     cfg, heads, kv_heads, dim = LAYERS[a.layer]
     gen = torch.Generator(device="cuda:0")
     gen.manual_seed(1)
     layer = Layer(cfg, a.beams)
-    g = Generation(layer, heads, kv_heads, dim, a.beams, a.prompt + a.steps, window=a.window, sinks=a.sinks)
+    g = Generation(layer, heads, kv_heads, dim, a.beams, a.prompt + a.steps, window=a.window, sinks=a.sinks, rotary=a.rotary, shared=a.shared)
     g.prompt(*(torch.randn(a.prompt, kv_heads, dim, device="cuda:0", generator=gen).to(torch.bfloat16) for _ in "kv"))
     layer.x.copy_(torch.randn(layer.x.shape, device="cuda:0", generator=gen))
     parent = torch.zeros(a.beams, dtype=torch.int32, device="cuda:0")

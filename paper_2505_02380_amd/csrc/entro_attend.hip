@@ -1163,7 +1163,7 @@ SharedShape shared_shape_of(const entro_cache *c, const entro_cache_table *t, co
     // that leaves more than 16 tiles to a workgroup, two
     const uint64_t slots = cus * (entro_cache_width(c->head_dim) > 128 || (s.many && q->type == ENTRO_F32) ? 1 : 2);
     const uint64_t own_blocks = own_fill * s.g.own_splits, fill = units * s.g.row_tiles;
-    const auto leaves = [&](uint64_t room) { return own_blocks < room && own_tiles >= 8 ? room - own_blocks : room; };
+    const auto leaves = [&](uint64_t room) { return own_blocks < room && own_tiles > 3 ? room - own_blocks : room; };
     uint64_t want = leaves(cus) / fill;
     if (want * 16 < tiles) want = leaves(slots) / fill;
     if (want < 2) want = (tiles + 23) / 24;                    // several rounds: none of them long

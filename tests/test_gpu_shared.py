@@ -308,3 +308,35 @@ def test_refusals_on_the_gpu():
         with pytest.raises(E.EntroError) as err:
             E.entro_cache_attend_shared(cache, t, query, g, ws)
         assert err.value.status == status
+
+
+def test_the_example_s_steps_with_positions_and_a_shared_prefix():
+    """The example's last step of a few, beams forking, with norms, rotations and what the beams share: rotated queries, cache and attention against
+    the definitions."""
+    import rotary_reference as rot
+    from examples import token_step as ex
+    cfg, heads, kv_heads, dim = ex.LAYERS["smol"]
+    beams, tokens = 3, 205
+    layer = ex.Layer(cfg, beams)
+    g = ex.Generation(layer, heads, kv_heads, dim, beams, 220, page=16, rotary=True, shared=True)
+    torch.manual_seed(6)
+    g.prompt(*(torch.randn(200, kv_heads, dim, device=DEV).to(torch.bfloat16) for _ in "kv"))
+    for parent in ([0, 0, 0], [2, 0, 2], [0, 1, 1], [1, 1, 0], [0, 1, 2]):
+        layer.x.copy_(torch.randn(layer.x.shape, device=DEV))
+        g.step(ints(parent))
+    torch.cuda.synchronize()
+    assert g.status.tolist()[0] == 0 and g.table.lengths.tolist() == [tokens] * beams and g.groups.shared.tolist() == [192]
+    pool = ref.Pool(np.random.default_rng(0), 1, 1, kv_heads, 16, dim)
+    pool.pages = g.cache.pages
+    pool.k, pool.v, pool.k_scale, pool.v_scale = (x.cpu().numpy() for x in (g.cache.k, g.cache.v, g.cache.k_scale, g.cache.v_scale))
+    table, start = g.table.slots.cpu().numpy(), np.arange(beams + 1)
+    q = layer.q.view(beams, heads, dim).float().cpu().numpy()
+    check_attend(pool, table, [tokens] * beams, q, start, "bf16", layer.attended.view(beams, heads, dim), None, dim ** -0.5)
+    E.entro_plan_run(layer.plans[0][0])                         # the rows before they were rotated
+    turns, at = E.entro_rotary_turns(dim), np.full(beams, tokens - 1)
+    want, bound = rot.rotate(layer.q.view(beams, heads, dim).float().cpu().numpy(), at, turns, "halves", "rms")
+    assert np.all(np.abs(q - want) <= rot.tolerance(want, bound, "bf16"))
+    want, bound = rot.rotate(layer.k.view(beams, kv_heads, dim).float().cpu().numpy(), at, turns, "halves", "rms")
+    k, _ = ref.read(pool, table, [tokens] * beams, start, beams)
+    step = pool.k_scale[0, table[:, (tokens - 1) // 16]][..., None]
+    assert np.all(np.abs(k - want) <= step * 0.5 * (1 + 2.0 ** -16) + bound)
