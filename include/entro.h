@@ -420,8 +420,8 @@ typedef struct {
     uint32_t reserved;           /* 0 */
 } entro_rotary;
 
-/* Rows [tokens][heads][head_dim] with strides in elements (dimensions lie side by side).  They and the gains need no more than their
- * elements' own alignment; rows that begin at multiples of 16 bytes are faster. */
+/* Rows [tokens][heads][head_dim] with strides in elements (dimensions lie side by side).  They, the gains and the positions need no more
+ * than their elements' own alignment; rows that begin at multiples of four elements are faster. */
 typedef struct {
     const void *x;               /* device: read */
     void *y;                     /* device: written; x itself (with the same strides), or memory apart from it */

@@ -879,8 +879,10 @@ struct Groups {
     uint32_t groups;
     uint32_t blocks;                         // workgroups for shared tokens: they come first
     uint32_t row_tiles, splits, least;       // of those
-    uint32_t own_tiles, own_splits, own_least;   // own_tiles: 0 where few rows have a kernel of their own
+    uint32_t own_tiles, own_splits, own_least;   // of own tokens; own_tiles: 0 where wavefronts take them
 };
+
+constexpr uint32_t kMostParts = 256;         // of a row
 
 // A number that all lanes have alike, as a scalar.
 __device__ inline int32_t scalar(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -1001,34 +1003,45 @@ __global__ __launch_bounds__(kWG, MANY ? (sizeof(T) == 2 && W <= 128 ? 2 : 1) : 
     attend_few<W, T, kOwn>(p, a, w, lds.few);
 }
 
-// Joins the parts of every row and head, a wavefront each, no more than a lane a part.  A part that saw nothing has minus infinity as its lse and
+// Joins the parts of every row and head, a wavefront each; a lane has the lse of every 64th part.  A part that saw nothing has minus infinity as its lse and
 // left its sums unwritten: they are read, as nothing waits for what the lse says, and left out.
 template <int W, typename T>
 __global__ __launch_bounds__(kWG) void k_shared_join(Pool p, Query a) {
     constexpr uint32_t kLanes = W / 4, kSets = 64 / kLanes, kAhead = 4;
-    const uint32_t lane = threadIdx.x & 63u, set = lane / kLanes, d = lane % kLanes, parts = a.splits;
-    const int32_t from = a.start[0], until = a.start[p.seqs];
+    const uint32_t lane = threadIdx.x & 63u, set = lane / kLanes, d = lane % kLanes, parts = min(a.splits, kMostParts);
+    const int32_t first = a.start[0], last = a.start[p.seqs];
     const uint32_t all = a.tokens * a.q_heads, step = gridDim.x * (kWG / 64);
     for (uint64_t i = blockIdx.x * (kWG / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); i < all; i += step) {
         const uint32_t at = static_cast<uint32_t>(i), token = at / a.q_heads, h = at % a.q_heads;
-        const float mine = lane < parts ? a.part_lse[uint64_t{at} * parts + lane] : -INFINITY;
-        if (static_cast<int32_t>(token) < from || static_cast<int32_t>(token) >= until) continue;      // a row of no sequence
-        float most = mine;
+        float share[kMostParts / 64];
+#pragma unroll
+        for (uint32_t n = 0; n < kMostParts / 64; ++n) {
+            const uint32_t nth = 64 * n + lane;
+            share[n] = nth < parts ? a.part_lse[uint64_t{at} * parts + nth] : -INFINITY;
+        }
+        if (static_cast<int32_t>(token) < first || static_cast<int32_t>(token) >= last) continue;      // a row of no sequence
+        float most = fmaxf(fmaxf(share[0], share[1]), fmaxf(share[2], share[3]));
         for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
-        const float base = most == -INFINITY ? 0.0f : most, share = __builtin_amdgcn_exp2f(mine - base);
-        float sum = share;
+        const float base = most == -INFINITY ? 0.0f : most;
+        float sum = 0.0f;
+#pragma unroll
+        for (uint32_t n = 0; n < kMostParts / 64; ++n) sum += share[n] = __builtin_amdgcn_exp2f(share[n] - base);
         for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
         const f32x4 *part = reinterpret_cast<const f32x4 *>(a.part_o + uint64_t{at} * parts * W);
         f32x4 x = {0, 0, 0, 0};
-        for (uint32_t i0 = 0; i0 < parts; i0 += kAhead * kSets) {
-            f32x4 y[kAhead];
 #pragma unroll
-            for (uint32_t n = 0; n < kAhead; ++n) y[n] = part[min(i0 + n * kSets + min(set, kSets - 1), parts - 1) * kLanes + d];
+        for (uint32_t m = 0; m < kMostParts / 64; ++m) {
+            const uint32_t until = min(parts, 64 * m + 64);
+            for (uint32_t i0 = 64 * m; i0 < until; i0 += kAhead * kSets) {
+                f32x4 y[kAhead];
 #pragma unroll
-            for (uint32_t n = 0; n < kAhead; ++n) {
-                const uint32_t i = i0 + n * kSets + set;
-                const float by = __shfl(share, static_cast<int>(min(i, 63u)));
-                if (set < kSets && i < parts && by != 0.0f) x += y[n] * by;
+                for (uint32_t n = 0; n < kAhead; ++n) y[n] = part[min(i0 + n * kSets + min(set, kSets - 1), parts - 1) * kLanes + d];
+#pragma unroll
+                for (uint32_t n = 0; n < kAhead; ++n) {
+                    const uint32_t i = i0 + n * kSets + set;
+                    const float by = __shfl(share[m], static_cast<int>(i & 63u));
+                    if (set < kSets && i < until && by != 0.0f) x += y[n] * by;
+                }
             }
         }
 #pragma unroll
@@ -1064,8 +1077,8 @@ __device__ inline int32_t full_slots(const Pool &p, int32_t begin, int32_t end, 
 // The first of 64 slots from s0 on in which the rows part, `full` if none before that: every wavefront takes a quarter of the rows.
 __device__ inline int32_t first_parting(const Pool &p, int32_t begin, int32_t end, int32_t s0, int32_t full, int32_t *lds) {
     const uint32_t tid = threadIdx.x;
-    const int32_t s = s0 + static_cast<int32_t>(tid & 63u);
-    const int32_t *column = p.slots + min(s, static_cast<int32_t>(p.stride) - 1);
+    const int32_t s = static_cast<int32_t>(min(static_cast<uint32_t>(s0) + (tid & 63u), p.stride - 1));
+    const int32_t *column = p.slots + s;
     const int32_t id = column[uint64_t{static_cast<uint32_t>(begin)} * p.stride];
     bool parts = static_cast<uint32_t>(id) >= p.pages;
 #pragma unroll 8
@@ -1125,7 +1138,7 @@ entro_status check_groups(const entro_cache_groups *g) {
 
 constexpr uint32_t kShortTable = 512;                 // slots that one workgroup goes through
 constexpr uint64_t kHalfGroups = kMostGroups / 2;     // workgroups for shared and for own tokens
-constexpr uint32_t kMostShared = 48, kMostOwn = 16;   // parts of either: the join has a lane for each
+constexpr uint32_t kMostShared = 128, kMostOwn = kMostParts - kMostShared;
 
 struct SharedShape {
     bool many;
@@ -1152,15 +1165,19 @@ SharedShape shared_shape_of(const entro_cache *c, const entro_cache_table *t, co
     s.many = rows > 32;
     s.g.groups = groups->groups;
     s.g.row_tiles = s.many ? between((rows + kManyRows - 1) / kManyRows, 1, kHalfGroups / units) : 1;
-    // own tokens: at most 32 tiles a wavefront
+    // own tokens: up to 24 tiles in one piece; of longer ones as many pieces of 8 tiles and more as give every compute unit a workgroup (64 sequences with
+    // up to 33 tiles of their own behind 32768 shared tokens: one piece 113 us, two 106 to 110)
     const bool own_many = s.many && own_rows > 32;
     s.g.own_tiles = own_many ? between((own_rows + kManyRows - 1) / kManyRows, 1, kHalfGroups / own_units) : 0;
     const uint64_t own_fill = own_many ? own_units * s.g.own_tiles : (own_units + 3) / 4;
+    const uint64_t own_fills = (cus + own_fill - 1) / own_fill, own_least = (own_tiles + 23) / 24, own_most = (own_tiles + 7) / 8;
+    const uint64_t own_want = own_tiles <= 24 ? 1 : own_fills < own_least ? own_least : own_fills < own_most ? own_fills : own_most;
     uint64_t fit = kHalfGroups / own_fill;
-    s.g.own_splits = between((own_tiles + 31) / 32, 1, fit < kMostOwn ? fit : kMostOwn);
+    s.g.own_splits = between(own_want, 1, fit < kMostOwn ? fit : kMostOwn);
     s.g.own_least = between((own_tiles + s.g.own_splits - 1) / s.g.own_splits, 1, 0x7fffffff);
-    // shared tokens: one workgroup a compute unit, those for own tokens counted unless they are short, as two on one get in each other's way; where
-    // that leaves more than 16 tiles to a workgroup, two
+    // shared tokens: one workgroup a compute unit, those for own tokens counted unless they are short, as two on one wait for each other's loads (48
+    // sequences behind 4001 tokens, 96 workgroups for own tokens: 8 pieces, 128 workgroups for shared ones, 35 us, 12 pieces 45, 24 pieces 48); where that
+    // leaves more than 16 tiles to a workgroup, two (64 behind 32768, own tokens in one piece: 8, 16, 24, 32 pieces 156, 118, 108, 141 us)
     const uint64_t slots = cus * (entro_cache_width(c->head_dim) > 128 || (s.many && q->type == ENTRO_F32) ? 1 : 2);
     const uint64_t own_blocks = own_fill * s.g.own_splits, fill = units * s.g.row_tiles;
     const auto leaves = [&](uint64_t room) { return own_blocks < room && own_tiles > 3 ? room - own_blocks : room; };

@@ -181,7 +181,7 @@ __device__ inline float over_head(float v, uint32_t shift, F f) {
 }
 
 // The norm of a head, whose elements are x and, as they were read, raw.  All lanes are here.  Where the squares of some head of the wavefront leave the
-// range, all is done again on elements less the exponent of their head's largest one.
+// range, all is done again, for those heads on elements less the exponent of the largest one.
 template <typename T>
 __device__ inline void norm_head(const Turning &r, const Piece &c, const float *gain, bool gain_wide, const Raw<T> &raw, float *x) {
     constexpr uint32_t P = kRun, N = 2 * P;
@@ -208,7 +208,7 @@ __device__ inline void norm_head(const Turning &r, const Piece &c, const float *
 #pragma unroll
         for (uint32_t j = 0; j < N; ++j) most = fmaxf(most, fabsf(x[j]));
         most = over_head(most, r.shift, [](float a, float b) { return fmaxf(a, b); });
-        const int e = most > 1e17f && most < INFINITY ? static_cast<int>(__float_as_uint(most) >> 23) - 127 : 0;
+        const int e = !(mean < INFINITY) && most < INFINITY ? static_cast<int>(__float_as_uint(most) >> 23) - 127 : 0;
 #pragma unroll
         for (uint32_t j = 0; j < N; ++j) x[j] = ldexpf(x[j], -e);
         if (e) eps = fmaxf(ldexpf(eps, -2 * e), kLeastEps);

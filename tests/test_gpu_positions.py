@@ -133,6 +133,22 @@ def test_norms_of_extreme_heads(norm):
     assert np.isnan(got[6, 1, 5]) and np.isnan(got[7, 0, 0])
 
 
+@pytest.mark.parametrize("norm", ["rms", "centred"])
+def test_a_head_s_bits_do_not_depend_on_the_heads_beside_it(norm):
+    rng = np.random.default_rng(4)
+    turns, r = rotary(24, "halves", norm)
+    x = rng.standard_normal((7, 8, 24)).astype(np.float32)
+    x[:, ::3] *= np.float32(3e17)                               # squares within the range
+    rows_of = [x.copy(), x.copy()]
+    rows_of[1][:, 1::3], rows_of[1][0, 2] = np.nan, 1e30
+    got = []
+    for y in rows_of:
+        d = dev(y)
+        E.entro_rotate(r, E.RotaryRows(d), None, ints(range(7)))
+        got.append(d)
+    assert torch.equal(got[0][:, ::3], got[1][:, ::3]) and torch.equal(got[0][1:, 2::3], got[1][1:, 2::3])
+
+
 # ------------------------------------------------------------------------------------------------------- into the cache
 #          kind, heads, kv_heads, page, dim, dims, lengths, new
 APPEND = [("bf16", 32, 8, 64, 128, 128, [70, 1, 64, 128], [1, 1, 1, 1]), ("f32", 4, 2, 16, 24, 24, [40, 5, 0, 33], [40, 5, 0, 7]),

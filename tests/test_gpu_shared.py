@@ -297,6 +297,23 @@ def test_steps_of_beams_in_a_graph():
     assert max(seen) >= 96
 
 
+@pytest.mark.parametrize("kind,dim", [("bf16", 64), ("f32", 96), ("bf16", 192)])
+def test_more_than_64_sequences_and_more_than_64_parts(kind, dim):
+    """A group of 150 sequences (more than a wavefront has lanes); rows in parts of both kinds beyond 64, by hints that ask for them."""
+    rng = np.random.default_rng(12)
+    pool, table, lengths, shared = make(rng, [(128, [129 + i % 40 for i in range(150)]), (64, [70] * 3)], [], 1, 16, dim)
+    n = len(lengths)
+    q = rounded(rng.standard_normal((n, 2, dim)), kind)
+    out, lse = run(pool, table, lengths, [0, 150, n], shared, q, starts([1] * n), kind)
+    check_attend(pool, table, lengths, q, starts([1] * n), kind, out, lse, dim ** -0.5)
+    pool, table, lengths, shared = make(rng, [(6400, [6500, 6410])], [5000], 1, 16, dim)
+    q = rounded(rng.standard_normal((3, 2, dim)), kind)
+    out, lse = run(pool, table, lengths, [0, 2], shared, q, starts([1] * 3), kind, max_len=200000, max_shared=100000)
+    check_attend(pool, table, lengths, q, starts([1] * 3), kind, out, lse, dim ** -0.5)
+    out, lse = run(pool, table, lengths, [0, 2], shared, q, starts([1] * 3), kind, max_len=120000, max_shared=6400)
+    check_attend(pool, table, lengths, q, starts([1] * 3), kind, out, lse, dim ** -0.5)
+
+
 def test_refusals_on_the_gpu():
     rng = np.random.default_rng(11)
     pool, table, lengths, shared = make(rng, [(64, [70, 80])], [], 1, 16, 64)

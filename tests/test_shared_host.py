@@ -157,7 +157,7 @@ def test_what_is_shared_as_host_code(host, first_wave, first, long):
 @pytest.mark.parametrize("seqs,stride,kv_heads,group,tokens,groups", [(64, 128, 8, 4, 64, 1), (64, 128, 8, 4, 3000, 16), (1, 8, 1, 1, 1, 1), (1, 1 << 20, 8, 8, 1 << 20, 5),
                                                                       (4096, 4096, 32, 1, 4096, 4096), (60000, 30000, 64, 1, 60000, 2), (7, 100, 2, 16, 40, 100000)])
 def test_hints_of_any_size_make_launches_that_a_gpu_takes(host, seqs, stride, kv_heads, group, tokens, groups):
-    """Whatever hints say: less than 2^32 lanes along x, less than 2^16 workgroups along y, a workspace of 64 parts a row at most, and the call succeeds."""
+    """Whatever hints say: less than 2^32 lanes along x, less than 2^16 workgroups along y, a workspace of 256 parts a row at most, and the call succeeds."""
     at, out = 1 << 16, (C.c_uint64 * 3000)()
     cache, table = B.CCache(at, at, at, at, 1, 1 << 20, 64, kv_heads, 64, 0), B.CCacheTable(at, at, seqs, stride)
     row = kv_heads * 64
@@ -172,7 +172,7 @@ def test_hints_of_any_size_make_launches_that_a_gpu_takes(host, seqs, stride, kv
                         g = B.CCacheGroups(at, at, groups, max_seqs, max_shared, 0)
                         refs = [C.byref(x) for x in (cache, table, query, g)]
                         need = host.entro_cache_attend_shared_workspace_bytes(*refs)
-                        assert 0 < need <= tokens * kv_heads * group * 64 * 65 * 4
+                        assert 0 < need <= tokens * kv_heads * group * 256 * 65 * 4
                         assert host.entro_cache_attend_shared(*refs, at, need, None) == B.ENTRO_OK
         n = host.host_launches(out, 3000)
         assert n == 3 * 2 * 6 * 18
