@@ -471,7 +471,8 @@ struct ManyLds {
     int32_t ok[2][4];
 };
 
-template <int W, typename T, int MODE>
+// ONE: a tile lies in one page (of 64 tokens and more). Its number is then a scalar, and so is all of the codes' addresses but a lane's place in the tile.
+template <int W, typename T, int MODE, bool ONE = false>
 __device__ __forceinline__ void attend_many(const Pool &p, const Query &a, const Part &w, uint32_t tile_from_end, uint32_t row_tiles, ManyLds<W> &lds) {
     constexpr int kThreads = kWG, kRows = kManyRows;
     constexpr int kParts = sizeof(T) == 2 ? 1 : 3, kWeights = sizeof(T) == 2 ? 2 : 3;
@@ -578,6 +579,10 @@ __device__ __forceinline__ void attend_many(const Pool &p, const Query &a, const
         int32_t s_ok = 0;
         const auto ask_pages = [&](int32_t i) {
             const int32_t t0 = tiles.at(min(i, end - 1)) * kTile;
+            if constexpr (ONE) {
+                s_page = table_entry(p, b, t0);
+                return;
+            }
 #pragma unroll
             for (int n = 0; n < kChunks; ++n) {
                 const int32_t ch = n * kThreads + static_cast<int32_t>(tid);
@@ -588,6 +593,24 @@ __device__ __forceinline__ void attend_many(const Pool &p, const Query &a, const
         };
         const auto ask_codes = [&](int32_t i) {
             const int32_t t0 = tiles.at(min(i, end - 1)) * kTile;
+            if constexpr (ONE) {
+                const int32_t id = __builtin_amdgcn_readfirstlane(checked_page(p, s_page, t0));
+                const uint64_t page = static_cast<uint32_t>(max(id, 0));
+                const uint32_t at = static_cast<uint32_t>(t0) & in_page;
+                const uint8_t *k = k_head + page * page_stride + at * W, *v = v_head + page * page_stride + at;
+#pragma unroll
+                for (int n = 0; n < kChunks; ++n) {
+                    const uint32_t ch = min(static_cast<uint32_t>(n * kThreads) + tid, W * 4u - 1);
+                    kc[n] = *reinterpret_cast<const u32x4 *>(k + 16 * ch);
+                    vc[n] = *reinterpret_cast<const u32x4 *>(v + (((ch >> 2) << p.page_shift) + 16 * (ch & 3u)));
+                }
+                if (wave == 0) {
+                    ks = p.k_scale[page * p.kv_heads + head];
+                    vs = p.v_scale[page * p.kv_heads + head];
+                    s_ok = id >= 0;
+                }
+                return;
+            }
 #pragma unroll
             for (int n = 0; n < kChunks; ++n) {
                 const int32_t ch = min(n * kThreads + static_cast<int32_t>(tid), W * 4 - 1);
@@ -965,8 +988,13 @@ __global__ __launch_bounds__(kWG, MANY ? (sizeof(T) == 2 && W <= 128 ? 2 : 1) : 
         take_group(p, a, g, unit / p.kv_heads, &w);
         if (w.s.count == 0) return;
         w.table = w.first;
-        if constexpr (MANY) attend_many<W, T, kShared>(p, a, w, blockIdx.x / units / g.splits, g.row_tiles, lds.many);
-        else attend_few<W, T, kShared>(p, a, w, lds.few);
+        if constexpr (MANY) {
+            const uint32_t tile = blockIdx.x / units / g.splits;
+            if (p.page_shift >= 6) attend_many<W, T, kShared, true>(p, a, w, tile, g.row_tiles, lds.many);
+            else attend_many<W, T, kShared, false>(p, a, w, tile, g.row_tiles, lds.many);
+        } else {
+            attend_few<W, T, kShared>(p, a, w, lds.few);
+        }
         return;
     }
     // few rows: a wavefront for itself takes a sequence, key head and split, so that heads whose codes lie side by side are in one workgroup
