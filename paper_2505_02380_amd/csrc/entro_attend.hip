@@ -897,6 +897,12 @@ __global__ __launch_bounds__(kWG) void k_attend_join_rows(Pool p, Query a) {
 // are read, turned and multiplied once and not once a sequence; every sequence's further tokens go by the same launch's other
 // workgroups, and k_shared_join brings the parts of a row together.  What is shared is rounded down to whole tiles, and to
 // what all of the group's rows see where there is no window; the rest of it is taken as each sequence's own.
+//
+// Bound by issue for many rows of long prefixes: 64 sequences of 32 / 8 heads of 128 behind 32768 shared and up to 2048 own tokens 95 us (of
+// a compute unit's time vector instructions 48 %, matrix instructions 30 %; wavefronts wait for a third of theirs), the shared ones alone 72 (0.48 PFLOP/s; each sequence for
+// itself, 64 of 32768 tokens and more, is 2.3 GB of codes).  Short ones are bound by the way to the first tile (bounds of
+// the group 3 us, queries, page and codes 4 to 5) and by 2.3 us a tile: 48 answers to 4001 tokens 25 us and 5 for the join.  fp32 rows: one
+// wavefront a SIMD, and three times the matrix instructions (five groups of pieces, 216 us).
 struct Groups {
     const int32_t *first, *shared;
     uint32_t groups;
@@ -1194,7 +1200,7 @@ SharedShape shared_shape_of(const entro_cache *c, const entro_cache_table *t, co
     s.g.groups = groups->groups;
     s.g.row_tiles = s.many ? between((rows + kManyRows - 1) / kManyRows, 1, kHalfGroups / units) : 1;
     // own tokens: up to 24 tiles in one piece; of longer ones as many pieces of 8 tiles and more as give every compute unit a workgroup (64 sequences with
-    // up to 33 tiles of their own behind 32768 shared tokens: one piece 113 us, two 106 to 110)
+    // up to 33 tiles of their own behind 32768 shared tokens: one piece 101 us at the best, two 94, four 94)
     const bool own_many = s.many && own_rows > 32;
     s.g.own_tiles = own_many ? between((own_rows + kManyRows - 1) / kManyRows, 1, kHalfGroups / own_units) : 0;
     const uint64_t own_fill = own_many ? own_units * s.g.own_tiles : (own_units + 3) / 4;
@@ -1204,8 +1210,9 @@ SharedShape shared_shape_of(const entro_cache *c, const entro_cache_table *t, co
     s.g.own_splits = between(own_want, 1, fit < kMostOwn ? fit : kMostOwn);
     s.g.own_least = between((own_tiles + s.g.own_splits - 1) / s.g.own_splits, 1, 0x7fffffff);
     // shared tokens: one workgroup a compute unit, those for own tokens counted unless they are short, as two on one wait for each other's loads (48
-    // sequences behind 4001 tokens, 96 workgroups for own tokens: 8 pieces, 128 workgroups for shared ones, 35 us, 12 pieces 45, 24 pieces 48); where that
-    // leaves more than 16 tiles to a workgroup, two (64 behind 32768, own tokens in one piece: 8, 16, 24, 32 pieces 156, 118, 108, 141 us)
+    // sequences behind 4001 tokens, 96 workgroups for own tokens: 8, 10, 12, 24 pieces of the shared ones, 16 workgroups each, 31, 29, 35, 37 us); where that
+    // leaves more than 16 tiles to a workgroup, two (64 behind 32768, 256 workgroups for own tokens: 8, 12, 16, 20, 32 pieces 151, 109, 94, 112, 107 us;
+    // without own tokens 147, 105, 84, 91, 72)
     const uint64_t slots = cus * (entro_cache_width(c->head_dim) > 128 || (s.many && q->type == ENTRO_F32) ? 1 : 2);
     const uint64_t own_blocks = own_fill * s.g.own_splits, fill = units * s.g.row_tiles;
     const auto leaves = [&](uint64_t room) { return own_blocks < room && own_tiles > 3 ? room - own_blocks : room; };
