@@ -187,7 +187,7 @@ __device__ inline void norm_head(const Turning &r, const Piece &c, const float *
     constexpr uint32_t P = kRun, N = 2 * P;
     const auto here = [&](uint32_t j) { return j % P < c.count[j / P]; };
     const auto add = [](float a, float b) { return a + b; };
-    const auto mean_square = [&]() {
+    const auto squares = [&]() {
         if (r.norm == ENTRO_NORM_CENTRED) {
             float sum = 0.0f;
 #pragma unroll
@@ -199,22 +199,22 @@ __device__ inline void norm_head(const Turning &r, const Piece &c, const float *
         float sum = 0.0f;
 #pragma unroll
         for (uint32_t j = 0; j < N; ++j) sum = fmaf(x[j], x[j], sum);
-        return over_head(sum, r.shift, add) * r.inverse_dim;
+        return over_head(sum, r.shift, add);
     };
-    float mean = mean_square(), eps = r.eps;
-    if (__any(!(mean < INFINITY))) {
+    float sum = squares(), eps = r.eps;
+    if (__any(!(sum < INFINITY))) {
         head_values<T>(raw, x);
         float most = 0.0f;
 #pragma unroll
         for (uint32_t j = 0; j < N; ++j) most = fmaxf(most, fabsf(x[j]));
         most = over_head(most, r.shift, [](float a, float b) { return fmaxf(a, b); });
-        const int e = !(mean < INFINITY) && most < INFINITY ? static_cast<int>(__float_as_uint(most) >> 23) - 127 : 0;
+        const int e = !(sum < INFINITY) && most < INFINITY ? static_cast<int>(__float_as_uint(most) >> 23) - 127 : 0;
 #pragma unroll
         for (uint32_t j = 0; j < N; ++j) x[j] = ldexpf(x[j], -e);
         if (e) eps = fmaxf(ldexpf(eps, -2 * e), kLeastEps);
-        mean = mean_square();
+        sum = squares();
     }
-    const float by = rsqrtf(mean + eps);
+    const float by = rsqrtf(fmaf(sum, r.inverse_dim, eps));
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         if (!gain) {

@@ -185,8 +185,6 @@ def same_pool(a, b):
 def test_append_rotated_is_rotate_then_append(case, layout, norm):
     """The same codes and scales as keys rotated to fp32 rows and appended, whatever the blocks held before; the same queries as rotate's."""
     kind, q_heads, heads, page, dim, dims, lengths, new = APPEND[case]
-    if kind == "bf16":
-        norm = "none"                                           # sums of 8 elements a lane where fp32 rows have 4
     rng = np.random.default_rng(case)
     pool, table = pool_and_table(rng, lengths, heads, page, dim)
     if case % 2:
