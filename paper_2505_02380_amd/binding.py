@@ -391,7 +391,7 @@ def to_device(enc: EncodedTensor, device="cuda") -> DeviceTensor:
 def _stream_ptr(stream) -> Optional[int]:
     if stream is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        return torch.cuda.current_stream(torch.cuda.current_device()).cuda_stream          # (by its number: without one torch takes longer to find it)
     return getattr(stream, "cuda_stream", stream)
 
 
@@ -569,8 +569,8 @@ def _rows_type(x, what: str) -> int:
 
 def _ints(x, n: Optional[int], what: str):
     import torch
-    _need(x.dtype == torch.int32 and x.is_contiguous() and (n is None or x.numel() == n), f"{what} is a contiguous int32 tensor"
-          + ("" if n is None else f" of {n}"))
+    if x.dtype != torch.int32 or not x.is_contiguous() or (n is not None and x.numel() != n):
+        raise ValueError(f"{what} is a contiguous int32 tensor" + ("" if n is None else f" of {n}"))
     return x.data_ptr()
 
 
@@ -754,9 +754,10 @@ class Rotary:
         self.device = _device_of(*given) if given else True              # True: there is nothing that lies anywhere
         at, stride = (lambda x: None if x is None else x.data_ptr()), (lambda g: 0 if g is None or g.dim() == 1 else g.stride(0))
         self.c = CRotary(at(turns), at(q_gain), at(k_gain), stride(q_gain), stride(k_gain), dims, layout, norm, eps, amplitude, 0)
+        self.q_shape, self.k_shape = (None if g is None else tuple(g.shape) for g in (q_gain, k_gain))
 
-    def fits(self, gain, heads: int, head_dim: int):
-        _need(gain is None or gain.shape == (head_dim,) or gain.shape == (heads, head_dim), "gains are [head_dim] or [heads][head_dim]")
+    def fits(self, shape, heads: int, head_dim: int):
+        _need(shape is None or shape == (head_dim,) or shape == (heads, head_dim), "gains are [head_dim] or [heads][head_dim]")
 
 
 class RotaryRows:
@@ -765,7 +766,7 @@ class RotaryRows:
     def __init__(self, x, y=None):
         y = x if y is None else y
         _need(x.shape == y.shape and x.dtype == y.dtype, "x and y have one shape and type")
-        self.x, self.y, self.device, self.type = x, y, _device_of(x, y), _rows_type(x, "x")
+        self.x, self.y, self.device, self.type, self.shape = x, y, _device_of(x, y), _rows_type(x, "x"), tuple(x.shape)
         self.c = CRotaryRows(x.data_ptr(), y.data_ptr(), *_row_strides(x, "x"), *_row_strides(y, "y"), x.shape[1], 0)
         _need(_own_places(y), "y's elements have places of their own")
 
@@ -783,14 +784,15 @@ def entro_rotate(rotary: Rotary, q: Optional[RotaryRows], k: Optional[RotaryRows
     """Norms and rotations of q and k (either may be None) at positions, int32 [tokens]."""
     side = q if k is None else k
     _need(side is not None, "q or k is given")
-    tokens, heads, dim = side.x.shape
+    tokens, heads, dim = side.shape
     if q is not None:
-        _need(side is q or (q.x.shape[0] == tokens and q.x.shape[2] == dim and q.type == side.type), "q and k have one type, as many tokens and dimensions")
-        rotary.fits(rotary.q_gain, q.x.shape[1], dim)
+        rows, q_heads, q_dim = q.shape
+        _need(rows == tokens and q_dim == dim and q.type == side.type, "q and k have one type, as many tokens and dimensions")
+        rotary.fits(rotary.q_shape, q_heads, dim)
     if k is not None:
-        rotary.fits(rotary.k_gain, heads, dim)
+        rotary.fits(rotary.k_shape, heads, dim)
     at, device = _ints(positions, tokens, "positions"), positions.device
-    _need(device.type == "cuda" and all(s is None or s.device == device for s in (q, k)) and (rotary.device is True or rotary.device == device),
+    _need(device.type == "cuda" and (q is None or q.device == device) and (k is None or k.device == device) and (rotary.device is True or rotary.device == device),
           "all tensors of a call lie on one GPU")
     _run_on(device, lambda: _check(lib().entro_rotate(C.byref(rotary.c), None if q is None else C.byref(q.c), None if k is None else C.byref(k.c), at, tokens, dim,
                                                       side.type, _stream_ptr(stream)), "entro_rotate"))
@@ -800,11 +802,11 @@ def entro_cache_append_rotated(cache: Cache, table: CacheTable, rows: CacheRows,
     """entro_cache_append of keys that are normed and rotated on their way, and `queries` normed and rotated beside them."""
     _same_heads(cache, table, rows.k, rows.start)
     _need(rows.k.shape[1] == cache.kv_heads, f"rows have {cache.kv_heads} heads")
-    rotary.fits(rotary.k_gain, cache.kv_heads, cache.head_dim)
+    rotary.fits(rotary.k_shape, cache.kv_heads, cache.head_dim)
     if queries is not None:
-        x = queries.x
-        _need(x.dtype == rows.k.dtype and x.shape[0] == rows.k.shape[0] and x.shape[2] == cache.head_dim, "queries have the type, tokens and dimensions of the rows")
-        rotary.fits(rotary.q_gain, x.shape[1], cache.head_dim)
+        tokens, heads, dim = queries.shape
+        _need(queries.type == rows.c.type and tokens == rows.c.tokens and dim == cache.head_dim, "queries have the type, tokens and dimensions of the rows")
+        rotary.fits(rotary.q_shape, heads, dim)
     _on_gpu(cache, table, rows, queries, None if rotary.device is True else rotary)
     q = None if queries is None else C.byref(queries.c)
     _run_on(cache.device, lambda: _check(lib().entro_cache_append_rotated(C.byref(cache.c), C.byref(table.c), C.byref(rows.c), C.byref(rotary.c), q,
