@@ -1170,7 +1170,9 @@ entro_status check_groups(const entro_cache_groups *g) {
     return aligned16(g->first) && aligned16(g->shared) ? ENTRO_OK : ENTRO_ERR_ALIGN;
 }
 
-constexpr uint32_t kShortTable = 512;                 // slots that one workgroup goes through
+// Slots that one workgroup a group goes through; longer tables take two launches (8 groups of 8 rows, one and two: 100 slots 3.6 and 4.7 us, 200 4.4
+// and 4.8, 300 5.6 and 4.8, 800 10.5 and 5.2).
+constexpr uint32_t kShortTable = 256;
 constexpr uint64_t kHalfGroups = kMostGroups / 2;     // workgroups for shared and for own tokens
 constexpr uint32_t kMostShared = 128, kMostOwn = kMostParts - kMostShared;
 
@@ -1196,6 +1198,8 @@ SharedShape shared_shape_of(const entro_cache *c, const entro_cache_table *t, co
     const uint64_t shared = groups->max_shared < q->max_len ? groups->max_shared : q->max_len;
     const uint64_t tiles = tiles_in(shared, q, max_new), own_tiles = tiles_in(uint64_t{q->max_len} - shared + kTile, q, max_new);
     const uint64_t cus = static_cast<uint64_t>(compute_units()), units = uint64_t{groups->groups} * c->kv_heads, own_units = uint64_t{t->seqs} * c->kv_heads;
+    // rows of a key head over 8192 and 32768 tokens of 8 of them, by tiles of 16 rows and of 128: 16 rows 16, 24 and 20, 47 us; 32 rows 22, 37 and 20, 47;
+    // 40 rows 29, 51 and 21, 48; in fp32 over 8192 32 rows 26 and 33, 64 rows 45 and 38
     s.many = rows > 32;
     s.g.groups = groups->groups;
     s.g.row_tiles = s.many ? between((rows + kManyRows - 1) / kManyRows, 1, kHalfGroups / units) : 1;

@@ -12,8 +12,12 @@ constexpr int kWG = 256;
 // Heads that a lane group takes one after the other in large calls, with the angles of its position found once: 8192 rows of 40 heads of 128 in bf16,
 // four heads 41 us, eight 38; 4999 rows of 24 heads of 80 in fp32, four 26 us, eight 37 (152 registers).
 template <typename T> constexpr uint32_t kHeads = sizeof(T) == 2 ? 8 : 4;
-constexpr uint64_t kManyLanes = 64 * 2048;   // a call is large from here on: two wavefronts for every SIMD
-constexpr uint64_t kApartLanes = 64 * 8192;  // and its queries are rotated by a launch of their own
+// A call is large from so many lanes on (one head a lane group and several: 40 heads of 128 in bf16, 1600 rows 13.6 and 15.2 us, 2400 18.5 and 17.5, 3200
+// 23.4 and 20.8; 24 heads of 80 in fp32, 3200 rows 18.6 and 21.1),
+template <typename T> constexpr uint64_t kManyLanes = sizeof(T) == 2 ? 64 * 2560 : 64 * 6144;
+// and from so many on the queries of rows for the cache have a launch of their own (32 query and 8 key heads of 128 in bf16, written and read, one launch and
+// two: 3200 rows 42.5 and 45 us, 6400 76 and 78, 12 800 160 and 131).
+constexpr uint64_t kApartLanes = 64 * 8192;
 constexpr float kLeastEps = 1.2e-38f;
 
 struct Turning {
@@ -483,7 +487,7 @@ Side side_of(const entro_rotary_rows *s, const float *gain, uint32_t gain_stride
 template <typename T, bool kPairs>
 void launch_rotate(const Turning &r, const Side &q, const Side &k, const int32_t *positions, uint32_t tokens, hipStream_t st) {
     const uint32_t heads = q.heads + k.heads, few = (heads + kHeads<T> - 1) / kHeads<T>;
-    const bool many = ((uint64_t{tokens} * few) << r.shift) >= kManyLanes;
+    const bool many = ((uint64_t{tokens} * few) << r.shift) >= kManyLanes<T>;
     const uint32_t per_token = many ? few : heads, items = tokens * per_token;
     const uint64_t groups = (uint64_t{items} + (kWG >> r.shift) - 1) / (kWG >> r.shift);
     const dim3 grid(static_cast<uint32_t>(groups < (1u << 23) ? groups : 1u << 23));

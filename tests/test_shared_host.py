@@ -133,14 +133,15 @@ template <int W, typename T, typename... A> void k_shared_join(const A &...) {}
 def test_what_is_shared_as_host_code(host, first_wave, first, long):
     host.host_first_wave(first_wave)
     rng, mem = np.random.default_rng(len(first)), Memory()
-    page, pages, stride = 16, 900, 300
+    page, pages, stride = 16, 900, 250
     table = np.tile(rng.permutation(pages)[:stride], (5, 1))
-    lengths = np.array([4800, 4790, 4800, 4500, 5000])
-    table[3:, 270:] = 0
-    table[2, 290], table[1, 258] = 5, 7
+    lengths = np.array([4000, 3990, 4000, 3700, 4200])
+    table[3:, 220:] = 0
+    table[2, 240], table[1, 208] = 5, 7
     if long:
-        table = np.concatenate([np.full((5, 1), 3), table[:, :299], table], 1)
-        stride, lengths = 600, np.array([9600, 9590, 9600, 9300, 9700])
+        table = np.concatenate([np.full((5, 1), 3), table, table], 1)
+        stride = table.shape[1]
+        lengths = stride * page - np.array([0, 10, 0, 300, -100])
     slots, at = mem(table, np.int32), mem(lengths, np.int32)
     begin, out = mem(first, np.int32), mem(np.full(len(first) + 1, 77), np.int32)
     cache, t, g = B.CCache(PTR, PTR, PTR, PTR, 1, pages, page, 1, 64, 0), B.CCacheTable(slots.ctypes.data, at.ctypes.data, 5, stride), B.CCacheGroups(
