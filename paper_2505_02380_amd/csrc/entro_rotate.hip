@@ -193,12 +193,16 @@ __device__ inline void norm_head(const Turning &r, const Piece &c, const float *
     const auto add = [](float a, float b) { return a + b; };
     const auto squares = [&]() {
         if (r.norm == ENTRO_NORM_CENTRED) {
-            float sum = 0.0f;
+            // twice: the rounded sum and inverse leave part of a mean that is large beside the elements' spread
 #pragma unroll
-            for (uint32_t j = 0; j < N; ++j) sum += x[j];
-            sum = over_head(sum, r.shift, add);
+            for (int i = 0; i < 2; ++i) {
+                float sum = 0.0f;
 #pragma unroll
-            for (uint32_t j = 0; j < N; ++j) x[j] = here(j) ? fmaf(-sum, r.inverse_dim, x[j]) : 0.0f;
+                for (uint32_t j = 0; j < N; ++j) sum += x[j];
+                sum = over_head(sum, r.shift, add);
+#pragma unroll
+                for (uint32_t j = 0; j < N; ++j) x[j] = here(j) ? fmaf(-sum, r.inverse_dim, x[j]) : 0.0f;
+            }
         }
         float sum = 0.0f;
 #pragma unroll

@@ -149,6 +149,21 @@ def test_a_head_s_bits_do_not_depend_on_the_heads_beside_it(norm):
     assert torch.equal(got[0][:, ::3], got[1][:, ::3]) and torch.equal(got[0][1:, 2::3], got[1][1:, 2::3])
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("tokens", [3, 13000])
+@pytest.mark.parametrize("dim", [17, 80, 96, 112, 128])
+def test_centred_norm_of_heads_far_from_zero(dim, tokens, kind):
+    """Equal elements give nothing, whatever their mean's rounding, in small calls and large ones."""
+    rng = np.random.default_rng(dim)
+    x = dev(np.tile(rot.far_heads(rng, dim)[None], (tokens, 1, 1))).to(TYPES[kind])
+    _, r = rotary(0, "halves", "centred", eps=1e-6)
+    y = torch.full_like(x, 7)
+    E.entro_rotate(r, E.RotaryRows(x, y), None, ints(range(tokens)))
+    want, bound = rot.centred(x[:1].float().cpu().numpy(), 1e-6)
+    check(y[:1], want, bound, kind)
+    assert torch.equal(y, y[:1].expand_as(y))
+
+
 # ------------------------------------------------------------------------------------------------------- into the cache
 #          kind, heads, kv_heads, page, dim, dims, lengths, new
 APPEND = [("bf16", 32, 8, 64, 128, 128, [70, 1, 64, 128], [1, 1, 1, 1]), ("f32", 4, 2, 16, 24, 24, [40, 5, 0, 33], [40, 5, 0, 7]),

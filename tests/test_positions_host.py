@@ -210,6 +210,22 @@ def test_rotate_as_host_code(host, dim, dims, norm, layout):
         assert np.all(np.abs(b[1:-1] - want) <= rot.tolerance(want, bound, "f32")) and np.all(b[[0, -1]] == 7)
 
 
+@pytest.mark.parametrize("dim", [17, 80, 96, 112, 128, 192])
+def test_centred_norm_of_heads_far_from_zero(host, dim):
+    """Heads whose elements are equal, or nearly so, give what is left after their mean and not the mean's own rounding."""
+    rng = np.random.default_rng(dim)
+    mem, eps = Memory(), 1e-6
+    heads = rot.far_heads(rng, dim)
+    x = mem(heads[None], np.float32)
+    y, at = mem(np.zeros_like(x)), mem([5], np.int32)
+    rotary = B.CRotary(None, None, None, 0, 0, 0, 0, 2, eps, 1.0, 0)
+    side = B.CRotaryRows(x.ctypes.data, y.ctypes.data, x[0].size, dim, x[0].size, dim, len(heads), 0)
+    host.host_first_wave(0)
+    assert host.entro_rotate(C.byref(rotary), C.byref(side), None, at.ctypes.data, 1, dim, E.ENTRO_F32, None) == B.ENTRO_OK
+    want, bound = rot.centred(x, eps)
+    assert np.all(np.abs(y - want) <= bound), np.argwhere(~(np.abs(y - want) <= bound))[:4]
+
+
 @pytest.mark.parametrize("first_wave", [0, 1, 3])
 @pytest.mark.parametrize("page,dim,dims", [(64, 128, 128), (16, 24, 16)])
 def test_append_rotated_moves_older_codes_whichever_wavefront_comes_first(host, first_wave, page, dim, dims):
