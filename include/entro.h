@@ -595,9 +595,10 @@ typedef struct {
 } entro_cache_groups;
 
 /* shared[g] = page_tokens times the number of leading slots in which all rows of t in group g name the same page (one of the
- * pool's) and hold page_tokens tokens; 0 for a group without sequences.  Pages that regroup shares are found whoever forked from whom; a program
- * that forks only within its groups may also keep older values, as what its sequences share only grows.  (For the phase of "Latency
- * Reduction from Huffman Coding"; no passage of the paper defines it.) */
+ * pool's) and hold page_tokens tokens; 0 for a group without sequences.  Pages that regroup shares are found whoever forked from whom.
+ * An older value may be kept as long as every row of its group has gone on from a row of the group, with no token taken back and no page dropped
+ * by a window: then what they share has only grown.  Otherwise it may have shrunk, and the value is to be written anew.  (For the phase of
+ * "Latency Reduction from Huffman Coding"; no passage of the paper defines it.) */
 entro_status entro_cache_shared(const entro_cache *c, const entro_cache_table *t, const entro_cache_groups *g, void *hip_stream);
 
 /* Bytes of device workspace entro_cache_attend_shared needs for these sizes on the current device.  Only hints and sizes count, no pointer is

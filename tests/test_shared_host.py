@@ -9,7 +9,7 @@ import cache_reference as ref
 import paper_2505_02380_amd as E
 from paper_2505_02380_amd import binding as B
 from test_cache_host import Placed, calls_made  # noqa: F401
-from test_cache_on_cpu import HINTS, Memory, compiled, source
+from test_cache_on_cpu import HINTS, Memory, compiled, own_memory, page_call, source
 
 PTR = 0x10000          # an address that is aligned; no call below gets as far as using it
 
@@ -153,6 +153,45 @@ def test_what_is_shared_as_host_code(host, first_wave, first, long):
             n += 1
         assert out[i] == n * page
     assert list(out[-2:]) == [77, 77]
+
+
+@pytest.mark.parametrize("what", ["fork", "take back", "window", "end"])
+def test_what_a_group_shares_shrinks_where_tokens_or_pages_go(host, what):
+    """Three rows behind 64 tokens of a prompt, forked among themselves and grown: they share no less than before. With tokens of one taken back and others in
+    their place, pages dropped by a window or a row that ends and begins anew they share less, though every row goes on from one of the group."""
+    host.host_first_wave(0)
+    host.entro_cache_regroup.argtypes = B.lib().entro_cache_regroup.argtypes
+    host.entro_cache_pages_workspace_bytes.restype = C.c_uint64
+    mem, page, pages, rows, stride = Memory(), 16, 60, 3, 20
+    pool = ref.Pool(np.random.default_rng(1), 1, pages, 1, page, 1)
+    own_memory(mem, pool)
+    table, lengths = np.full((rows, stride), -1, np.int32), np.array([64, 64, 64], np.int32)
+    table[:, :4] = [7, 3, 11, 20]
+
+    def shared():
+        slots, at, first, out = mem(table, np.int32), mem(lengths, np.int32), mem([0, rows], np.int32), mem([77], np.int32)
+        cache, t, g = B.CCache(PTR, PTR, PTR, PTR, 1, pages, page, 1, 1, 0), B.CCacheTable(slots.ctypes.data, at.ctypes.data, rows, stride), B.CCacheGroups(
+            first.ctypes.data, out.ctypes.data, 1, rows, 64, 0)
+        assert host.entro_cache_shared(C.byref(cache), C.byref(t), C.byref(g), None) == B.ENTRO_OK
+        n = 0
+        while all((n + 1) * page <= lengths[r] and table[r, n] == table[0, n] and table[r, n] >= 0 for r in range(rows)):
+            n += 1
+        assert out[0] == n * page
+        return n * page
+
+    def regroup(parent, grow, window=0):
+        parent, grow = mem(parent, np.int32), mem(grow, np.int32)
+        to, then, status = page_call(host, mem, pool, table, lengths, rows, stride, lambda c, t, n, st, ws, size: host.entro_cache_regroup(
+            c, t, parent.ctypes.data, grow.ctypes.data, window, 0, n, st, ws, size, None))
+        assert status[0] == 0
+        return to, then
+    before = shared()
+    assert before == 64
+    steps = {"fork": [([0, 1, 2], [40, 7, 20]), ([0, 0, 2], [1, 1, 1])], "take back": [([0, 1, 2], [-30, 5, 5]), ([0, 1, 2], [60, 60, 60])],
+             "window": [([0, 1, 2], [200, 1, 2], 0), ([0, 1, 2], [1, 1, 1], 50)], "end": [([-1, 1, 2], [0, 5, 5]), ([0, 1, 2], [100, 5, 5])]}[what]
+    for step in steps:
+        table, lengths = regroup(*step)
+    assert shared() >= before if what == "fork" else shared() < before
 
 
 @pytest.mark.parametrize("seqs,stride,kv_heads,group,tokens,groups", [(64, 128, 8, 4, 64, 1), (64, 128, 8, 4, 3000, 16), (1, 8, 1, 1, 1, 1), (1, 1 << 20, 8, 8, 1 << 20, 5),
