@@ -67,7 +67,9 @@ class Generation:
                                    q_gain=torch.ones(dim, device=dev), k_gain=torch.ones(dim, device=dev))
             self.query_rows = E.RotaryRows(rows(layer.q, heads))                    # rotated where they lie
         if shared:
-            self.groups = E.CacheGroups(torch.tensor([0, beams], dtype=torch.int32, device=dev), torch.zeros(1, dtype=torch.int32, device=dev), beams, most_tokens)
+            # beams may share all of their tokens, or part early and go on alone
+            self.groups = E.CacheGroups(torch.tensor([0, beams], dtype=torch.int32, device=dev), torch.zeros(1, dtype=torch.int32, device=dev), beams, most_tokens,
+                                        max_own=most_tokens)
             need = E.entro_cache_attend_shared_workspace_bytes(self.cache, self.tables[0], self.query, self.groups)
         else:
             need = E.entro_cache_attend_workspace_bytes(self.cache, self.tables[0], self.query)

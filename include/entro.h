@@ -591,7 +591,8 @@ typedef struct {
                                   * read by entro_cache_attend_shared */
     uint32_t groups;
     uint32_t max_seqs, max_shared;   /* most sequences and most shared tokens of a group: hints, as max_new and max_len */
-    uint32_t reserved;           /* 0 */
+    uint32_t max_own;            /* most tokens of a sequence behind what its group shares, all of them where it is in none: a hint, too; 0: max_len less
+                                  * max_shared, which is too few where a long sequence shares little: few wavefronts then go through what it has alone */
 } entro_cache_groups;
 
 /* shared[g] = page_tokens times the number of leading slots in which all rows of t in group g name the same page (one of the

@@ -77,7 +77,7 @@ class CCacheQuery(C.Structure):
 
 class CCacheGroups(C.Structure):
     _fields_ = [("first", C.c_void_p), ("shared", C.c_void_p), ("groups", C.c_uint32), ("max_seqs", C.c_uint32), ("max_shared", C.c_uint32),
-                ("reserved", C.c_uint32)]
+                ("max_own", C.c_uint32)]
 
 
 class CRotary(C.Structure):
@@ -816,13 +816,13 @@ def entro_cache_append_rotated(cache: Cache, table: CacheTable, rows: CacheRows,
 # ---------------------------------------------------------------------------------------------------- groups behind a prefix
 class CacheGroups:
     """Groups of sequences that begin with the same pages. first: int32 [groups + 1], ascending; shared: int32 [groups], tokens in shared pages
-    (entro_cache_shared writes it)."""
+    (entro_cache_shared writes it); max_own: most tokens that a sequence has behind those (0: max_len less max_shared)."""
 
-    def __init__(self, first, shared, max_seqs: int, max_shared: int):
+    def __init__(self, first, shared, max_seqs: int, max_shared: int, max_own: int = 0):
         n = first.numel() - 1
         _need(n > 0, "first is [groups + 1]")
         self.first, self.shared, self.device = first, shared, _device_of(first, shared)
-        self.c = CCacheGroups(_ints(first, None, "first"), _ints(shared, n, "shared"), n, max_seqs, max_shared, 0)
+        self.c = CCacheGroups(_ints(first, None, "first"), _ints(shared, n, "shared"), n, max_seqs, max_shared, max_own)
 
 
 def entro_cache_shared(cache: Cache, table: CacheTable, groups: CacheGroups, stream=None):

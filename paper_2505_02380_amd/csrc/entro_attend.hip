@@ -1196,7 +1196,8 @@ SharedShape shared_shape_of(const entro_cache *c, const entro_cache_table *t, co
     const uint64_t seqs = between(groups->max_seqs, 1, t->seqs), own_rows = uint64_t{max_new} * group;
     const uint64_t all = seqs * max_new, rows = (all < q->tokens ? all : q->tokens) * group;
     const uint64_t shared = groups->max_shared < q->max_len ? groups->max_shared : q->max_len;
-    const uint64_t tiles = tiles_in(shared, q, max_new), own_tiles = tiles_in(uint64_t{q->max_len} - shared + kTile, q, max_new);
+    const uint64_t alone = groups->max_own < 1 ? q->max_len - shared : groups->max_own < q->max_len ? groups->max_own : q->max_len;
+    const uint64_t tiles = tiles_in(shared, q, max_new), own_tiles = tiles_in(alone + kTile, q, max_new);
     const uint64_t cus = static_cast<uint64_t>(compute_units()), units = uint64_t{groups->groups} * c->kv_heads, own_units = uint64_t{t->seqs} * c->kv_heads;
     // rows of a key head over 8192 and 32768 tokens of 8 of them, by tiles of 16 rows and of 128: 16 rows 16, 24 and 20, 47 us; 32 rows 22, 37 and 20, 47;
     // 40 rows 29, 51 and 21, 48; in fp32 over 8192 32 rows 26 and 33, 64 rows 45 and 38
@@ -1204,7 +1205,8 @@ SharedShape shared_shape_of(const entro_cache *c, const entro_cache_table *t, co
     s.g.groups = groups->groups;
     s.g.row_tiles = s.many ? between((rows + kManyRows - 1) / kManyRows, 1, kHalfGroups / units) : 1;
     // own tokens: up to 24 tiles in one piece; of longer ones as many pieces of 8 tiles and more as give every compute unit a workgroup (64 sequences with
-    // up to 33 tiles of their own behind 32768 shared tokens: one piece 101 us at the best, two 94, four 94)
+    // up to 33 tiles of their own behind 32768 shared tokens: one piece 101 us at the best, two 94, four 94).  max_own says how many there may be: 32
+    // sequences with 100 of their own behind 32768 beside one of 32868 in no group 969 us by max_len less max_shared, 98 by max_own
     const bool own_many = s.many && own_rows > 32;
     s.g.own_tiles = own_many ? between((own_rows + kManyRows - 1) / kManyRows, 1, kHalfGroups / own_units) : 0;
     const uint64_t own_fill = own_many ? own_units * s.g.own_tiles : (own_units + 3) / 4;

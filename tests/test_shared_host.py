@@ -70,6 +70,22 @@ def test_nothing_given_sizes_of_no_launch_and_calls_without_rows():
     assert L.entro_cache_attend_shared(*refs, None, 0, None) == B.ENTRO_OK
 
 
+def test_own_tokens_are_split_by_their_own_hint():
+    """Parts of a row for tokens that a sequence has alone: by max_own where it is given, whatever max_shared says; no more than for all of max_len."""
+    L, (cache, table, query, groups) = B.lib(), good()
+    refs = [C.byref(x) for x in (cache, table, query, groups)]
+    query.max_len, groups.max_shared = 32868, 32768
+
+    def parts(max_own):
+        groups.max_own = max_own
+        need = L.entro_cache_attend_shared_workspace_bytes(*refs)
+        assert need % (query.tokens * query.q_heads * (128 + 1) * 4) == 0
+        return need // (query.tokens * query.q_heads * (128 + 1) * 4)
+    assert parts(0) == parts(100) < parts(20000) <= parts(32868) == parts((1 << 32) - 1) <= 256
+    groups.max_shared = (1 << 32) - 1
+    assert parts(0) == parts(1) < parts(32868) == parts((1 << 32) - 1) <= 256
+
+
 @pytest.mark.parametrize("call,tensor", [(call, tensor) for call, more in [("shared", []), ("attend_shared", ["q", "out", "lse", "start", "workspace"])]
                                          for tensor in [None, "pool.k", "pool.v", "pool.k_scale", "pool.v_scale", "slots", "lengths", "first", "shared"] + more])
 def test_calls_refuse_any_one_tensor_in_host_memory(calls_made, monkeypatch, call, tensor):  # noqa: F811
