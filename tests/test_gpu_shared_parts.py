@@ -1,12 +1,13 @@
-"""Attention behind shared prefixes where its work is cut finer, through the C ABI against the definition in 64 bits: own tokens in several parts.
-(Bounds as in test_gpu_shared.)"""
+"""Attention behind shared prefixes where its work is cut finer, through the C ABI against the definition in 64 bits: own tokens in several parts, row tiles
+of many rows over pages of 64 tokens and more, and what is shared after tokens were taken back. (Bounds as in test_gpu_shared.)"""
 import numpy as np
 import pytest
 import torch
 
+import cache_reference as ref
 import paper_2505_02380_amd as E
 from test_gpu_cache import TYPES, cache_of, check_attend, dev, ints, rounded, starts
-from test_gpu_shared import first_of, make
+from test_gpu_shared import first_of, make, run
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -51,3 +52,59 @@ def test_own_tokens_in_several_parts(case, window, sinks, kind):
         out.fill_(7), lse.fill_(7)
         E.entro_cache_attend_shared(cache, t, query, g, ws)
         check_attend(pool, table, lengths, q, start, kind, out, lse, dim ** -0.5, window, sinks)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("dim,page", [(128, 64), (64, 128), (80, 256), (192, 64)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (300, 70), (90, 0)])
+def test_row_tiles_whose_tiles_lie_in_one_page(window, sinks, dim, page, kind):
+    """Pages of 64 tokens and more, more than 32 rows a key head: windows within and over the shared tokens, pages that none of the group has and such
+    that are none, in the first, a middle and the last shared page; then without those."""
+    rng = np.random.default_rng(dim + page)
+    pool, table, lengths, shared = make(rng, [(1024, [1030 + 23 * i for i in range(13)]), (512, [520 + i for i in range(10)])], [100], 2, page, dim)
+    first, start = [0, 13, 23], starts([1] * 24)
+    q = rounded(rng.standard_normal((24, 8, dim)), kind)
+    out, lse = run(pool, table, lengths, first, shared, q, start, kind, window, sinks)
+    check_attend(pool, table, lengths, q, start, kind, out, lse, dim ** -0.5, window, sinks)
+    last = 1024 // page - 1
+    table[:13, 0], table[:13, last // 2], table[13:23, 512 // page - 1] = -1, pool.pages, -7
+    out, lse = run(pool, table, lengths, first, shared, q, start, kind, window, sinks)
+    check_attend(pool, table, lengths, q, start, kind, out, lse, dim ** -0.5, window, sinks)
+    table[:13, last] = pool.pages + 9
+    out, lse = run(pool, table, lengths, first, shared, q, start, kind, window, sinks)
+    check_attend(pool, table, lengths, q, start, kind, out, lse, dim ** -0.5, window, sinks)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_what_is_shared_written_anew_after_tokens_were_taken_back(kind):
+    """Three beams behind 96 tokens; one gives up 70 of them and goes on with others. What they share is then 16 tokens, and attention by it is the definition's."""
+    rng = np.random.default_rng(13)
+    heads, dim, page, beams = 2, 64, 16, 3
+    cache = E.Cache.empty(1, 60, heads, page, dim, DEV)
+    for x in (cache.k_scale, cache.v_scale):
+        x.fill_(1.0)
+    tables = [E.CacheTable.empty(beams, 12, DEV) for _ in range(2)]
+    status = torch.zeros(4, dtype=torch.int32, device=DEV)
+    room = torch.empty(E.entro_cache_pages_workspace_bytes(cache, *tables), dtype=torch.uint8, device=DEV)
+    groups = E.CacheGroups(ints([0, beams]), torch.zeros(1, dtype=torch.int32, device=DEV), beams, 96)
+
+    def go_on(parent, grow, rows):
+        E.entro_cache_regroup(cache, tables[0], tables[1], status, room, parent=ints(parent), grow=ints(grow))
+        tables.reverse()
+        if sum(rows):
+            k, v = (dev(rng.standard_normal((sum(rows), heads, dim)).astype(np.float32)).to(TYPES[kind]) for _ in "kv")
+            E.entro_cache_append(cache, tables[0], E.CacheRows(k, v, ints(starts(rows)), max(rows)))
+        E.entro_cache_shared(cache, tables[0], groups)
+        assert status[0].item() == 0
+        return groups.shared.item()
+    go_on([0, -1, -1], [100, 0, 0], [100, 0, 0])
+    assert go_on([0, 0, 0], [1, 1, 1], [1, 1, 1]) == 96
+    assert go_on([0, 1, 2], [-71, 5, 5], [0, 5, 5]) == 16
+    assert go_on([0, 1, 2], [90, 5, 5], [90, 5, 5]) == 16
+    table, lengths = tables[0].slots.cpu().numpy(), tables[0].lengths.tolist()
+    assert lengths == [120, 111, 111]
+    pool = ref.Pool(rng, 1, cache.pages, heads, page, dim)
+    pool.k, pool.v, pool.k_scale, pool.v_scale = (x.cpu().numpy() for x in (cache.k, cache.v, cache.k_scale, cache.v_scale))
+    q = rounded(rng.standard_normal((3, 4, dim)), kind)
+    out, lse = run(pool, table, lengths, [0, beams], groups.shared.tolist(), q, starts([1] * 3), kind)
+    check_attend(pool, table, lengths, q, starts([1] * 3), kind, out, lse, dim ** -0.5)
