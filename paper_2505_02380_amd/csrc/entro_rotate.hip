@@ -10,14 +10,16 @@ using namespace entro_detail;
 
 constexpr int kWG = 256;
 // Heads that a lane group takes one after the other in large calls, with the angles of its position found once: 8192 rows of 40 heads of 128 in bf16,
-// four heads 41 us, eight 38; 4999 rows of 24 heads of 80 in fp32, four 26 us, eight 37 (152 registers).
-template <typename T> constexpr uint32_t kHeads = sizeof(T) == 2 ? 8 : 4;
-// A call is large from so many lanes on (one head a lane group and several: 40 heads of 128 in bf16, 1600 rows 13.6 and 15.2 us, 2400 18.5 and 17.5, 3200
-// 23.4 and 20.8; 24 heads of 80 in fp32, 3200 rows 18.6 and 21.1),
-template <typename T> constexpr uint64_t kManyLanes = sizeof(T) == 2 ? 64 * 2560 : 64 * 6144;
+// four heads 41 us, eight 38.  In fp32, bound by bytes sooner, one is as fast (one head and four: 24 heads of 80, 3000 rows 18.4 and 21.9 us, 5000 27.8
+// and 27.9, 12 000 56.7 and 54.7; 40 of 128, 3000 rows 22.8 and 22.2, 5000 34.3 and 35.4, 12 000 90.9 and 94.3).
+template <typename T> constexpr uint32_t kHeads = sizeof(T) == 2 ? 8 : 1;
+// A call is large from so many lanes on (one head a lane group and several: 40 heads of 128 in bf16 with a norm, 1600 rows 14.1 and 15.6 us, 3000 23.1 and
+// 21.2, 8000 52.3 and 44.5; without 12.5 and 10.6, 20.0 and 14.9, 44.4 and 30.4; 40 heads of 96 with a norm 15.0 and 19.5, 25.1 and 25.2, 57.9 and 55.6),
+constexpr uint64_t kManyLanes = 64 * 2560;
 // and from so many on the queries of rows for the cache have a launch of their own (32 query and 8 key heads of 128 in bf16, written and read, one launch and
-// two: 3200 rows 42.5 and 45 us, 6400 76 and 78, 12 800 160 and 131).
-constexpr uint64_t kApartLanes = 64 * 8192;
+// two: 3200 rows 42.5 and 45 us, 6400 76 and 78, 12 800 160 and 131; written alone in fp32, 4000 rows 39.7 and 41.1, 5600 53.0 and 52.1, 12 000 130.7 and
+// 115.4, of 24 and 4 heads of 96 32.4 and 34.5, 42.6 and 40.8, 92.6 and 72.1).
+template <typename T> constexpr uint64_t kApartLanes = sizeof(T) == 2 ? 64 * 8192 : 64 * 32768;
 constexpr float kLeastEps = 1.2e-38f;
 
 struct Turning {
@@ -491,7 +493,7 @@ Side side_of(const entro_rotary_rows *s, const float *gain, uint32_t gain_stride
 template <typename T, bool kPairs>
 void launch_rotate(const Turning &r, const Side &q, const Side &k, const int32_t *positions, uint32_t tokens, hipStream_t st) {
     const uint32_t heads = q.heads + k.heads, few = (heads + kHeads<T> - 1) / kHeads<T>;
-    const bool many = ((uint64_t{tokens} * few) << r.shift) >= kManyLanes<T>;
+    const bool many = ((uint64_t{tokens} * few) << r.shift) >= kManyLanes;
     const uint32_t per_token = many ? few : heads, items = tokens * per_token;
     const uint64_t groups = (uint64_t{items} + (kWG >> r.shift) - 1) / (kWG >> r.shift);
     const dim3 grid(static_cast<uint32_t>(groups < (1u << 23) ? groups : 1u << 23));
@@ -507,7 +509,7 @@ void launch_append(const Pool &p, const Rows &rows, const Turning &r, const Side
     g.cache_groups = groups < 65536 ? groups : 65536;
     if (q.heads) {
         const uint32_t few = (q.heads + kHeads<T> - 1) / kHeads<T>;
-        const bool many = ((uint64_t{rows.tokens} * few) << r.shift) >= kApartLanes;
+        const bool many = ((uint64_t{rows.tokens} * few) << r.shift) >= kApartLanes<T>;
         const uint32_t per_token = many ? few : q.heads;
         const uint64_t each = kWG >> r.shift, wanted = (most_new * per_token + each - 1) / each, fit = (1u << 23) / p.seqs;
         const uint32_t query_groups = wanted < 1 ? 1 : static_cast<uint32_t>(wanted < fit ? wanted : fit);
