@@ -7,6 +7,7 @@ import pytest
 import torch
 
 import cache_reference as ref
+import large_rows as large
 import paper_2505_02380_amd as E
 import rotary_reference as rot
 from paper_2505_02380_amd import binding as B
@@ -224,6 +225,28 @@ def test_centred_norm_of_heads_far_from_zero(host, dim):
     assert host.entro_rotate(C.byref(rotary), C.byref(side), None, at.ctypes.data, 1, dim, E.ENTRO_F32, None) == B.ENTRO_OK
     want, bound = rot.centred(x, eps)
     assert np.all(np.abs(y - want) <= bound), np.argwhere(~(np.abs(y - want) <= bound))[:4]
+
+
+def test_the_rows_of_large_calls_take_the_kernels_they_are_meant_for(host):
+    """The cases that the GPU tests of large calls have, by their launches: one head a lane group or several, queries with the cache's workgroups or apart."""
+    at, out = 1 << 16, (C.c_uint64 * 12)()
+    host.host_only_note(1)
+    host.host_launches(out, 12)
+    for kind, tokens, q_heads, kv_heads, dim, dims, each in large.ROTATE:
+        rotary = B.CRotary(at, None, None, 0, 0, dims, 0, 1, 1e-5, 1.0, 0)
+        q, k = (B.CRotaryRows(at, 2 * at, h * dim, dim, h * dim, dim, h, 0) if h else None for h in (q_heads, kv_heads))
+        assert host.entro_rotate(C.byref(rotary), C.byref(q), k and C.byref(k), at, tokens, dim, E.ENTRO_BF16 if kind == "bf16" else E.ENTRO_F32, None) == B.ENTRO_OK
+        assert host.host_launches(out, 12) == 3
+        assert out[1] == large.workgroups(tokens, q_heads + kv_heads, each, dim, dims), (kind, tokens)
+        assert large.workgroups(tokens, q_heads + kv_heads, 1, dim, dims) != large.workgroups(tokens, q_heads + kv_heads, 8, dim, dims)
+    for kind, q_heads, heads, dim, dims, page, new, apart in large.APPEND:
+        rotary, tokens = B.CRotary(at, None, None, 0, 0, dims, 0, 1, 1e-5, 1.0, 0), sum(new) + 1
+        cache, table = B.CCache(at, at, at, at, 1, 100, page, heads, dim, 0), B.CCacheTable(at, at, len(new), 5000)
+        q = B.CRotaryRows(at, 2 * at, q_heads * dim, dim, q_heads * dim, dim, q_heads, 0)
+        rows = B.CCacheRows(at, at, heads * dim, dim, heads * dim, dim, at, tokens, max(new), E.ENTRO_BF16 if kind == "bf16" else E.ENTRO_F32, 0)
+        assert host.entro_cache_append_rotated(C.byref(cache), C.byref(table), C.byref(rows), C.byref(rotary), C.byref(q), None) == B.ENTRO_OK
+        assert host.host_launches(out, 12) == (6 if apart else 3), (kind, new)
+    host.host_only_note(0)
 
 
 @pytest.mark.parametrize("first_wave", [0, 1, 3])
