@@ -462,7 +462,7 @@ __global__ __launch_bounds__(kWG, W > 128 ? 1 : 2) void k_attend_few(Pool p, Que
 // matrix units', as weights are two bf16 numbers). Left out one at a time, the second product takes 288 us with it, the first 202, the codes'
 // way to LDS 71. fp32 rows take twice the matrix instructions, and one workgroup a compute unit (382 registers at 96 dimensions): 98 row
 // groups of 4 key heads of 80 dimensions, each over about 1100 tokens, 182 us. Registers that do not fit are kept in memory: at 256 dimensions
-// 162 for fp32 and 30 for bf16, at 192 35 for fp32, at 96 and 128 2 and 5 for bf16.
+// 170 for fp32 and 37 for bf16, at 192 36 for fp32, at 96 and 128 2 and 4 for bf16.
 template <int W>
 struct ManyLds {
     static constexpr int kKeyRow = 2 * W + 16, kValueRow = 2 * kTile + 16;   // bytes
@@ -658,7 +658,10 @@ __device__ __forceinline__ void attend_many(const Pool &p, const Query &a, const
         }
         __syncthreads();
 
-        // What the matrix units take from LDS is asked for kAhead pieces before it is used.
+        // What the matrix units take from LDS is asked for kAhead pieces before it is used.  The first product tells the compiler so in groups (matrix
+        // instructions 8, LDS reads 256), as it otherwise moves each read to its use where registers are short: 1024 rows of 16 heads over 4096 tokens
+        // in bf16, 192 dimensions 173 and 165 us, 256 227 and 213, in fp32 96 dimensions 136 and 132, 128 153 and 148.  (The second product's reads
+        // in groups as well leave the weights' instructions behind one another: 167 and 220, 137 and 156 us.)
         constexpr int kAhead = 4;
         // the second product: weights of four times 16 tokens
         const auto add_values = [&](const bf16x8 (*weights)[kWeights], int half) {
@@ -688,12 +691,15 @@ __device__ __forceinline__ void attend_many(const Pool &p, const Query &a, const
                 bf16x8 k[kAhead];
 #pragma unroll
                 for (int j = 0; j < kAhead; ++j) k[j] = piece(j);
+                __builtin_amdgcn_sched_group_barrier(256, kAhead, 0);
 #pragma unroll
                 for (int j = 0; j < W / 8; ++j) {
                     const bf16x8 now = k[j % kAhead];
                     if (j + kAhead < W / 8) k[j % kAhead] = piece(j + kAhead);
 #pragma unroll
                     for (int n = 0; n < kParts; ++n) z[j & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(now, q[j >> 1][n], z[j & 1], 0, 0, 0);
+                    __builtin_amdgcn_sched_group_barrier(8, kParts, 0);
+                    if (j + kAhead < W / 8) __builtin_amdgcn_sched_group_barrier(256, 1, 0);
                 }
             }
             if (i + 1 < end) to_lds(half ^ 1);
