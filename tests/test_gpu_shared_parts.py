@@ -1,5 +1,5 @@
 """Attention behind shared prefixes where its work is cut finer, through the C ABI against the definition in 64 bits: own tokens in several parts, row tiles
-of many rows over pages of 64 tokens and more, and what is shared after tokens were taken back. (Bounds as in test_gpu_shared.)"""
+of many rows over pages of 64 tokens and more, what is shared after tokens were taken back, and long sums. (Bounds as in test_gpu_shared.)"""
 import numpy as np
 import pytest
 import torch
@@ -108,3 +108,20 @@ def test_what_is_shared_written_anew_after_tokens_were_taken_back(kind):
     q = rounded(rng.standard_normal((3, 4, dim)), kind)
     out, lse = run(pool, table, lengths, [0, beams], groups.shared.tolist(), q, starts([1] * 3), kind)
     check_attend(pool, table, lengths, q, starts([1] * 3), kind, out, lse, dim ** -0.5)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("seqs,group,shared,adds", [(2, 2, True, 256), (12, 4, True, 1024), (2, 2, False, 1024), (12, 4, False, 1024)])
+def test_small_weights_behind_a_large_one_are_not_lost(seqs, group, shared, adds, kind):
+    """65536 tokens, the first with a score of 16.875 and all others with 0: each of these has 0.39 of the first one's last place, and all together 0.3 %. In one
+    part, by tiles of 16 rows and of 128, as shared tokens and as own ones. `adds`: tiles that one lane adds up. With u = 2^-24: the score goes
+    through 8 roundings, the logarithms (up to 25, base 2) of part and join through 16, a lane's sum through one a tile and 40 within tiles and between lanes."""
+    tokens, heads, dim, page = 65536, 1, 64, 64
+    pool, table, lengths, _ = make(np.random.default_rng(14), [(tokens, [tokens] * seqs)], [], heads, page, dim)
+    pool.k[...], pool.v[...], pool.k_scale[...], pool.v_scale[...] = 128, 128, 2.0 ** -7, 1.0
+    pool.k[0, table[0, 0], 0, 0, 0] = 128 + 64
+    q = np.zeros((seqs, group, dim), np.float32)
+    q[..., 0] = 33.75
+    out, lse = run(pool, table, lengths, [0, seqs], [tokens - 64 if shared else 0], q, starts([1] * seqs), kind, max_shared=64 if shared else tokens, scale=1.0)
+    want = 16.875 + np.log1p((tokens - 1) * np.exp(-16.875))
+    assert np.abs(lse.cpu().numpy().astype(np.float64) - want).max() <= (8 * 16.875 + 16 * 25 + adds + 40) * 2.0 ** -24
