@@ -555,7 +555,7 @@ uint64_t entro_cache_codes_bytes(const entro_cache *c);
 entro_status entro_cache_append(const entro_cache *c, const entro_cache_table *t, const entro_cache_rows *r, void *hip_stream);
 
 /* entro_cache_append of keys that entro_rotate has normed and rotated in fp32 (no rounding between), at the positions of their rows; values
- * are written as they are.  q, or NULL: query rows of the same tokens and type, which are normed and rotated in the same launch (q->x to
+ * are written as they are.  q, or NULL: query rows of the same tokens and type, which are normed and rotated in the same call (q->x to
  * q->y, q->heads heads); rows that no sequence has are left alone.  Query rows are rotated wherever they stand, also before position 0 or where
  * there is no page.  Rows need no more than their elements' own alignment.  Writing the same rows again changes nothing in the cache.
  * (Eq. 1's grid map behind a rotation; no passage of the paper defines it.) */
@@ -611,8 +611,10 @@ uint64_t entro_cache_attend_shared_workspace_bytes(const entro_cache *c, const e
  * share are read and multiplied once for all its rows, each sequence's further tokens for its own, and both are joined by their lse.
  * shared[g] must not exceed what entro_cache_shared gives: its tokens are taken from the pages of the group's first sequence.  A query may stand
  * among the shared tokens (then fewer are taken as shared), windows may begin there, groups may be of one sequence or none.
- * The order of sums depends on sizes and lengths, never on the run.  ENTRO_ERR_SIZE also where groups or sequences times kv_heads reach
- * 2^23.  (For the phase of "Latency Reduction from Huffman Coding"; no passage of the paper defines it.) */
+ * The order of sums depends on sizes and lengths, never on the run.  It takes a launch more for the join: with fewer than some 1000 shared tokens
+ * (4000 for 17 to 32 rows a key head, 500 for 64 sequences) entro_cache_attend, which needs no groups, is as fast or faster.
+ * ENTRO_ERR_SIZE also where groups or sequences times kv_heads reach 2^23.  (For the phase of "Latency Reduction from Huffman Coding"; no
+ * passage of the paper defines it.) */
 entro_status entro_cache_attend_shared(const entro_cache *c, const entro_cache_table *t, const entro_cache_query *q, const entro_cache_groups *g,
                                        void *workspace, uint64_t workspace_bytes, void *hip_stream);
 

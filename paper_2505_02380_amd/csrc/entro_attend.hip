@@ -1211,8 +1211,10 @@ SharedShape shared_shape_of(const entro_cache *c, const entro_cache_table *t, co
     const uint64_t alone = groups->max_own < 1 ? q->max_len - shared : groups->max_own < q->max_len ? groups->max_own : q->max_len;
     const uint64_t tiles = tiles_in(shared, q, max_new), own_tiles = tiles_in(alone + kTile, q, max_new);
     const uint64_t cus = static_cast<uint64_t>(compute_units()), units = uint64_t{groups->groups} * c->kv_heads, own_units = uint64_t{t->seqs} * c->kv_heads;
-    // rows of a key head over 8192 and 32768 tokens of 8 of them, by tiles of 16 rows and of 128: 16 rows 16, 24 and 20, 47 us; 32 rows 22, 37 and 20, 47;
-    // 40 rows 29, 51 and 21, 48; in fp32 over 8192 32 rows 26 and 33, 64 rows 45 and 38
+    // rows of a key head over 1024, 4096, 8192 and 32768 shared tokens of 8 of them, with 30 own ones a sequence, by tiles of 16 rows and of 128, us: 20 rows
+    // 21, 22, 23, 38 and 14, 17, 21, 47; 32 rows 21, 22, 24, 39 and 15, 17, 22, 48; 40 rows 28, 29, 31, 53 and 15, 17, 22, 48; 64 rows 35, 37, 40, 69 and 16,
+    // 19, 24, 50; in fp32 32 rows 24, 26, 26, 42 and 18, 28, 34, 73; 40 rows 33, 34, 35, 55 and 18, 29, 36, 74; 64 rows 42, 44, 46, 72 and 19, 30, 38, 76.
+    // (The length is not looked at: up to 32 rows of prefixes below some 16384 tokens would be faster in bf16 by tiles of 128, 33 to 64 in fp32 of longer ones by those of 16.)
     s.many = rows > 32;
     s.g.groups = groups->groups;
     s.g.row_tiles = s.many ? between((rows + kManyRows - 1) / kManyRows, 1, kHalfGroups / units) : 1;
@@ -1230,7 +1232,8 @@ SharedShape shared_shape_of(const entro_cache *c, const entro_cache_table *t, co
     // shared tokens: one workgroup a compute unit, those for own tokens counted unless they are short, as two on one wait for each other's loads (48
     // sequences behind 4001 tokens, 96 workgroups for own tokens: 8, 10, 12, 24 pieces of the shared ones, 16 workgroups each, 31, 29, 35, 37 us); where that
     // leaves more than 16 tiles to a workgroup, two (64 behind 32768, 256 workgroups for own tokens: 8, 12, 16, 20, 32 pieces 151, 109, 94, 112, 107 us;
-    // without own tokens 147, 105, 84, 91, 72)
+    // without own tokens 147, 105, 84, 91, 72).  Short are 3 tiles and less; 3 and 7, with up to 280 tokens of their own: 16 sequences behind 8192 24 and 31 us,
+    // 48 behind 4001 27 and 31, 64 behind 2048 23 and 30, behind 8192 43 and 37, in fp32 29 and 42, behind 32768 198 and 135; over 296 such calls 3 is 2 % ahead
     const uint64_t slots = cus * (entro_cache_width(c->head_dim) > 128 || (s.many && q->type == ENTRO_F32) ? 1 : 2);
     const uint64_t own_blocks = own_fill * s.g.own_splits, fill = units * s.g.row_tiles;
     const auto leaves = [&](uint64_t room) { return own_blocks < room && own_tiles > 3 ? room - own_blocks : room; };
