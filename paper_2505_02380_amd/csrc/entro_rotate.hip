@@ -174,16 +174,19 @@ __device__ inline float other_part(float v) {
     else return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), STEP == 1 ? kSwap1 : STEP == 2 ? kSwap2 : STEP == 4 ? kHalfMirror : kMirror, 0xf, 0xf, true));
 }
 
-// v brought together over the lanes of a head by f.
-template <typename F>
-__device__ inline float over_head(float v, uint32_t shift, F f) {
-    if (shift > 0) v = f(v, other_part<1>(v));
-    if (shift > 1) v = f(v, other_part<2>(v));
-    if (shift > 2) v = f(v, other_part<4>(v));
-    if (shift > 3) v = f(v, other_part<8>(v));
-    if (shift > 4) v = f(v, other_part<16>(v));
-    if (shift > 5) v = f(v, other_part<32>(v));
-    return v;
+// N numbers, each brought together over the lanes of a head by f.
+template <int N, typename F>
+__device__ inline void over_head(float (&v)[N], uint32_t shift, F f) {
+    const auto step = [&](auto far) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = f(v[i], other_part<decltype(far)::value>(v[i]));
+    };
+    if (shift > 0) step(std::integral_constant<int, 1>{});
+    if (shift > 1) step(std::integral_constant<int, 2>{});
+    if (shift > 2) step(std::integral_constant<int, 4>{});
+    if (shift > 3) step(std::integral_constant<int, 8>{});
+    if (shift > 4) step(std::integral_constant<int, 16>{});
+    if (shift > 5) step(std::integral_constant<int, 32>{});
 }
 
 // The norm of a head, whose elements are x and, as they were read, raw.  All lanes are here.  Where the squares of some head of the wavefront leave the
@@ -194,31 +197,41 @@ __device__ inline void norm_head(const Turning &r, const Piece &c, const float *
     const auto here = [&](uint32_t j) { return j % P < c.count[j / P]; };
     const auto add = [](float a, float b) { return a + b; };
     const auto squares = [&]() {
+        const auto less = [&](float sum) {
+#pragma unroll
+            for (uint32_t j = 0; j < N; ++j) x[j] = here(j) ? fmaf(-sum, r.inverse_dim, x[j]) : 0.0f;
+        };
         if (r.norm == ENTRO_NORM_CENTRED) {
-            // twice: the rounded sum and inverse leave part of a mean that is large beside the elements' spread
+            float sum[1] = {0.0f};
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                float sum = 0.0f;
-#pragma unroll
-                for (uint32_t j = 0; j < N; ++j) sum += x[j];
-                sum = over_head(sum, r.shift, add);
-#pragma unroll
-                for (uint32_t j = 0; j < N; ++j) x[j] = here(j) ? fmaf(-sum, r.inverse_dim, x[j]) : 0.0f;
-            }
+            for (uint32_t j = 0; j < N; ++j) sum[0] += x[j];
+            over_head(sum, r.shift, add);
+            less(sum[0]);
         }
-        float sum = 0.0f;
+        float sums[2] = {0.0f, 0.0f};
 #pragma unroll
-        for (uint32_t j = 0; j < N; ++j) sum = fmaf(x[j], x[j], sum);
-        return over_head(sum, r.shift, add);
+        for (uint32_t j = 0; j < N; ++j) sums[0] = fmaf(x[j], x[j], sums[0]);
+        if (r.norm != ENTRO_NORM_CENTRED) {
+            float sum[1] = {sums[0]};
+            over_head(sum, r.shift, add);
+            return sum[0];
+        }
+        // Sum and inverse are rounded: of a mean that is large beside the elements' spread some is left.  It goes in the same pass as the squares.
+#pragma unroll
+        for (uint32_t j = 0; j < N; ++j) sums[1] += x[j];
+        over_head(sums, r.shift, add);
+        less(sums[1]);
+        const float sum = fmaf(-sums[1] * r.inverse_dim, sums[1], sums[0]);
+        return sum < 0.0f ? 0.0f : sum;
     };
     float sum = squares(), eps = r.eps;
     if (__any(!(sum < INFINITY))) {
         head_values<T>(raw, x);
-        float most = 0.0f;
+        float most[1] = {0.0f};
 #pragma unroll
-        for (uint32_t j = 0; j < N; ++j) most = fmaxf(most, fabsf(x[j]));
-        most = over_head(most, r.shift, [](float a, float b) { return fmaxf(a, b); });
-        const int e = !(sum < INFINITY) && most < INFINITY ? static_cast<int>(__float_as_uint(most) >> 23) - 127 : 0;
+        for (uint32_t j = 0; j < N; ++j) most[0] = fmaxf(most[0], fabsf(x[j]));
+        over_head(most, r.shift, [](float a, float b) { return fmaxf(a, b); });
+        const int e = !(sum < INFINITY) && most[0] < INFINITY ? static_cast<int>(__float_as_uint(most[0]) >> 23) - 127 : 0;
 #pragma unroll
         for (uint32_t j = 0; j < N; ++j) x[j] = ldexpf(x[j], -e);
         if (e) eps = fmaxf(ldexpf(eps, -2 * e), kLeastEps);

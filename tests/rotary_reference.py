@@ -56,11 +56,11 @@ def far_heads(rng, dim):
 def centred(x, eps):
     """(the centred norm alone, how far fp32 results may be off), also where the mean is far from zero. With D the mean |x - mean| and A the mean |x|: sum and
     product leave a mean that is off by 40 u A; the same again of what is left takes that away, off by 40 u (D + 40 u A) and three roundings
-    of elements of at most |x - mean| + 40 u A. An error of all elements moves their sum of squares as well; the factor is off by 24 u, the last
-    product by one."""
+    of elements of at most |x - mean| + 40 u A. An error of all elements moves their sum of squares as well; the factor is off by 24 u of what it is taken
+    of, the squares before that mean is taken away among them, and the last product by one."""
     x = x.astype(np.float64)
     off = x - x.mean(-1, keepdims=True)
     first = 40 * U * np.abs(x).mean(-1, keepdims=True)
     away = 40 * U * (np.abs(off).mean(-1, keepdims=True) + first) + 3 * U * (np.abs(off) + first)
     by = 1 / np.sqrt((off * off).mean(-1, keepdims=True) + eps)
-    return off * by, (away + np.abs(off) * (by * by * (np.abs(off) * away).mean(-1, keepdims=True) + 25 * U)) * by + 1e-37
+    return off * by, (away + np.abs(off) * (by * by * (np.abs(off) * away).mean(-1, keepdims=True) + 25 * U + 24 * U * (first * by) ** 2)) * by + 1e-37
