@@ -10,12 +10,14 @@ using namespace entro_detail;
 
 constexpr int kWG = 256;
 // Heads that a lane group takes one after the other in large calls, with the angles of its position found once: 8192 rows of 40 heads of 128 in bf16,
-// four heads 41 us, eight 38.  In fp32, bound by bytes sooner, one is as fast (one head and four: 24 heads of 80, 3000 rows 18.4 and 21.9 us, 5000 27.8
-// and 27.9, 12 000 56.7 and 54.7; 40 of 128, 3000 rows 22.8 and 22.2, 5000 34.3 and 35.4, 12 000 90.9 and 94.3).
-template <typename T> constexpr uint32_t kHeads = sizeof(T) == 2 ? 8 : 1;
+// four heads 41 us, eight 38.  In fp32 four, and only where a quarter and more of the lanes of a head have no elements: what they ask for at a time is less
+// (one head and four, memory not read before: 24 heads of 80, 5000 rows 25.2 and 22.1 us, 16 000 69.4 and 59.2, with a norm 31.7 and 29.1, 91.0 and 82.0; 28 of
+// 96, 8000 rows 44.8 and 42.0; 40 of 72 58.0 and 48.1; all lanes at work: 40 of 128, 5000 rows 41.1 and 44.8, 16 000 116.6 and 123.1, with a norm 46.9 and 49.6, 137
+// and 129; 28 of 112, 8000 rows 47.3 and 49.0).
+template <typename T> constexpr uint32_t kHeads = sizeof(T) == 2 ? 8 : 4;
 // A call is large from so many lanes on (one head a lane group and several: 40 heads of 128 in bf16 with a norm, 1600 rows 14.1 and 15.6 us, 3000 23.1 and
-// 21.2, 8000 52.3 and 44.5; without 12.5 and 10.6, 20.0 and 14.9, 44.4 and 30.4; 40 heads of 96 with a norm 15.0 and 19.5, 25.1 and 25.2, 57.9 and 55.6),
-constexpr uint64_t kManyLanes = 64 * 2560;
+// 21.2, 8000 52.3 and 44.5; without 12.5 and 10.6, 20.0 and 14.9, 44.4 and 30.4; 40 heads of 96 with a norm 15.0 and 19.5, 25.1 and 25.2, 57.9 and 55.6; in fp32 24 heads of 80, 3000 rows, 64 * 4500 lanes, 16.2 and 17.3),
+template <typename T> constexpr uint64_t kManyLanes = sizeof(T) == 2 ? 64 * 2560 : 64 * 6144;
 // and from so many on the queries of rows for the cache have a launch of their own (32 query and 8 key heads of 128 in bf16, written and read, one launch and
 // two: 3200 rows 42.5 and 45 us, 6400 76 and 78, 12 800 160 and 131; written alone in fp32, 4000 rows 39.7 and 41.1, 5600 53.0 and 52.1, 12 000 130.7 and
 // 115.4, of 24 and 4 heads of 96 32.4 and 34.5, 42.6 and 40.8, 92.6 and 72.1).
@@ -324,9 +326,9 @@ __device__ inline void rotate_queries(const Pool &p, const Rows &rows, const Tur
 // Query rows of sequences on their own, with many new rows: beside the cache's workgroups they would have the registers of those (26 800 rows of 32 query
 // and 8 key heads of 128: 302 us in one launch, 178 in two; 1600 rows of 24 and 4 heads of 96 in fp32: 24 in one, 33 in two).  Bound by bytes: 93 us
 // for those of the first, 4.7 TB/s.
-template <typename T, bool kPairs>
+template <typename T, bool kPairs, int HEADS>
 __global__ __launch_bounds__(kWG) void k_rotate_queries(Pool p, Rows rows, Turning r, Side q, uint32_t each, uint32_t per_token) {
-    rotate_queries<T, kPairs, kHeads<T>>(p, rows, r, q, blockIdx.x / each, blockIdx.x % each, each, per_token);
+    rotate_queries<T, kPairs, HEADS>(p, rows, r, q, blockIdx.x / each, blockIdx.x % each, each, per_token);
 }
 
 // The grid of k_append_rotated: workgroups for blocks of the cache, then some for the query rows of each sequence.
@@ -488,8 +490,14 @@ entro_status check_side(const entro_rotary_rows *s, uint32_t tokens, uint32_t ty
     return ENTRO_OK;
 }
 
+// Lanes that have elements of a head.
+uint32_t units_of(uint32_t half, uint32_t head_dim) { return (half + kRun - 1) / kRun + (head_dim - 2 * half + 2 * kRun - 1) / (2 * kRun); }
+
+// Whether several heads a lane group pay in a large call.
+template <typename T> bool heads_together(const Turning &r) { return sizeof(T) == 2 || 4 * units_of(r.half, r.head_dim) <= 3u << r.shift; }
+
 Turning turning_of(const entro_rotary *r, uint32_t head_dim) {
-    const uint32_t half = r->dims / 2, units = (half + kRun - 1) / kRun + (head_dim - r->dims + 2 * kRun - 1) / (2 * kRun);
+    const uint32_t half = r->dims / 2, units = units_of(half, head_dim);
     uint32_t shift = 0;
     while ((1u << shift) < units) ++shift;                   // at most 33 units
     return {r->turns, half, head_dim, r->norm, shift, r->eps, r->amplitude, 1.0f / static_cast<float>(head_dim)};
@@ -506,7 +514,7 @@ Side side_of(const entro_rotary_rows *s, const float *gain, uint32_t gain_stride
 template <typename T, bool kPairs>
 void launch_rotate(const Turning &r, const Side &q, const Side &k, const int32_t *positions, uint32_t tokens, hipStream_t st) {
     const uint32_t heads = q.heads + k.heads, few = (heads + kHeads<T> - 1) / kHeads<T>;
-    const bool many = ((uint64_t{tokens} * few) << r.shift) >= kManyLanes;
+    const bool many = heads_together<T>(r) && ((uint64_t{tokens} * few) << r.shift) >= kManyLanes<T>;
     const uint32_t per_token = many ? few : heads, items = tokens * per_token;
     const uint64_t groups = (uint64_t{items} + (kWG >> r.shift) - 1) / (kWG >> r.shift);
     const dim3 grid(static_cast<uint32_t>(groups < (1u << 23) ? groups : 1u << 23));
@@ -522,12 +530,15 @@ void launch_append(const Pool &p, const Rows &rows, const Turning &r, const Side
     g.cache_groups = groups < 65536 ? groups : 65536;
     if (q.heads) {
         const uint32_t few = (q.heads + kHeads<T> - 1) / kHeads<T>;
-        const bool many = ((uint64_t{rows.tokens} * few) << r.shift) >= kApartLanes<T>;
-        const uint32_t per_token = many ? few : q.heads;
+        const bool many = ((uint64_t{rows.tokens} * (sizeof(T) == 2 ? few : q.heads)) << r.shift) >= kApartLanes<T>, together = many && heads_together<T>(r);
+        const uint32_t per_token = together ? few : q.heads;
         const uint64_t each = kWG >> r.shift, wanted = (most_new * per_token + each - 1) / each, fit = (1u << 23) / p.seqs;
         const uint32_t query_groups = wanted < 1 ? 1 : static_cast<uint32_t>(wanted < fit ? wanted : fit);
-        if (many) {
-            hipLaunchKernelGGL((k_rotate_queries<T, kPairs>), dim3(query_groups * p.seqs), dim3(kWG), 0, st, p, rows, r, q, query_groups, per_token);
+        if (together) {
+            hipLaunchKernelGGL((k_rotate_queries<T, kPairs, kHeads<T>>), dim3(query_groups * p.seqs), dim3(kWG), 0, st, p, rows, r, q, query_groups, per_token);
+        } else if (many) {
+            if constexpr (sizeof(T) == 4)
+                hipLaunchKernelGGL((k_rotate_queries<T, kPairs, 1>), dim3(query_groups * p.seqs), dim3(kWG), 0, st, p, rows, r, q, query_groups, per_token);
         } else {
             g.query_groups = query_groups;
             g.per_token = per_token;
