@@ -908,11 +908,13 @@ __global__ __launch_bounds__(kWG) void k_attend_join_rows(Pool p, Query a) {
 // workgroups, and k_shared_join brings the parts of a row together.  What is shared is rounded down to whole tiles, and to
 // what all of the group's rows see where there is no window; the rest of it is taken as each sequence's own.
 //
-// Bound by issue for many rows of long prefixes: 64 sequences of 32 / 8 heads of 128 behind 32768 shared and up to 2048 own tokens 95 us (of
-// a compute unit's time vector instructions 48 %, matrix instructions 30 %; wavefronts wait for a third of theirs), the shared ones alone 72 (0.48 PFLOP/s; each sequence for
+// Bound by issue for many rows of long prefixes: 64 sequences of 32 / 8 heads of 128 behind 32768 shared and up to 2048 own tokens 89 to 93 us (of
+// a compute unit's time vector instructions 52 %, matrix instructions 32 %; wavefronts wait for a quarter of theirs), the shared ones alone 72 (0.48 PFLOP/s; each sequence for
 // itself, 64 of 32768 tokens and more, is 2.3 GB of codes).  Short ones are bound by the way to the first tile (bounds of
 // the group 3 us, queries, page and codes 4 to 5) and by 2.3 us a tile: 48 answers to 4001 tokens 25 us and 5 for the join.  fp32 rows: one
-// wavefront a SIMD, and three times the matrix instructions (five groups of pieces, 216 us).
+// wavefront a SIMD, and three times the matrix instructions (five groups of pieces, 216 us).  A kernel holds the bodies for shared and own tokens and, with
+// many rows, for both kinds of pages, which takes registers: 41 are kept in memory at 128 dimensions in bf16 (k_attend_many 4), 8 at 96, 56 at 256, in
+// fp32 43 at 192, 426 at 256.
 // A lane adds up a tile's weights before it adds them to its sum, which may hold a weight some 2^23 times as large: of 65536 tokens in one part, the first
 // with all but 0.3 % of the weight, the lse was 1.5e-3 off with one addition a token.
 struct Groups {
